@@ -472,6 +472,63 @@ const char *ep_strerror(int err);
 /* cudaError_t value of the most recent failed CUDA call in this process, 0 if none. */
 int ep_last_cuda_error(void);
 
+/*
+ * The experts' matrix products. After ep_group, the rows of expert e are
+ * x[expert_offsets[e] .. expert_offsets[e+1]) of the pair space; one call multiplies
+ * each segment with its expert's weights:
+ *   z[p] = x[p] W[e]^T + b[e]          y[p] = bf16( act(z[p]) (+ or *) operand[p] )
+ * x [rows][in_features], weight [num_experts][out_features][in_features], bias
+ * [num_experts][out_features] (may be NULL), operand and y [rows][out_features],
+ * all bf16 and 16-byte aligned; operand may be NULL; pre (may be NULL) receives
+ * bf16(z), which the gradient of an activation needs. Sums, bias, activation and
+ * operand are fp32, one rounding to bf16 at the end. A gated expert is two calls:
+ * u = x Wu^T, then silu(x Wg^T) * u with operand = u, EP_OPERAND_MUL.
+ * EP_ACT_GELU is z * Phi(z) (the error-function form).
+ *
+ * expert_offsets [num_experts+1] (device, int32) is ep_layout's array: it starts at
+ * 0 and does not decrease. `rows` is the capacity of the row buffers; rows from
+ * expert_offsets[num_experts] on are neither used nor written, whatever they hold;
+ * an offset past `rows` is cut there and sets EP_STATUS_CAPACITY in *status
+ * (device, may be NULL). Experts without rows cost nothing here.
+ * Limits: in_features and out_features multiples of 8, from 8 to 2^24 - 8;
+ * 1 <= num_experts <= 4096; 0 <= rows < 2^31. y, pre and operand may not overlap
+ * x or weight; operand may be y itself.
+ * Waits inside the kernel are bounded: one that ran out sets EP_STATUS_TIMEOUT.
+ */
+enum { EP_ACT_NONE = 0, EP_ACT_RELU = 1, EP_ACT_SILU = 2, EP_ACT_GELU = 3 };
+enum { EP_OPERAND_ADD = 0, EP_OPERAND_MUL = 1 };
+typedef struct {
+    int64_t rows;
+    int32_t in_features;
+    int32_t out_features;
+    int32_t num_experts;
+    int32_t activation; /* EP_ACT_*     */
+    int32_t operand_op; /* EP_OPERAND_* */
+} ep_matmul_t;
+int ep_expert_matmul(const ep_matmul_t *m, const void *x, const int32_t *expert_offsets, const void *weight,
+                     const void *bias, const void *operand, void *y, void *pre, int32_t *status, void *stream);
+
+/*
+ * The gradients of ep_expert_matmul for dy [rows][out_features] (bf16), from the
+ * x, weight, pre and operand of the forward call:
+ *   dz = dy * act'(pre) (* operand)    dx = dz W[e]      dweight[e] = sum_p dz[p]^T x[p]
+ *   dbias[e] = sum_p dz[p]             doperand = dy * act(pre)   (EP_OPERAND_MUL)
+ * Each of dx, dweight (bf16, the shapes of x and weight), dbias (fp32, [E][N]) and
+ * doperand (bf16) may be NULL and is then not computed. doperand is refused where
+ * the operand is added or absent: the gradient of an added operand is dy. pre may
+ * be NULL only for EP_ACT_NONE without doperand. dz is rounded to bf16 once, as
+ * the operand of two products whose sums are fp32; dbias is summed before that
+ * rounding. Experts without rows get zero dweight and dbias; rows from
+ * expert_offsets[num_experts] on are neither used nor written. No atomics: the
+ * same bits every time. workspace: ep_expert_matmul_backward_workspace_bytes()
+ * bytes (device, 256-byte aligned), uninitialised.
+ */
+size_t ep_expert_matmul_backward_workspace_bytes(const ep_matmul_t *m);
+int ep_expert_matmul_backward(const ep_matmul_t *m, const void *dy, const void *x, const int32_t *expert_offsets,
+                              const void *weight, const void *pre, const void *operand, void *dx, void *dweight,
+                              float *dbias, void *doperand, int32_t *status, void *workspace,
+                              size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -21,12 +21,15 @@ STATUS_CAPACITY = 2
 STATUS_TIMEOUT = 4
 PROBE_READ, PROBE_WRITE, PROBE_COPY, PROBE_MEMCPY = 0, 1, 2, 3
 HOST_DUPLEX, HOST_PER_PEER, HOST_LOCAL_ON_DEVICE = 1, 2, 4
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU = 0, 1, 2, 3
+OPERAND_ADD, OPERAND_MUL = 0, 1
 
 EXPORTS = [
     "ep_layout_workspace_bytes", "ep_layout", "ep_layout_ranks", "ep_layout_pairs", "ep_layout_static", "ep_layout_static_scratch_bytes", "ep_layout_dispatch", "ep_dispatch", "ep_combine", "ep_group",
     "ep_combine_partial", "ep_dense_allgather", "ep_dense_reduce_scatter",
     "ep_host_roundtrip", "ep_host_dispatch_per_sender", "ep_host_combine", "ep_wait_senders", "ep_post_flags", "ep_host_step_pipelined",
     "ep_dispatch_copy_engine", "ep_host_step_arena_bytes", "ep_host_step", "ep_status",
+    "ep_expert_matmul", "ep_expert_matmul_backward", "ep_expert_matmul_backward_workspace_bytes",
     "ep_probe_bandwidth", "ep_launch_count", "ep_strerror", "ep_last_cuda_error",
 ]
 
@@ -50,6 +53,11 @@ _LAYOUT_FIELDS = ["expert_counts", "expert_offsets", "rank_rows", "rank_row_offs
 
 class _Layout(ctypes.Structure):
     _fields_ = [(f, ctypes.c_void_p) for f in _LAYOUT_FIELDS]
+
+
+class _Matmul(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("in_features", ctypes.c_int32), ("out_features", ctypes.c_int32),
+                ("num_experts", ctypes.c_int32), ("activation", ctypes.c_int32), ("operand_op", ctypes.c_int32)]
 
 
 def lib() -> ctypes.CDLL:
@@ -91,6 +99,11 @@ def lib() -> ctypes.CDLL:
         L.ep_host_step.argtypes = [sp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.ep_host_step_pipelined.argtypes = [sp, vp, vp, vp, vp, vp, vp, sz, i32, vp, vp, vp, i32, vp]
         L.ep_host_step_pipelined.restype = i32
+        mp = ctypes.POINTER(_Matmul)
+        L.ep_expert_matmul.argtypes = [mp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.ep_expert_matmul_backward.argtypes = [mp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.ep_expert_matmul_backward_workspace_bytes.restype = sz
+        L.ep_expert_matmul_backward_workspace_bytes.argtypes = [mp]
         L.ep_status.argtypes = [vp, vp, vp]
         L.ep_probe_bandwidth.argtypes = [i32, vp, vp, sz, i32, vp, ctypes.POINTER(ctypes.c_double)]
         L.ep_launch_count.restype = i64
@@ -99,7 +112,7 @@ def lib() -> ctypes.CDLL:
         for name in ["ep_layout", "ep_dispatch", "ep_combine", "ep_group", "ep_dispatch_copy_engine",
                      "ep_combine_partial", "ep_dense_allgather", "ep_dense_reduce_scatter",
                      "ep_host_roundtrip", "ep_host_dispatch_per_sender", "ep_host_combine", "ep_wait_senders", "ep_post_flags",
-                     "ep_host_step", "ep_status", "ep_probe_bandwidth", "ep_last_cuda_error"]:
+                     "ep_host_step", "ep_expert_matmul", "ep_expert_matmul_backward", "ep_status", "ep_probe_bandwidth", "ep_last_cuda_error"]:
             getattr(L, name).restype = i32
         _lib = L
     return _lib
@@ -412,6 +425,88 @@ def ep_host_step_pipelined(x_host, topk_idx_host, topk_weights_host, y_host, are
                                         None if step_events is None else ctypes.cast(step_events.array, ctypes.c_void_p)),
            "ep_host_step_pipelined")
     return y_host
+
+
+def _matmul_args(rows, weight, expert_offsets, activation, operand_op) -> _Matmul:
+    _want(weight, torch.bfloat16, "weight"), _want(expert_offsets, torch.int32, "expert_offsets")
+    E, N, H = weight.shape
+    if expert_offsets.numel() != E + 1:
+        raise ValueError(f"expert_offsets must hold {E + 1} entries for {E} experts, got {expert_offsets.numel()}")
+    return _Matmul(int(rows), int(H), int(N), int(E), int(activation), int(operand_op))
+
+
+def _want_rows(t, rows, cols, name):
+    """A [rows, cols] bf16 tensor, or None."""
+    if t is not None:
+        _want(t, torch.bfloat16, name)
+        if tuple(t.shape) != (rows, cols):
+            raise ValueError(f"{name} must be [{rows}, {cols}], got {list(t.shape)}")
+
+
+def ep_expert_matmul(x, expert_offsets, weight, bias=None, activation=ACT_NONE, operand=None, operand_op=OPERAND_ADD, y=None,
+                     pre=None, status=None):
+    """y[p] = act(x[p] weight[e]^T + bias[e]) (+ or *) operand[p] for the rows p of expert e's segment of the pair space.
+    x [rows, in], weight [experts, out, in], bias [experts, out], operand, y and pre [rows, out], all bf16."""
+    m = _matmul_args(x.shape[0], weight, expert_offsets, activation, operand_op)
+    E, N, H = weight.shape
+    _want_rows(x, m.rows, H, "x"), _want_rows(operand, m.rows, N, "operand"), _want_rows(bias, E, N, "bias")
+    if y is None:
+        y = torch.empty(m.rows, N, dtype=torch.bfloat16, device=x.device)
+    _want_rows(y, m.rows, N, "y"), _want_rows(pre, m.rows, N, "pre")
+    _check(lib().ep_expert_matmul(ctypes.byref(m), _ptr(x), _ptr(expert_offsets), _ptr(weight), _ptr(bias), _ptr(operand), _ptr(y),
+                                  _ptr(pre), _ptr(status), _stream()), "ep_expert_matmul")
+    return y
+
+
+@dataclass
+class ExpertGrads:
+    """Gradients of `ep_expert_matmul` and the workspace of the call that computes them; None: not computed."""
+    dx: torch.Tensor
+    dweight: torch.Tensor
+    dbias: torch.Tensor
+    doperand: torch.Tensor
+    workspace: torch.Tensor
+
+
+def ep_expert_matmul_backward_workspace_bytes(rows, in_features, out_features, num_experts) -> int:
+    m = _Matmul(int(rows), int(in_features), int(out_features), int(num_experts), 0, 0)
+    return int(lib().ep_expert_matmul_backward_workspace_bytes(ctypes.byref(m)))
+
+
+def alloc_expert_grads(rows, in_features, out_features, num_experts, x=True, weight=True, bias=False, operand=False,
+                       device="cuda") -> ExpertGrads:
+    """Allocates the outputs and the workspace of `ep_expert_matmul_backward` (torch owns the memory)."""
+    def mk(wanted, *shape, dtype=torch.bfloat16):
+        return torch.empty(*shape, dtype=dtype, device=device) if wanted else None
+    nbytes = max(256, ep_expert_matmul_backward_workspace_bytes(rows, in_features, out_features, num_experts))
+    return ExpertGrads(mk(x, rows, in_features), mk(weight, num_experts, out_features, in_features),
+                       mk(bias, num_experts, out_features, dtype=torch.float32), mk(operand, rows, out_features),
+                       mk(True, nbytes, dtype=torch.uint8))
+
+
+def ep_expert_matmul_backward(dy, x, expert_offsets, weight, pre=None, activation=ACT_NONE, operand=None, operand_op=OPERAND_ADD,
+                              grads: ExpertGrads = None, status=None) -> ExpertGrads:
+    """The gradients of `ep_expert_matmul` for dy, written to the tensors that `grads` has (default: dx and dweight).
+    `pre` is what the forward call wrote; the gradient of an added operand is dy itself."""
+    m = _matmul_args(dy.shape[0], weight, expert_offsets, activation, operand_op)
+    E, N, H = weight.shape
+    if grads is None:
+        grads = alloc_expert_grads(m.rows, H, N, E, device=dy.device)
+    _want_rows(dy, m.rows, N, "dy"), _want_rows(x, m.rows, H, "x"), _want_rows(pre, m.rows, N, "pre")
+    _want_rows(operand, m.rows, N, "operand"), _want_rows(grads.dx, m.rows, H, "dx"), _want_rows(grads.doperand, m.rows, N, "doperand")
+    if grads.dweight is not None:
+        _want(grads.dweight, torch.bfloat16, "dweight")
+        if grads.dweight.shape != weight.shape:
+            raise ValueError(f"dweight must be {list(weight.shape)}, got {list(grads.dweight.shape)}")
+    if grads.dbias is not None:
+        _want(grads.dbias, torch.float32, "dbias")
+        if tuple(grads.dbias.shape) != (E, N):
+            raise ValueError(f"dbias must be [{E}, {N}], got {list(grads.dbias.shape)}")
+    _check(lib().ep_expert_matmul_backward(
+        ctypes.byref(m), _ptr(dy), _ptr(x), _ptr(expert_offsets), _ptr(weight), _ptr(pre), _ptr(operand), _ptr(grads.dx),
+        _ptr(grads.dweight), _ptr(grads.dbias), _ptr(grads.doperand), _ptr(status), _ptr(grads.workspace),
+        grads.workspace.numel(), _stream()), "ep_expert_matmul_backward")
+    return grads
 
 
 def ep_status(status: torch.Tensor) -> int:
