@@ -61,6 +61,7 @@ typedef enum {
 #define EP_STATUS_BAD_INDEX 1 /* an expert id outside [-1, E) was seen and masked */
 #define EP_STATUS_CAPACITY  2 /* a slot >= the buffer's row capacity was skipped  */
 #define EP_STATUS_TIMEOUT   4 /* ep_wait_senders gave up on at least one sender     */
+#define EP_STATUS_BAD_LOGIT 8 /* a router logit (or its biased score) was NaN or +inf; that expert was not picked */
 
 typedef struct {
     int32_t num_tokens;  /* T */
@@ -471,6 +472,76 @@ int64_t ep_launch_count(void);
 const char *ep_strerror(int err);
 /* cudaError_t value of the most recent failed CUDA call in this process, 0 if none. */
 int ep_last_cuda_error(void);
+
+/*
+ * The router (Section 2.1: a gate picks K of E experts for every token): the
+ * topk_idx and topk_weights tables that layout, dispatch and combine take, from
+ * logits [T][E] (device, fp32 or bf16, row-major).
+ *   score   EP_SCORE_SOFTMAX: exp(l_e) / sum over the token's experts
+ *           EP_SCORE_SIGMOID: 1 / (1 + exp(-l_e))
+ *   picks   the K largest l_e, or, with bias [E] (fp32, may be NULL), the K largest
+ *           score_e + bias_e; equal values by ascending expert id, -0 equal to +0;
+ *           topk_idx[t][k] in descending order
+ *   weight  scale * score of the pick (never with the bias), divided by the sum of
+ *           the token's K picked scores if renormalize is set (0 if that sum is 0)
+ * A logit of -inf masks an expert for that token. NaN and +inf mask it too and set
+ * EP_STATUS_BAD_LOGIT in *status (device, may be NULL; bits are OR-ed in). Where
+ * fewer than K experts are left, the rest of the row is -1 with weight 0, which
+ * every later call skips. All arithmetic is fp32.
+ *
+ * balance (may be NULL): the balance loss over the same pass,
+ *   f_e = E * expert_counts[e] / sum(expert_counts)
+ *   mean_probs[e] = mean over the tokens with a pick of p_e (softmax: the score;
+ *                   sigmoid: the score over the sum of the token's scores)
+ *   loss = balance_coef * sum_e f_e * mean_probs[e]
+ * with expert_counts the valid picks per expert and tokens the tokens with a pick
+ * (all 0, and loss 0, where there is none). Every sum has a fixed order: the same
+ * bits every time. It needs a workspace of ep_route_workspace_bytes() bytes
+ * (device, 16-byte aligned, uninitialised); without balance none.
+ *
+ * ep_balance_loss computes the same from a routing table that is already there
+ * (entries -1 are skipped, ids outside [-1, E) too, with EP_STATUS_BAD_INDEX; a
+ * token without a valid pick or without an unmasked logit is not counted).
+ * Limits: T >= 0, T*K < 2^31, 1 <= K <= 32, 1 <= E <= 4096.
+ */
+enum { EP_DTYPE_F32 = 0, EP_DTYPE_BF16 = 1 };
+enum { EP_SCORE_SOFTMAX = 0, EP_SCORE_SIGMOID = 1 };
+typedef struct {
+    int32_t num_tokens;
+    int32_t num_experts;
+    int32_t top_k;
+    int32_t logits_dtype; /* EP_DTYPE_*  */
+    int32_t scoring;      /* EP_SCORE_*  */
+    int32_t renormalize;  /* 0 or 1      */
+    float scale;          /* of the weights */
+    float balance_coef;
+} ep_router_t;
+typedef struct { /* device pointers to caller-allocated arrays */
+    int32_t *expert_counts; /* [E] */
+    int32_t *tokens;        /* [1] */
+    float *mean_probs;      /* [E] */
+    float *loss;            /* [1] */
+} ep_balance_t;
+size_t ep_route_workspace_bytes(const ep_router_t *router);
+int ep_route(const ep_router_t *router, const void *logits, const float *bias, int32_t *topk_idx,
+             float *topk_weights, const ep_balance_t *balance, int32_t *status, void *workspace,
+             size_t workspace_bytes, void *stream);
+int ep_balance_loss(const ep_router_t *router, const void *logits, const int32_t *topk_idx,
+                    const ep_balance_t *balance, int32_t *status, void *workspace, size_t workspace_bytes,
+                    void *stream);
+
+/*
+ * Gradient with respect to the logits (their type, [T][E], every element written):
+ * of the weights for d_weights [T][K] (fp32, may be NULL), plus of the loss for
+ * d_loss [1] (fp32, device) where balance is given (its expert_counts and tokens
+ * are read; the counts are constants of the loss). topk_idx is what ep_route wrote
+ * (a token's picks are distinct) or, for the loss alone, the table ep_balance_loss
+ * was given. The selection and its bias have no gradient. Masked logits, and the
+ * whole rows of tokens without a pick, get 0.
+ */
+int ep_route_backward(const ep_router_t *router, const void *logits, const int32_t *topk_idx,
+                      const float *d_weights, const ep_balance_t *balance, const float *d_loss, void *dlogits,
+                      void *stream);
 
 /*
  * The experts' matrix products. After ep_group, the rows of expert e are

@@ -19,6 +19,9 @@ _lib = None
 STATUS_BAD_INDEX = 1
 STATUS_CAPACITY = 2
 STATUS_TIMEOUT = 4
+STATUS_BAD_LOGIT = 8
+DTYPE_F32, DTYPE_BF16 = 0, 1
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
 PROBE_READ, PROBE_WRITE, PROBE_COPY, PROBE_MEMCPY = 0, 1, 2, 3
 HOST_DUPLEX, HOST_PER_PEER, HOST_LOCAL_ON_DEVICE = 1, 2, 4
 ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU = 0, 1, 2, 3
@@ -29,6 +32,7 @@ EXPORTS = [
     "ep_combine_partial", "ep_dense_allgather", "ep_dense_reduce_scatter",
     "ep_host_roundtrip", "ep_host_dispatch_per_sender", "ep_host_combine", "ep_wait_senders", "ep_post_flags", "ep_host_step_pipelined",
     "ep_dispatch_copy_engine", "ep_host_step_arena_bytes", "ep_host_step", "ep_status",
+    "ep_route", "ep_route_backward", "ep_route_workspace_bytes", "ep_balance_loss",
     "ep_expert_matmul", "ep_expert_matmul_backward", "ep_expert_matmul_backward_workspace_bytes",
     "ep_probe_bandwidth", "ep_launch_count", "ep_strerror", "ep_last_cuda_error",
 ]
@@ -53,6 +57,19 @@ _LAYOUT_FIELDS = ["expert_counts", "expert_offsets", "rank_rows", "rank_row_offs
 
 class _Layout(ctypes.Structure):
     _fields_ = [(f, ctypes.c_void_p) for f in _LAYOUT_FIELDS]
+
+
+class _Router(ctypes.Structure):
+    _fields_ = [("num_tokens", ctypes.c_int32), ("num_experts", ctypes.c_int32), ("top_k", ctypes.c_int32),
+                ("logits_dtype", ctypes.c_int32), ("scoring", ctypes.c_int32), ("renormalize", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("balance_coef", ctypes.c_float)]
+
+
+_BALANCE_FIELDS = ["expert_counts", "tokens", "mean_probs", "loss"]
+
+
+class _Balance(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_void_p) for f in _BALANCE_FIELDS]
 
 
 class _Matmul(ctypes.Structure):
@@ -99,7 +116,12 @@ def lib() -> ctypes.CDLL:
         L.ep_host_step.argtypes = [sp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.ep_host_step_pipelined.argtypes = [sp, vp, vp, vp, vp, vp, vp, sz, i32, vp, vp, vp, i32, vp]
         L.ep_host_step_pipelined.restype = i32
-        mp = ctypes.POINTER(_Matmul)
+        rp, bp, mp = ctypes.POINTER(_Router), ctypes.POINTER(_Balance), ctypes.POINTER(_Matmul)
+        L.ep_route_workspace_bytes.restype = sz
+        L.ep_route_workspace_bytes.argtypes = [rp]
+        L.ep_route.argtypes = [rp, vp, vp, vp, vp, bp, vp, vp, sz, vp]
+        L.ep_balance_loss.argtypes = [rp, vp, vp, bp, vp, vp, sz, vp]
+        L.ep_route_backward.argtypes = [rp, vp, vp, vp, bp, vp, vp, vp]
         L.ep_expert_matmul.argtypes = [mp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
         L.ep_expert_matmul_backward.argtypes = [mp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.ep_expert_matmul_backward_workspace_bytes.restype = sz
@@ -112,7 +134,7 @@ def lib() -> ctypes.CDLL:
         for name in ["ep_layout", "ep_dispatch", "ep_combine", "ep_group", "ep_dispatch_copy_engine",
                      "ep_combine_partial", "ep_dense_allgather", "ep_dense_reduce_scatter",
                      "ep_host_roundtrip", "ep_host_dispatch_per_sender", "ep_host_combine", "ep_wait_senders", "ep_post_flags",
-                     "ep_host_step", "ep_expert_matmul", "ep_expert_matmul_backward", "ep_status", "ep_probe_bandwidth", "ep_last_cuda_error"]:
+                     "ep_host_step", "ep_route", "ep_balance_loss", "ep_route_backward", "ep_expert_matmul", "ep_expert_matmul_backward", "ep_status", "ep_probe_bandwidth", "ep_last_cuda_error"]:
             getattr(L, name).restype = i32
         _lib = L
     return _lib
@@ -425,6 +447,121 @@ def ep_host_step_pipelined(x_host, topk_idx_host, topk_weights_host, y_host, are
                                         None if step_events is None else ctypes.cast(step_events.array, ctypes.c_void_p)),
            "ep_host_step_pipelined")
     return y_host
+
+
+@dataclass(frozen=True)
+class Router:
+    """How logits become picks and weights (`ep_router_t` without the batch)."""
+    num_experts: int
+    top_k: int
+    scoring: int = SCORE_SOFTMAX
+    renormalize: bool = True
+    scale: float = 1.0
+    balance_coef: float = 0.0
+
+    def _struct(self, logits) -> _Router:
+        if logits.dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError(f"logits must be float32 or bfloat16, got {logits.dtype}")
+        if logits.dim() != 2 or logits.shape[1] != self.num_experts:
+            raise ValueError(f"logits must be [T, {self.num_experts}], got {list(logits.shape)}")
+        return _Router(logits.shape[0], self.num_experts, self.top_k, DTYPE_F32 if logits.dtype == torch.float32 else DTYPE_BF16,
+                       int(self.scoring), int(bool(self.renormalize)), float(self.scale), float(self.balance_coef))
+
+
+@dataclass
+class Routing:
+    """Device tensors written by `ep_route`; the last five only with a balance loss (None otherwise)."""
+    topk_idx: torch.Tensor            # [T, K] int32
+    topk_weights: torch.Tensor        # [T, K] fp32
+    status: torch.Tensor              # [1] int32, bits OR-ed in
+    expert_counts: torch.Tensor = None   # [E] int32
+    tokens: torch.Tensor = None          # [1] int32
+    mean_probs: torch.Tensor = None      # [E] fp32
+    loss: torch.Tensor = None            # [1] fp32
+    workspace: torch.Tensor = None
+
+    def _balance(self):
+        if self.expert_counts is None:
+            return None
+        return ctypes.byref(_Balance(*[getattr(self, f).data_ptr() for f in _BALANCE_FIELDS]))
+
+
+def ep_route_workspace_bytes(T, K, E) -> int:
+    return int(lib().ep_route_workspace_bytes(ctypes.byref(_Router(int(T), int(E), int(K), 0, 0, 0, 1.0, 0.0))))
+
+
+def alloc_routing(T, E, K, balance=False, topk_idx=None, device="cuda") -> Routing:
+    """Allocates the outputs of `ep_route` (torch owns the memory); balance: with those of the balance loss."""
+    def mk(dtype, *shape):
+        return torch.empty(*shape, dtype=dtype, device=device)
+    r = Routing(mk(torch.int32, T, K) if topk_idx is None else topk_idx, mk(torch.float32, T, K) if topk_idx is None else None,
+                torch.zeros(1, dtype=torch.int32, device=device))
+    if balance:
+        r.expert_counts, r.tokens = mk(torch.int32, E), mk(torch.int32, 1)
+        r.mean_probs, r.loss = mk(torch.float32, E), mk(torch.float32, 1)
+        r.workspace = mk(torch.uint8, max(16, ep_route_workspace_bytes(T, K, E)))
+    return r
+
+
+def _want_table(t, shape, dtype, name):
+    if t is not None:
+        _want(t, dtype, name)
+        if tuple(t.shape) != shape:
+            raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+
+
+def _check_routing(r: Routing, T, E, K, weights=True):
+    _want_table(r.topk_idx, (T, K), torch.int32, "topk_idx"), _want_table(r.status, (1,), torch.int32, "status")
+    if weights:
+        _want_table(r.topk_weights, (T, K), torch.float32, "topk_weights")
+    _want_table(r.expert_counts, (E,), torch.int32, "expert_counts"), _want_table(r.tokens, (1,), torch.int32, "tokens")
+    _want_table(r.mean_probs, (E,), torch.float32, "mean_probs"), _want_table(r.loss, (1,), torch.float32, "loss")
+
+
+def ep_route(logits: torch.Tensor, router: Router, bias: torch.Tensor = None, out: Routing = None) -> Routing:
+    """topk_idx and topk_weights [T, K] of logits [T, E] (fp32 or bf16); with an `out` that has them, expert counts, mean
+    probabilities and the balance loss too. bias [E] (fp32) takes part in the selection only."""
+    st = router._struct(logits)
+    T, E, K = st.num_tokens, st.num_experts, st.top_k
+    if out is None:
+        out = alloc_routing(T, E, K, balance=router.balance_coef != 0.0, device=logits.device)
+    _check_routing(out, T, E, K), _want_table(bias, (E,), torch.float32, "bias")
+    _check(lib().ep_route(ctypes.byref(st), _ptr(logits), _ptr(bias), _ptr(out.topk_idx), _ptr(out.topk_weights), out._balance(),
+                          _ptr(out.status), _ptr(out.workspace), 0 if out.workspace is None else out.workspace.numel(),
+                          _stream()), "ep_route")
+    return out
+
+
+def ep_balance_loss(logits: torch.Tensor, router: Router, topk_idx: torch.Tensor, out: Routing = None) -> Routing:
+    """Expert counts, mean probabilities and the balance loss for a routing table that is already there."""
+    st = router._struct(logits)
+    T, E, K = st.num_tokens, st.num_experts, st.top_k
+    if out is None:
+        out = alloc_routing(T, E, K, balance=True, topk_idx=topk_idx, device=logits.device)
+    _want_table(topk_idx, (T, K), torch.int32, "topk_idx"), _check_routing(out, T, E, K, weights=False)
+    if out.expert_counts is None:
+        raise ValueError("ep_balance_loss needs a Routing allocated with balance=True")
+    _check(lib().ep_balance_loss(ctypes.byref(st), _ptr(logits), _ptr(topk_idx), out._balance(), _ptr(out.status),
+                                 _ptr(out.workspace), out.workspace.numel(), _stream()), "ep_balance_loss")
+    return out
+
+
+def ep_route_backward(logits: torch.Tensor, router: Router, routing: Routing, d_weights: torch.Tensor = None,
+                      d_loss: torch.Tensor = None, dlogits: torch.Tensor = None) -> torch.Tensor:
+    """Gradient of the weights (for d_weights [T, K]) and of the balance loss (for d_loss [1]), either or both, with respect
+    to the logits; in the logits' type."""
+    st = router._struct(logits)
+    T, E, K = st.num_tokens, st.num_experts, st.top_k
+    if dlogits is None:
+        dlogits = torch.empty_like(logits)
+    _check_routing(routing, T, E, K, weights=False), _want_table(d_weights, (T, K), torch.float32, "d_weights")
+    _want_table(d_loss, (1,), torch.float32, "d_loss"), _want_table(dlogits, (T, E), logits.dtype, "dlogits")
+    if d_loss is not None and routing.expert_counts is None:
+        raise ValueError("the gradient of the balance loss needs the Routing that holds its counts")
+    _check(lib().ep_route_backward(ctypes.byref(st), _ptr(logits), _ptr(routing.topk_idx), _ptr(d_weights),
+                                   routing._balance() if d_loss is not None else None, _ptr(d_loss), _ptr(dlogits), _stream()),
+           "ep_route_backward")
+    return dlogits
 
 
 def _matmul_args(rows, weight, expert_offsets, activation, operand_op) -> _Matmul:
