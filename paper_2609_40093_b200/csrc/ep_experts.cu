@@ -27,11 +27,14 @@ namespace {
 
 enum { kForward = 0, kDx = 1, kDweight = 2 };
 
-constexpr int kThreads = 256;
+constexpr int kEpilogueWarps = 8;         // two per quarter of the lanes, taking turns at blocks of 32 columns
+constexpr int kThreads = 128 + 32 * kEpilogueWarps;
 constexpr int kTileM = 128;               // lanes of one CTA
 constexpr int kTileK = 64;                // contracted elements per stage: one 128-byte line
 constexpr int kAccColumns = 256;          // columns of one of the two accumulators
 constexpr int kBytesA = kTileM * kTileK * 2;
+constexpr int kStageLd = 36, kStageWords = 16 * kStageLd;      // an epilogue warp's buffer: 16 columns of 32 lanes
+constexpr int kStageBytes = kEpilogueWarps * kStageWords * 4;
 constexpr int kMaxStages = 12;
 constexpr int kSmemLimit = 227 * 1024;
 
@@ -49,6 +52,12 @@ struct ProductArgs {
     const uint16_t *bias, *operand;
     uint16_t *pre;
     int activation, operand_op;
+};
+
+// The column operand's boxes: of 128, 64, 32 and 16 rows where it is K-major, so that a tile's columns (a multiple of 16) are
+// fetched in at most five copies and no row more; box[0] alone (64 x 64) where it is MN-major.
+struct ColumnMaps {
+    CUtensorMap box[4];
 };
 
 struct Tile {
@@ -86,35 +95,37 @@ __device__ __forceinline__ float act_slope(int act, float z)
     }
 }
 
-__device__ __forceinline__ float bf16_value(uint16_t u) { return __uint_as_float((uint32_t)u << 16); }
-__device__ __forceinline__ uint16_t bf16_bits(float v) { return __bfloat16_as_ushort(__float2bfloat16_rn(v)); }
-
 // ---- the walk over tiles -----------------------------------------------------------------------------------------
 
+// Tiles are dealt out to the CTAs (pairs) round by round, an expert's row pieces next to each other, then its feature tiles: what
+// runs at the same time shares rows and weights in L2. Neither experts sorted by cost nor a shared counter was faster, with
+// segments of even and of Zipf-distributed lengths (counter: 3 to 6 % slower; order: within 2 % either way).
 template <int MODE, int CG>
 struct Walk {
     const ProductArgs &a;
     const int *first_tile;   // [E+1] shared memory: tiles of the experts before e (forward, dx)
-    const int *bound;        // [E+1] shared memory: the segments' bounds, clamped
-    int m_tiles, n_tiles, total;
+    const int *bound;        // [E+1] the segments' bounds, clamped
+    int m_tiles, n_tiles, total, tile, step;
 
-    __device__ Walk(const ProductArgs &args, const int *first, const int *b) : a(args), first_tile(first), bound(b)
+    __device__ Walk(const ProductArgs &args, const int *first, const int *b, int start, int stride)
+        : a(args), first_tile(first), bound(b), tile(start), step(stride)
     {
         m_tiles = (a.M + kTileM * CG - 1) / (kTileM * CG);
         n_tiles = MODE == kDweight ? (a.N + a.columns - 1) / a.columns : 0;
         total = MODE == kDweight ? a.E * m_tiles * n_tiles : first_tile[a.E];
     }
 
-    __device__ bool get(int tile, Tile &t) const
+    // This CTA's next tile; false when there is none left.
+    __device__ bool next(Tile &t)
     {
         if (tile >= total) return false;
         constexpr int kStep = 16 * CG;
         if (MODE == kDweight) {
             const int per = m_tiles * n_tiles;
             t.e = tile / per;
-            const int r = tile - t.e * per;
-            t.m0 = (r / n_tiles) * kTileM * CG;
-            t.c0 = (r % n_tiles) * a.columns;
+            const int r = tile - t.e * per, m = r / n_tiles;
+            t.m0 = m * kTileM * CG;
+            t.c0 = (r - m * n_tiles) * a.columns;
             t.cols = min(a.columns, a.N - t.c0);
             t.k0 = bound[t.e];
             t.nk = (max(0, bound[t.e + 1] - t.k0) + kTileK - 1) / kTileK;
@@ -126,44 +137,77 @@ struct Walk {
             }
             t.e = lo;
             const int r = tile - first_tile[lo], begin = bound[lo], count = bound[lo + 1] - begin;
-            const int pieces = (count + a.columns - 1) / a.columns;
+            const int pieces = (count + a.columns - 1) / a.columns, m = r / pieces, piece = r - m * pieces;
             const int width = ((count + pieces - 1) / pieces + kStep - 1) / kStep * kStep;   // equal pieces
-            const int piece = r % pieces;
-            t.m0 = (r / pieces) * kTileM * CG;
+            t.m0 = m * kTileM * CG;
             t.c0 = begin + piece * width;
             t.cols = max(0, min(width, count - piece * width));
             t.k0 = 0;
             t.nk = (a.K + kTileK - 1) / kTileK;
         }
         t.n = max(kStep, (t.cols + kStep - 1) / kStep * kStep);
+        tile += step;
         return true;
+    }
+};
+
+// Where a role stands in the ring of stages. Counted up, not divided: one thread issues all copies, one all products, and
+// a division by a run-time number of stages in either loop took longer than the products of a small tile.
+struct Ring {
+    uint32_t addr, base;
+    int stage, phase, stages, bytes;
+    __device__ Ring(uint32_t b, int stage_bytes, int n) : addr(b), base(b), stage(0), phase(0), stages(n), bytes(stage_bytes) {}
+    __device__ void next()
+    {
+        ++stage, addr += bytes;
+        if (stage == stages) stage = 0, phase ^= 1, addr = base;
+    }
+    __device__ void back()
+    {
+        if (stage == 0) stage = stages, phase ^= 1;
+        --stage;
     }
 };
 
 // ---- epilogues ---------------------------------------------------------------------------------------------------
 
-// One block of up to 32 columns of the forward product: rows p, p+1, ... of feature n.
-template <int ACT>
-__device__ __forceinline__ void store_forward(const ProductArgs &a, const uint32_t (&acc)[32], const uint16_t (&r)[32], float b, size_t at,
-                                              int cols)
+// A warp's 32 lanes x 32 columns of accumulators pass through shared memory, so that afterwards a lane holds 8 neighbouring
+// features of a column and reads and writes global memory 16 bytes at a time: the forward mode 16 columns of fp32 at a time,
+// the others, which do no more arithmetic, all 32 columns as rounded pairs. The pairs matter where the contracted axis is
+// short and a tile's epilogue takes as long as its products: shared memory feeds both, and with fp32 words the dweight mode
+// took 220 us at 128 experts of 1024 x 2048 and 32768 rows, with pairs 195. (Stored straight from the accumulators' order,
+// 2 bytes a lane, a column took ten instructions.) Rows are 36 words apart: 16-byte reads of eight lanes fall on all banks.
+__device__ __forceinline__ void unpack8(const uint4 &v, float (&f)[8])
 {
+    f[0] = bf16_lo(v.x), f[1] = bf16_hi(v.x), f[2] = bf16_lo(v.y), f[3] = bf16_hi(v.y);
+    f[4] = bf16_lo(v.z), f[5] = bf16_hi(v.z), f[6] = bf16_lo(v.w), f[7] = bf16_hi(v.w);
+}
+__device__ __forceinline__ uint4 pack8(const float (&f)[8])
+{
+    return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
+}
+
+// z (8 features of one row) -> y, and pre if asked for.
+template <int ACT>
+__device__ __forceinline__ void finish8(const ProductArgs &a, float (&z)[8], const uint4 &operand, size_t at)
+{
+    if (a.pre) *reinterpret_cast<uint4 *>(a.pre + at) = pack8(z);
 #pragma unroll
-    for (int c = 0; c < 32; ++c) {
-        if (c < cols) {
-            const float z = __uint_as_float(acc[c]) + b;
-            float v = act_value(ACT, z);
-            if (a.operand) v = a.operand_op == EP_OPERAND_MUL ? v * bf16_value(r[c]) : v + bf16_value(r[c]);
-            if (a.pre) a.pre[at + (size_t)c * a.M] = bf16_bits(z);
-            a.out[at + (size_t)c * a.M] = bf16_bits(v);
-        }
+    for (int i = 0; i < 8; ++i) z[i] = act_value(ACT, z[i]);
+    if (a.operand) {
+        float r[8];
+        unpack8(operand, r);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] = a.operand_op == EP_OPERAND_MUL ? z[i] * r[i] : z[i] + r[i];
     }
+    *reinterpret_cast<uint4 *>(a.out + at) = pack8(z);
 }
 
 // ---- the kernel --------------------------------------------------------------------------------------------------
 
 template <int MODE, int CG>
 __global__ void __launch_bounds__(kThreads, 1)
-product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b)
+product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ ColumnMaps map_b)
 {
     extern __shared__ char raw[];
     __shared__ uint64_t full_[kMaxStages], empty_[kMaxStages], acc_full_[2], acc_empty_[2];
@@ -172,13 +216,13 @@ product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, c
     __shared__ int warp_sum[kThreads / 32];
     volatile int *gave_up = &gave_up_;
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(kFullMask, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;   // uniform in the warp, and seen to be
     const uint32_t rank = CG == 2 ? cluster_rank() : 0;
     const int b_bytes = max(32, a.columns / CG) * kTileK * 2;
     const int stage_bytes = kBytesA + b_bytes;
-    const uint32_t ring = (smem_addr(raw) + 1023) & ~1023u;
-    char *tables = raw + (ring - smem_addr(raw)) + (size_t)a.stages * stage_bytes;
-    int *first_tile = reinterpret_cast<int *>(tables), *bound = first_tile + a.E + 1;
+    const uint32_t ring_base = (smem_addr(raw) + 1023) & ~1023u;
+    char *tables = raw + (ring_base - smem_addr(raw)) + (size_t)a.stages * stage_bytes;
+    int *first_tile = reinterpret_cast<int *>(tables + kStageBytes), *bound = first_tile + a.E + 1;   // the epilogue's buffers first
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < a.stages; ++s) {
@@ -187,18 +231,23 @@ product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, c
         }
         for (int s = 0; s < 2; ++s) {
             bar_init(smem_addr(&acc_full_[s]), 1);
-            bar_init(smem_addr(&acc_empty_[s]), 4 * CG);
+            bar_init(smem_addr(&acc_empty_[s]), kEpilogueWarps * CG);
         }
         gave_up_ = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 2) tmem_alloc<CG>(smem_addr(&tmem_slot), 2 * kAccColumns);
 
-    // the segments' bounds and, where tiles follow the segments, the experts' first tiles: each thread sums a run of experts
+    pdl_trigger();
+    pdl_wait();                                                              // nothing is read or written before this
+    // the segments' bounds and, where tiles follow the segments, the experts' first tiles
     for (int e = threadIdx.x; e <= a.E; e += kThreads) bound[e] = segment_bound(__ldg(a.offsets + e), a.rows);
     if (threadIdx.x == 0 && blockIdx.x == 0 && a.status && __ldg(a.offsets + a.E) > a.rows) atomicOr(a.status, EP_STATUS_CAPACITY);
+    if (MODE == kDweight)                                                    // once for all maps: a fence in front of every tile stalled the copies
+        for (int i = threadIdx.x; i < 2 * a.E; i += kThreads)
+            asm volatile("fence.proxy.tensormap::generic.acquire.gpu [%0], 128;" ::"l"(a.segment_maps + i) : "memory");
     __syncthreads();
-    if (MODE != kDweight) {
+    if (MODE != kDweight) {                                                  // each thread sums a run of experts
         const int m_tiles = (a.M + kTileM * CG - 1) / (kTileM * CG);
         const int per = (a.E + kThreads - 1) / kThreads, from = min(a.E, (int)threadIdx.x * per), to = min(a.E, from + per);
         int sum = 0;
@@ -223,34 +272,30 @@ product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, c
     __syncthreads();
     tmem_fence_after();
     const uint32_t tmem = tmem_slot;
-    const Walk<MODE, CG> walk(a, first_tile, bound);
-    const int start = blockIdx.x / CG, stride = gridDim.x / CG;
+    Walk<MODE, CG> walk(a, first_tile, bound, blockIdx.x / CG, gridDim.x / CG);   // one per role
+    const uint32_t full0 = smem_addr(full_), empty0 = smem_addr(empty_), full0_leader = CG == 2 ? in_cta(full0, 0) : full0;
     constexpr bool kAMn = MODE != kForward, kBMn = MODE == kDweight;
     Tile t;
 
-    if (warp == 0 && lane == 0) {
+    if (warp == 0 && elect_one()) {
         // ---- operands into the ring
-        int it = 0;
+        Ring ring(ring_base, stage_bytes, a.stages);
         bool ok = true;
-        for (int tile = start; ok && walk.get(tile, t); tile += stride) {
+        int sent = 0;
+        while (ok && walk.next(t)) {
             const int half = t.n / CG;                                       // columns this CTA brings
-            const int b_box = kBMn ? 64 : 32, boxes = (half + b_box - 1) / b_box;
-            const uint32_t bytes = CG * (kBytesA + boxes * b_box * kTileK * 2);
+            const int boxes = (half + 63) / 64;                              // MN-major
+            const uint32_t bytes = CG * (kBytesA + (kBMn ? boxes * 8192 : half * 128));
             const int m = t.m0 + rank * kTileM, c = t.c0 + rank * half;
-            const CUtensorMap *ma = &map_a, *mb = &map_b;
-            if (MODE == kDweight && t.nk) {
-                ma = a.segment_maps + 2 * (size_t)t.e, mb = ma + 1;
-                asm volatile("fence.proxy.tensormap::generic.acquire.gpu [%0], 128;" ::"l"(ma) : "memory");
-                asm volatile("fence.proxy.tensormap::generic.acquire.gpu [%0], 128;" ::"l"(mb) : "memory");
-            }
-            for (int kb = 0; kb < t.nk; ++kb, ++it) {
-                const int s = it % a.stages;
-                if (!(ok = bar_wait(smem_addr(&empty_[s]), ((it / a.stages) & 1) ^ 1, gave_up))) break;
-                uint32_t full = smem_addr(&full_[s]);
-                if (rank == 0) bar_expect(full, bytes);
-                if (CG == 2) full = in_cta(full, 0);
-                const uint32_t sa = ring + s * stage_bytes, sb = sa + kBytesA;
-                const int k = t.k0 + kb * kTileK;
+            const CUtensorMap *ma = &map_a, *mb = map_b.box;
+            if (MODE == kDweight) ma = a.segment_maps + 2 * (size_t)t.e, mb = ma + 1;
+            int k = t.k0;
+            for (int kb = 0; kb < t.nk; ++kb, k += kTileK) {
+                const int s = ring.stage;
+                if (!(ok = bar_wait(empty0 + 8 * s, ring.phase ^ 1, gave_up))) break;
+                const uint32_t full = full0_leader + 8 * s;
+                if (rank == 0) bar_expect(full0 + 8 * s, bytes);
+                const uint32_t sa = ring.addr, sb = sa + kBytesA;
                 if (MODE == kForward) {
                     tma_load<CG>(sa, ma, k, m, t.e, full);
                 } else if (MODE == kDx) {
@@ -260,40 +305,50 @@ product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, c
                     tma_load<CG>(sa, ma, m, k, 0, full);
                     tma_load<CG>(sa + 8192, ma, m + 64, k, 0, full);
                 }
-                for (int b = 0; b < boxes; ++b) {
-                    if (kBMn) tma_load<CG>(sb + b * 8192, mb, c + b * 64, k, 0, full);
-                    else tma_load<CG>(sb + b * 4096, mb, k, c + b * 32, 0, full);
+                if (kBMn) {
+#pragma unroll
+                    for (int b = 0; b < kAccColumns / CG / 64; ++b)
+                        if (b < boxes) tma_load<CG>(sb + b * 8192, mb, c + b * 64, k, 0, full);
+                } else {
+                    int row = 0;
+                    if (CG == 1 && half >= 256) tma_load<CG>(sb, mb, k, c, 0, full), row = 128;
+                    if (half - row >= 128) tma_load<CG>(sb + row * 128, mb, k, c + row, 0, full), row += 128;
+#pragma unroll
+                    for (int b = 1; b < 4; ++b)
+                        if (half & (128 >> b)) tma_load<CG>(sb + row * 128, mb + b, k, c + row, 0, full), row += 128 >> b;
                 }
+                ring.next();
+                ++sent;
             }
         }
         if (!ok && rank == 0)                                                // gave up: let the copies in flight land
-            for (int i = max(0, it - a.stages); i < it; ++i) {
+            for (int i = min(sent, a.stages); i > 0; --i) {
                 int none = 0;
-                bar_wait(smem_addr(&full_[i % a.stages]), (i / a.stages) & 1, &none);
+                ring.back();
+                bar_wait(full0 + 8 * ring.stage, ring.phase, &none);
             }
-    } else if (warp == 1 && lane == 0 && rank == 0) {
+    } else if (warp == 1 && rank == 0 && elect_one()) {
         // ---- products
-        int it = 0, used = 0;
+        Ring ring(ring_base, stage_bytes, a.stages);
+        int used = 0;
         bool ok = true;
-        for (int tile = start; ok && walk.get(tile, t); tile += stride) {
+        while (ok && walk.next(t)) {
             if (t.nk == 0) continue;
             const int acc = used & 1;
             if (!(ok = bar_wait(smem_addr(&acc_empty_[acc]), ((used >> 1) & 1) ^ 1, gave_up))) break;
             tmem_fence_after();
             const uint32_t d = tmem + acc * kAccColumns;
             const uint32_t idesc = instr_desc(kTileM * CG, t.n, kAMn, kBMn);
-            for (int kb = 0; kb < t.nk; ++kb, ++it) {
-                const int s = it % a.stages;
-                if (!(ok = bar_wait(smem_addr(&full_[s]), (it / a.stages) & 1, gave_up))) break;
+            for (int kb = 0; kb < t.nk; ++kb) {
+                if (!(ok = bar_wait(full0 + 8 * ring.stage, ring.phase, gave_up))) break;
                 tmem_fence_after();
-                const uint32_t sa = ring + s * stage_bytes, sb = sa + kBytesA;
+                const uint64_t da = kAMn ? desc_mn_major(ring.addr) : desc_k_major(ring.addr);
+                const uint64_t db = kBMn ? desc_mn_major(ring.addr + kBytesA) : desc_k_major(ring.addr + kBytesA);
 #pragma unroll
-                for (int j = 0; j < kTileK / 16; ++j) {
-                    const uint64_t da = kAMn ? desc_mn_major(sa + j * 2048) : desc_k_major(sa + j * 32);
-                    const uint64_t db = kBMn ? desc_mn_major(sb + j * 2048) : desc_k_major(sb + j * 32);
-                    mma_bf16<CG>(d, da, db, idesc, kb > 0 || j > 0);
-                }
-                mma_commit<CG>(smem_addr(&empty_[s]));
+                for (int j = 0; j < kTileK / 16; ++j)                        // the descriptors' addresses count 16 bytes
+                    mma_bf16<CG>(d, da + j * (kAMn ? 128 : 2), db + j * (kBMn ? 128 : 2), idesc, kb > 0 || j > 0);
+                mma_commit<CG>(empty0 + 8 * ring.stage);
+                ring.next();
             }
             if (!ok) break;
             mma_commit<CG>(smem_addr(&acc_full_[acc]));
@@ -301,53 +356,104 @@ product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, c
         }
     } else if (warp >= 4) {
         // ---- accumulators out
-        const int q = warp - 4;                                              // this warp's quarter of the lanes
+        const int q = warp & 3, first = (warp - 4) / 4 * 32;                 // a warp reaches the lanes 32 (warp mod 4) .. + 31
+        constexpr int kStep = kEpilogueWarps / 4 * 32;
+        uint32_t *stage = reinterpret_cast<uint32_t *>(tables) + (warp - 4) * kStageWords;
+        const int my_col = (lane >> 2) * (MODE == kForward ? 1 : 2), my_seg = (lane & 3) * 8;
+        const size_t ld = a.M;
         int used = 0;
-        for (int tile = start; walk.get(tile, t); tile += stride) {
-            const int feature = t.m0 + rank * kTileM + q * 32 + lane;
-            const bool live = feature < a.M;
+        while (walk.next(t)) {
+            const int feature = t.m0 + rank * kTileM + q * 32 + my_seg;
+            const bool live = feature < a.M;                                 // M is a multiple of 8
             const int acc = used & 1;
+            const uint32_t from = tmem + (uint32_t(q * 32) << 16) + acc * kAccColumns;
+            const size_t corner = ((MODE == kDweight ? (size_t)t.e * a.N + t.c0 : (size_t)t.c0) + my_col) * ld + feature;
+            const int cols = live ? t.cols - my_col : 0;                     // column c + my_col of the tile is real iff c < cols
+            uint4 r[4];                                                      // the operand of the lane's four columns of a block
+            float bias[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            if (MODE == kForward) {
+                if (a.bias && live) unpack8(__ldg(reinterpret_cast<const uint4 *>(a.bias + (size_t)t.e * a.M + feature)), bias);
+                if (a.operand)                                               // under the products
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (first + 8 * i < cols) r[i] = *reinterpret_cast<const uint4 *>(a.operand + corner + (first + 8 * i) * ld);
+            }
             if (t.nk) {
                 if (!bar_wait(smem_addr(&acc_full_[acc]), (used >> 1) & 1, gave_up)) break;
                 tmem_fence_after();
             }
-            const uint32_t from = tmem + (uint32_t(q * 32) << 16) + acc * kAccColumns;
-            size_t at = MODE == kDweight ? ((size_t)t.e * a.N + t.c0) * a.M + feature : (size_t)t.c0 * a.M + feature;
-            float b = 0.f;
-            if (MODE == kForward && a.bias && live) b = bf16_value(__ldg(a.bias + (size_t)t.e * a.M + feature));
-            for (int c0 = 0; c0 < t.cols; c0 += 32, at += (size_t)32 * a.M) {
-                const int cols = live ? min(32, t.cols - c0) : 0;
+            const auto release = [&] {                                       // this warp has read its last column of the accumulator
+                tmem_fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive_cluster(in_cta(smem_addr(&acc_empty_[acc]), 0));
+            };
+            for (int c0 = first; c0 < t.cols; c0 += kStep) {
                 uint32_t v[32];
-                uint16_t r[32];
-                if (MODE == kForward && a.operand) {
-#pragma unroll
-                    for (int c = 0; c < 32; ++c) r[c] = c < cols ? a.operand[at + (size_t)c * a.M] : (uint16_t)0;   // may be y: not through the read-only path
-                }
                 if (t.nk) {
                     tmem_load32(from + c0, v);
+                    if (c0 + kStep >= t.cols) release();
                 } else {
 #pragma unroll
                     for (int c = 0; c < 32; ++c) v[c] = 0u;
                 }
                 if (MODE == kForward) {
-                    switch (a.activation) {
-                    case EP_ACT_RELU: store_forward<EP_ACT_RELU>(a, v, r, b, at, cols); break;
-                    case EP_ACT_SILU: store_forward<EP_ACT_SILU>(a, v, r, b, at, cols); break;
-                    case EP_ACT_GELU: store_forward<EP_ACT_GELU>(a, v, r, b, at, cols); break;
-                    default: store_forward<EP_ACT_NONE>(a, v, r, b, at, cols); break;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        if (c0 + 16 * h >= t.cols) break;
+                        __syncwarp();
+#pragma unroll
+                        for (int c = 0; c < 16; ++c) stage[c * kStageLd + lane] = v[16 * h + c];
+                        __syncwarp();
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const int c = c0 + 16 * h + 8 * i;
+                            if (c < cols) {
+                                const uint4 *src = reinterpret_cast<const uint4 *>(stage + (8 * i + my_col) * kStageLd + my_seg);
+                                const uint4 lo = src[0], hi = src[1];
+                                const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+                                float z[8];
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) z[j] = __uint_as_float(w[j]) + bias[j];
+                                const size_t at = corner + c * ld;
+                                const uint4 mine = r[2 * h + i];
+                                // the same columns of the warp's next block (the operand may be y itself: an ordinary load)
+                                if (a.operand && c + kStep < cols)
+                                    r[2 * h + i] = *reinterpret_cast<const uint4 *>(a.operand + at + kStep * ld);
+                                switch (a.activation) {
+                                case EP_ACT_RELU: finish8<EP_ACT_RELU>(a, z, mine, at); break;
+                                case EP_ACT_SILU: finish8<EP_ACT_SILU>(a, z, mine, at); break;
+                                case EP_ACT_GELU: finish8<EP_ACT_GELU>(a, z, mine, at); break;
+                                default: finish8<EP_ACT_NONE>(a, z, mine, at); break;
+                                }
+                            }
+                        }
                     }
                 } else {
+                    // no arithmetic: a word carries two columns' results, rounded
+                    __syncwarp();
 #pragma unroll
-                    for (int c = 0; c < 32; ++c)
-                        if (c < cols) a.out[at + (size_t)c * a.M] = bf16_bits(__uint_as_float(v[c]));
+                    for (int c = 0; c < 16; ++c)
+                        stage[c * kStageLd + lane] = pack_bf16x2(__uint_as_float(v[2 * c]), __uint_as_float(v[2 * c + 1]));
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int c = c0 + 16 * i;
+                        if (c < cols) {
+                            const uint4 *src = reinterpret_cast<const uint4 *>(stage + (8 * i + (lane >> 2)) * kStageLd + my_seg);
+                            const uint4 lo = src[0], hi = src[1];
+                            uint16_t *dst = a.out + corner + c * ld;
+                            *reinterpret_cast<uint4 *>(dst) = make_uint4(__byte_perm(lo.x, lo.y, 0x5410), __byte_perm(lo.z, lo.w, 0x5410),
+                                                                         __byte_perm(hi.x, hi.y, 0x5410), __byte_perm(hi.z, hi.w, 0x5410));
+                            if (c + 1 < cols)
+                                *reinterpret_cast<uint4 *>(dst + ld) =
+                                    make_uint4(__byte_perm(lo.x, lo.y, 0x7632), __byte_perm(lo.z, lo.w, 0x7632),
+                                               __byte_perm(hi.x, hi.y, 0x7632), __byte_perm(hi.z, hi.w, 0x7632));
+                        }
+                    }
                 }
             }
-            if (t.nk) {
-                tmem_fence_before();
-                __syncwarp();
-                if (lane == 0) bar_arrive_cluster(in_cta(smem_addr(&acc_empty_[acc]), 0));
-                ++used;
-            }
+            if (t.nk && first >= t.cols) release();
+            used += t.nk > 0;
         }
     }
     __syncwarp();
@@ -398,18 +504,8 @@ struct SlopeArgs {
     int vecs, E, chunk, activation;       // vecs: 16-byte vectors per row; chunk: rows per run
 };
 
-__device__ __forceinline__ void unpack8(const uint4 &v, float (&f)[8])
-{
-    f[0] = bf16_lo(v.x), f[1] = bf16_hi(v.x), f[2] = bf16_lo(v.y), f[3] = bf16_hi(v.y);
-    f[4] = bf16_lo(v.z), f[5] = bf16_hi(v.z), f[6] = bf16_lo(v.w), f[7] = bf16_hi(v.w);
-}
-__device__ __forceinline__ uint4 pack8(const float (&f)[8])
-{
-    return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
-}
-
 template <int ACT>
-__global__ void __launch_bounds__(kSlopeWarps * 32)
+__global__ void __launch_bounds__(kSlopeWarps * 32, 5)
 slope_kernel(const SlopeArgs a)
 {
     const int lane = threadIdx.x & 31, vec = blockIdx.x * 32 + lane;
@@ -428,7 +524,7 @@ slope_kernel(const SlopeArgs a)
         e = lo;
     }
     const bool live = vec < a.vecs;
-    constexpr int kRows = 4;
+    constexpr int kRows = 2;
     while (p < end) {
         long long stop = end;
         if (a.partial) {
@@ -481,7 +577,7 @@ slope_kernel(const SlopeArgs a)
     }
 }
 
-// dbias[e][n] = sum of the expert's pieces in their order: eight runs of pieces at a time, then the eight sums.
+// dbias[e][n] = sum of the expert's pieces: eight warps take a run of pieces each, then the eight sums, both in order.
 __global__ void __launch_bounds__(256)
 bias_grad_kernel(const float *__restrict__ partial, const int32_t *__restrict__ offsets, long long rows, int N, int chunk, float *dbias)
 {
@@ -527,13 +623,13 @@ int sm_count(int *n)
 }
 
 template <int MODE, int CG>
-int launch_product(ProductArgs a, const CUtensorMap &map_a, const CUtensorMap &map_b, int64_t max_tiles, cudaStream_t stream)
+int launch_product(ProductArgs a, const CUtensorMap &map_a, const ColumnMaps &map_b, int64_t max_tiles, cudaStream_t stream)
 {
     int sms = 0;
     const int rc = sm_count(&sms);
     if (rc != EP_OK) return rc;
     const int stage = kBytesA + (a.columns / CG < 32 ? 32 : a.columns / CG) * kTileK * 2;
-    const int tables = 2 * (a.E + 1) * 4;
+    const int tables = kStageBytes + 2 * (a.E + 1) * 4;
     a.stages = (kSmemLimit - 2048 - tables) / stage;                         // 2048: alignment of the ring, static words
     if (a.stages > kMaxStages) a.stages = kMaxStages;
     int smem = 1024 + a.stages * stage + tables;
@@ -546,14 +642,25 @@ int launch_product(ProductArgs a, const CUtensorMap &map_a, const CUtensorMap &m
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = CG;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = CG;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
     EP_CUDA_TRY(cudaLaunchKernelEx(&cfg, product_kernel<MODE, CG>, a, map_a, map_b));
     EP_LAUNCH_CHECK(1);
+    return EP_OK;
+}
+
+int make_row_maps(TensorMapEncode encode, ColumnMaps *maps, const void *rows, int features, int64_t n)
+{
+    for (int b = 0; b < 4; ++b) {
+        const int rc = make_map(encode, &maps->box[b], rows, features, n, 1, 128 >> b);
+        if (rc != EP_OK) return rc;
+    }
     return EP_OK;
 }
 
@@ -565,17 +672,29 @@ int row_columns(int64_t rows, int E)
     return c;
 }
 
-int64_t row_tiles(int64_t rows, int E, int columns, int features, int CG)
+
+// Pairs of CTAs (256 features per tile, each operand row fetched once for both) wherever there is work for all pairs; with few
+// rows per expert the time is that of reading the weights and single CTAs spread it better. 128 experts of 1024 x 2048 on one
+// box: 16 rows each 86.9 us single, 88.9 paired; 256 experts of 2048 x 7168, 256 rows each: 1989 single, 1728 paired.
+constexpr int64_t kPairTiles = 74;
+
+template <int MODE>
+int launch_rows(const ProductArgs &a, const CUtensorMap &map_a, const ColumnMaps &map_b, cudaStream_t stream)
 {
-    const int64_t experts = rows < E ? rows : E;
-    return (experts + rows / columns) * ((features + kTileM * CG - 1) / (kTileM * CG));
+    const int64_t pieces = (a.rows < a.E ? a.rows : a.E) + a.rows / a.columns;    // at most
+    const int64_t single = pieces * ((a.M + kTileM - 1) / kTileM), paired = pieces * ((a.M + 2 * kTileM - 1) / (2 * kTileM));
+    if (a.columns >= 128 && paired >= kPairTiles) return launch_product<MODE, 2>(a, map_a, map_b, paired, stream);
+    return launch_product<MODE, 1>(a, map_a, map_b, single, stream);
 }
 
-int slope_chunk(int64_t rows)   // rows per run: short runs fill the GPU, and at most 512 of them leave little to add up
+// Rows per run of the slope kernel: about 40 warps per SM (a warp is one run of 256 columns), runs of at least 8 rows, and no
+// more than 1024 of them, which the second kernel adds up.
+int slope_chunk(int64_t rows, int features)
 {
-    int64_t c = (rows + 511) / 512;
-    c = (c + 3) / 4 * 4;
-    return (int)(c < 32 ? 32 : c);
+    const int64_t strips = (features + 255) / 256, runs = 148 * 40 / strips + 1;
+    int64_t c = (rows + runs - 1) / runs;
+    if (c < (rows + 1023) / 1024) c = (rows + 1023) / 1024;
+    return (int)(c < 8 ? 8 : (c + 1) / 2 * 2);
 }
 
 size_t up256(size_t n) { return (n + 255) & ~size_t(255); }
@@ -583,7 +702,8 @@ size_t up256(size_t n) { return (n + 255) & ~size_t(255); }
 size_t maps_bytes(const ep_matmul_t &m) { return up256(sizeof(CUtensorMap) * 2 * (size_t)m.num_experts); }
 size_t partial_bytes(const ep_matmul_t &m)
 {
-    const size_t chunks = (m.rows + slope_chunk(m.rows) - 1) / slope_chunk(m.rows);
+    const int chunk = slope_chunk(m.rows, m.out_features);
+    const size_t chunks = (m.rows + chunk - 1) / chunk;
     return up256((chunks + m.num_experts) * (size_t)m.out_features * 4);
 }
 size_t dz_bytes(const ep_matmul_t &m) { return up256((size_t)m.rows * m.out_features * 2); }
@@ -630,9 +750,10 @@ extern "C" int ep_expert_matmul(const ep_matmul_t *m, const void *x, const int32
     TensorMapEncode encode;
     rc = tensor_map_encoder(&encode);
     if (rc != EP_OK) return rc;
-    CUtensorMap map_w, map_x;
+    CUtensorMap map_w;
+    ColumnMaps map_x;
     rc = make_map(encode, &map_w, weight, m->in_features, m->out_features, m->num_experts, kTileM);
-    if (rc == EP_OK) rc = make_map(encode, &map_x, x, m->in_features, m->rows, 1, 32);
+    if (rc == EP_OK) rc = make_row_maps(encode, &map_x, x, m->in_features, m->rows);
     if (rc != EP_OK) return rc;
     ProductArgs a = {};
     a.offsets = expert_offsets;
@@ -645,7 +766,7 @@ extern "C" int ep_expert_matmul(const ep_matmul_t *m, const void *x, const int32
     a.pre = static_cast<uint16_t *>(pre);
     a.activation = m->activation, a.operand_op = m->operand_op;
     a.columns = row_columns(m->rows, m->num_experts);
-    return launch_product<kForward, 1>(a, map_w, map_x, row_tiles(m->rows, a.E, a.columns, a.M, 1), static_cast<cudaStream_t>(stream_));
+    return launch_rows<kForward>(a, map_w, map_x, static_cast<cudaStream_t>(stream_));
 }
 
 extern "C" size_t ep_expert_matmul_backward_workspace_bytes(const ep_matmul_t *m)
@@ -698,7 +819,7 @@ extern "C" int ep_expert_matmul_backward(const ep_matmul_t *m, const void *dy, c
         s.offsets = expert_offsets;
         s.rows = m->rows;
         s.vecs = (int)(N / 8), s.E = (int)E, s.activation = m->activation;
-        s.chunk = slope_chunk(m->rows);
+        s.chunk = slope_chunk(m->rows, (int)N);
         const int64_t chunks = (m->rows + s.chunk - 1) / s.chunk;
         const dim3 grid(ceil_div(s.vecs, 32), (unsigned)((chunks + kSlopeWarps - 1) / kSlopeWarps));
         switch (m->activation) {
@@ -722,30 +843,33 @@ extern "C" int ep_expert_matmul_backward(const ep_matmul_t *m, const void *dy, c
     a.status = status;
     a.rows = m->rows;
     a.E = m->num_experts;
-    CUtensorMap map_a, map_b;
+    CUtensorMap map_a;
+    ColumnMaps map_b;
     if (dx) {
         rc = make_map(encode, &map_a, weight, H, N, E, kTileK);
-        if (rc == EP_OK) rc = make_map(encode, &map_b, dz, N, m->rows, 1, 32);
+        if (rc == EP_OK) rc = make_row_maps(encode, &map_b, dz, N, m->rows);
         if (rc != EP_OK) return rc;
         a.M = m->in_features, a.K = m->out_features, a.N = 0;
         a.out = static_cast<uint16_t *>(dx);
         a.columns = row_columns(m->rows, m->num_experts);
-        rc = launch_product<kDx, 1>(a, map_a, map_b, row_tiles(m->rows, a.E, a.columns, a.M, 1), stream);
+            rc = launch_rows<kDx>(a, map_a, map_b, stream);
         if (rc != EP_OK) return rc;
     }
     if (dweight) {
         rc = make_map(encode, &map_a, x, H, m->rows, 1, kTileK);
-        if (rc == EP_OK) rc = make_map(encode, &map_b, dz, N, m->rows, 1, kTileK);
+        if (rc == EP_OK) rc = make_map(encode, &map_b.box[0], dz, N, m->rows, 1, kTileK);
         if (rc != EP_OK) return rc;
-        segment_maps_kernel<<<(unsigned)E, 32, 0, stream>>>(map_a, map_b, expert_offsets, m->rows, maps);
+        segment_maps_kernel<<<(unsigned)E, 32, 0, stream>>>(map_a, map_b.box[0], expert_offsets, m->rows, maps);
         EP_LAUNCH_CHECK(1);
         a.M = m->in_features, a.N = m->out_features, a.K = 0;
         a.out = static_cast<uint16_t *>(dweight);
         a.segment_maps = maps;
         a.columns = kAccColumns;
-        const int64_t tiles = (int64_t)E * ((a.M + kTileM - 1) / kTileM) * ((a.N + a.columns - 1) / a.columns);
-        if (tiles >= (int64_t(1) << 31)) return EP_ERR_INVALID_ARG;
-        rc = launch_product<kDweight, 1>(a, map_a, map_b, tiles, stream);
+        const int64_t per = (int64_t)E * ((a.N + a.columns - 1) / a.columns), tiles = per * ((a.M + kTileM - 1) / kTileM);
+        const int64_t pair_tiles = per * ((a.M + 2 * kTileM - 1) / (2 * kTileM));
+        if (tiles >= (int64_t(1) << 31) - (1 << 20)) return EP_ERR_INVALID_ARG;
+        rc = pair_tiles >= kPairTiles ? launch_product<kDweight, 2>(a, map_a, map_b, pair_tiles, stream)
+                                      : launch_product<kDweight, 1>(a, map_a, map_b, tiles, stream);
         if (rc != EP_OK) return rc;
     }
     return EP_OK;

@@ -52,11 +52,10 @@ __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count)
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity)
 {
     uint32_t ok;
-    asm volatile(
-        "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity)
-        : "memory");
+    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(ok)
+                 : "r"(bar), "r"(parity)
+                 : "memory");
     return ok != 0;
 }
 
@@ -89,9 +88,11 @@ __device__ __forceinline__ uint32_t in_cta(uint32_t addr, uint32_t rank)
     return r;
 }
 
+// Arrives on a barrier of any CTA of the cluster. Relaxed: what it hands over is tensor memory, ordered by tmem_fence_before();
+// a release at cluster scope would wait for the acknowledgement of every global store in front of it.
 __device__ __forceinline__ void bar_arrive_cluster(uint32_t bar)
 {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
 // --- TMA --------------------------------------------------------------------------------------------------------
@@ -198,6 +199,14 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&v)[32])
           "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
         : "r"(addr)
         : "memory");
+}
+
+// True in one lane of a converged warp.
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t one;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(one));
+    return one != 0;
 }
 
 __device__ __forceinline__ void cluster_sync()
