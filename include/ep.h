@@ -495,9 +495,10 @@ int ep_last_cuda_error(void);
  *                   sigmoid: the score over the sum of the token's scores)
  *   loss = balance_coef * sum_e f_e * mean_probs[e]
  * with expert_counts the valid picks per expert and tokens the tokens with a pick
- * (all 0, and loss 0, where there is none). Every sum has a fixed order: the same
+ * (all 0, and loss 0, where there is none). No sum depends on an order: the same
  * bits every time. It needs a workspace of ep_route_workspace_bytes() bytes
- * (device, 16-byte aligned, uninitialised); without balance none.
+ * (device, 16-byte aligned), zero-filled before its first use: every call leaves it
+ * zero-filled. Calls that share one must be stream-ordered. Without balance none.
  *
  * ep_balance_loss computes the same from a routing table that is already there
  * (entries -1 are skipped, ids outside [-1, E) too, with EP_STATUS_BAD_INDEX; a

@@ -82,16 +82,22 @@ __device__ __forceinline__ float act_value(int act, float z)
     }
 }
 
-__device__ __forceinline__ float act_slope(int act, float z)
+// act(z) and its derivative
+__device__ __forceinline__ void act_both(int act, float z, float &value, float &slope)
 {
     switch (act) {
-    case EP_ACT_RELU: return z <= 0.f ? 0.f : 1.f;
+    case EP_ACT_RELU: value = z <= 0.f ? 0.f : z, slope = z <= 0.f ? 0.f : 1.f; break;
     case EP_ACT_SILU: {
         const float s = __fdividef(1.f, 1.f + __expf(-z));
-        return s * (1.f + z * (1.f - s));
+        value = z * s, slope = s * (1.f + z * (1.f - s));
+        break;
     }
-    case EP_ACT_GELU: return 0.5f * (1.f + erff(z * 0.70710678f)) + z * __expf(-0.5f * z * z) * 0.39894228f;
-    default: return 1.f;
+    case EP_ACT_GELU: {
+        const float phi = 0.5f + 0.5f * erff(z * 0.70710678f);
+        value = z * phi, slope = phi + z * __expf(-0.5f * z * z) * 0.39894228f;
+        break;
+    }
+    default: value = z, slope = 1.f; break;
     }
 }
 
@@ -472,6 +478,8 @@ segment_maps_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
 {
     __shared__ alignas(128) uint32_t work[2][32];
     const int e = blockIdx.x, lane = threadIdx.x;
+    pdl_trigger();
+    pdl_wait();
     work[0][lane] = reinterpret_cast<const uint32_t *>(&map_x)[lane];
     work[1][lane] = reinterpret_cast<const uint32_t *>(&map_dz)[lane];
     const uint32_t end = max(1, segment_bound(__ldg(offsets + e + 1), rows));
@@ -505,9 +513,11 @@ struct SlopeArgs {
 };
 
 template <int ACT>
-__global__ void __launch_bounds__(kSlopeWarps * 32, 5)
+__global__ void __launch_bounds__(kSlopeWarps * 32, 8)
 slope_kernel(const SlopeArgs a)
 {
+    pdl_trigger();
+    pdl_wait();
     const int lane = threadIdx.x & 31, vec = blockIdx.x * 32 + lane;
     const long long chunk = (long long)blockIdx.y * kSlopeWarps + (threadIdx.x >> 5);
     const int total = segment_bound(__ldg(a.offsets + a.E), a.rows);
@@ -524,7 +534,7 @@ slope_kernel(const SlopeArgs a)
         e = lo;
     }
     const bool live = vec < a.vecs;
-    constexpr int kRows = 2;
+    constexpr int kRows = 1;
     while (p < end) {
         long long stop = end;
         if (a.partial) {
@@ -550,21 +560,17 @@ slope_kernel(const SlopeArgs a)
                     float fg[8], fz[8], fr[8], o[8];
                     unpack8(g[i], fg);
                     if (ACT != EP_ACT_NONE || a.doperand) unpack8(z[i], fz);
-                    if (a.doperand) {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) o[j] = fg[j] * act_value(ACT, fz[j]);
-                        st_stream(a.doperand + at, pack8(o));
-                    }
-                    if (a.operand) {
-                        unpack8(r[i], fr);
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) fg[j] *= fr[j];
-                    }
+                    if (a.operand) unpack8(r[i], fr);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        if (ACT != EP_ACT_NONE) fg[j] *= act_slope(ACT, fz[j]);
+                        float value = 0.f, slope = 1.f;
+                        if (ACT != EP_ACT_NONE || a.doperand) act_both(ACT, fz[j], value, slope);
+                        o[j] = fg[j] * value;
+                        if (a.operand) fg[j] *= fr[j];
+                        fg[j] *= slope;
                         sum[j] += fg[j];
                     }
+                    if (a.doperand) st_stream(a.doperand + at, pack8(o));
                     if (a.dz) a.dz[at] = pack8(fg);
                 }
         }
@@ -582,6 +588,8 @@ __global__ void __launch_bounds__(256)
 bias_grad_kernel(const float *__restrict__ partial, const int32_t *__restrict__ offsets, long long rows, int N, int chunk, float *dbias)
 {
     __shared__ float part[8][32];
+    pdl_trigger();
+    pdl_wait();
     const int e = blockIdx.y, lane = threadIdx.x & 31, w = threadIdx.x >> 5, n = blockIdx.x * 32 + lane;
     const int begin = segment_bound(__ldg(offsets + e), rows), end = segment_bound(__ldg(offsets + e + 1), rows);
     float s = 0.f;
@@ -708,11 +716,6 @@ size_t partial_bytes(const ep_matmul_t &m)
 }
 size_t dz_bytes(const ep_matmul_t &m) { return up256((size_t)m.rows * m.out_features * 2); }
 
-template <int ACT>
-void launch_slope(const SlopeArgs &a, dim3 grid, cudaStream_t stream)
-{
-    slope_kernel<ACT><<<grid, kSlopeWarps * 32, 0, stream>>>(a);
-}
 
 }  // namespace
 
@@ -822,16 +825,15 @@ extern "C" int ep_expert_matmul_backward(const ep_matmul_t *m, const void *dy, c
         s.chunk = slope_chunk(m->rows, (int)N);
         const int64_t chunks = (m->rows + s.chunk - 1) / s.chunk;
         const dim3 grid(ceil_div(s.vecs, 32), (unsigned)((chunks + kSlopeWarps - 1) / kSlopeWarps));
-        switch (m->activation) {
-        case EP_ACT_RELU: launch_slope<EP_ACT_RELU>(s, grid, stream); break;
-        case EP_ACT_SILU: launch_slope<EP_ACT_SILU>(s, grid, stream); break;
-        case EP_ACT_GELU: launch_slope<EP_ACT_GELU>(s, grid, stream); break;
-        default: launch_slope<EP_ACT_NONE>(s, grid, stream); break;
-        }
+        void (*kernel)(const SlopeArgs) = m->activation == EP_ACT_RELU   ? slope_kernel<EP_ACT_RELU>
+                                          : m->activation == EP_ACT_SILU ? slope_kernel<EP_ACT_SILU>
+                                          : m->activation == EP_ACT_GELU ? slope_kernel<EP_ACT_GELU>
+                                                                         : slope_kernel<EP_ACT_NONE>;
+        EP_CUDA_TRY(launch_pdl(kernel, grid, dim3(kSlopeWarps * 32), 0, stream, s));
         EP_LAUNCH_CHECK(1);
         if (dbias) {
-            bias_grad_kernel<<<dim3((unsigned)((N + 31) / 32), (unsigned)E), 256, 0, stream>>>(partial, expert_offsets, m->rows, (int)N,
-                                                                                              s.chunk, dbias);
+            EP_CUDA_TRY(launch_pdl(bias_grad_kernel, dim3((unsigned)((N + 31) / 32), (unsigned)E), dim3(256), 0, stream, partial,
+                                   expert_offsets, (long long)m->rows, (int)N, s.chunk, dbias));
             EP_LAUNCH_CHECK(1);
         }
     }
@@ -859,7 +861,8 @@ extern "C" int ep_expert_matmul_backward(const ep_matmul_t *m, const void *dy, c
         rc = make_map(encode, &map_a, x, H, m->rows, 1, kTileK);
         if (rc == EP_OK) rc = make_map(encode, &map_b.box[0], dz, N, m->rows, 1, kTileK);
         if (rc != EP_OK) return rc;
-        segment_maps_kernel<<<(unsigned)E, 32, 0, stream>>>(map_a, map_b.box[0], expert_offsets, m->rows, maps);
+        EP_CUDA_TRY(launch_pdl(segment_maps_kernel, dim3((unsigned)E), dim3(32), 0, stream, map_a, map_b.box[0], expert_offsets,
+                               (long long)m->rows, maps));
         EP_LAUNCH_CHECK(1);
         a.M = m->in_features, a.N = m->out_features, a.K = 0;
         a.out = static_cast<uint16_t *>(dweight);

@@ -7,20 +7,27 @@
 //              (p = s for softmax, s / sum(s) for sigmoid); the counts are constants of the gradient
 //
 // One warp owns a token and holds its row in registers: NV values a lane, four neighbouring experts at a time, so that a
-// row of 128 fp32 logits is one 16-byte load per lane. The picks are K rounds of a warp-wide maximum over order-preserving
-// integer keys and a warp-wide minimum over the ids that hold it. A token's row is read once and nothing of size E is
-// written in the forward pass. For the balance loss a warp adds its tokens' probabilities into a row of shared memory of
-// its own (no atomics, a fixed order of additions), a CTA writes its sums once, and one small cluster adds the CTAs' rows
-// in their order: the same bits every time.
+// row of 128 fp32 logits is one 16-byte load per lane. A token's row is read once and nothing of size E is written in the
+// forward pass.
+//
+// Picks. Order-preserving integer keys; the K-th largest of the 32 lanes' maxima bounds the K-th largest key from below, so
+// the keys that reach it hold all the picks. They are few (some 12 for 8 of 256): one per lane, they go through K rounds
+// of a warp-wide maximum and a warp-wide minimum over the ids that hold it, about 6 instructions a round. (The same rounds
+// over all NV values of a lane, which stay for rows where more than 32 keys reach the bound, take 45 at E = 256.)
+//
+// For the balance loss a warp adds up its tokens' probabilities by itself and a CTA, one per SM, its warps' sums, both in a
+// fixed order; a CTA adds its sums to one of kRows rows of 64-bit whole numbers of 2^-shift, whose sum does not depend on the
+// order: the same bits every time. The CTA that comes last adds the rows and leaves zeros. At 4096 x 128 this takes 4.5 us on top of
+// the picks' 4.0; one row per CTA, read by the last one, 7.1 (an SM reads some 60 bytes a cycle); a second kernel, a cluster of
+// eight CTAs, 5.4 and 3 us of the host's time for its launch; a single row of atomics 5.5.
 #include "ep_common.cuh"
-
-#include <cooperative_groups.h>
 
 namespace ep {
 namespace {
 
-constexpr int kMaxRouteCtas = 296;
-constexpr int kFinishCtas = 8, kFinishThreads = 256;
+constexpr int kBalanceCtas = 148;          // at most: one per SM
+constexpr int kRows = 8;                   // that the CTAs' sums are spread over
+constexpr uint32_t kDead = 0x007fffffu;    // key of -inf: an expert that may not be picked
 
 enum { kRoute = 0, kRouteBalance = 1, kBalance = 2 };
 
@@ -29,11 +36,13 @@ struct RouteArgs {
     const float *bias;
     int32_t *topk_idx;                    // written (route) or read (balance alone)
     float *topk_weights;
-    float *partial;                       // [ctas][E] sums of probabilities
-    int32_t *partial_counts;              // [ctas][E + 1] picks, tokens
+    unsigned long long *sums;             // [kRows][E] sums of probabilities in units of 2^-shift; zero between calls, as all of the workspace
+    int32_t *sum_counts;                  // [kRows][E] picks; then: tokens, CTAs that are done
+    int32_t *expert_counts, *tokens;      // the loss's outputs
+    float *mean_probs, *loss;
     int32_t *status;
-    int T, E, K, scoring, renormalize, vec;
-    float scale;
+    int T, E, K, scoring, renormalize, vec, vec_bias, shift;
+    float scale, coef;
 };
 
 __device__ __forceinline__ float value(const float *p, size_t i) { return __ldg(p + i); }
@@ -59,9 +68,9 @@ __device__ __forceinline__ int expert_of(int j, int lane)
     return NV < 4 ? j * 32 + lane : (j >> 2) * 128 + lane * 4 + (j & 3);
 }
 
-// A row of logits; an expert that may not be picked (-inf, NaN, +inf, or past E) comes as -inf. Returns whether a NaN or +inf was seen.
+// A row of logits, -inf past E.
 template <int NV, class T>
-__device__ __forceinline__ bool load_row(const T *row, int E, int lane, int vec, float (&l)[NV])
+__device__ __forceinline__ void load_row(const T *row, int E, int lane, int vec, float (&l)[NV])
 {
     if (NV >= 4 && vec) {
 #pragma unroll
@@ -79,12 +88,18 @@ __device__ __forceinline__ bool load_row(const T *row, int E, int lane, int vec,
             l[j] = e < E ? value(row, e) : -INFINITY;
         }
     }
+}
+
+// NaN and +inf, which may not be picked either, become -inf. Returns whether there were any (of this lane's).
+template <int NV>
+__device__ __forceinline__ bool clean_row(float (&l)[NV])
+{
     bool bad = false;
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const bool ok = l[j] < INFINITY;                 // false for NaN and +inf
-        bad |= !ok;
-        l[j] = ok ? l[j] : -INFINITY;
+    for (int j = 0; j < NV; ++j) bad |= !(l[j] < INFINITY);
+    if (__any_sync(kFullMask, bad)) {                     // hardly ever
+#pragma unroll
+        for (int j = 0; j < NV; ++j) l[j] = l[j] < INFINITY ? l[j] : -INFINITY;
     }
     return bad;
 }
@@ -102,43 +117,219 @@ __device__ __forceinline__ float warp_sum(float v)
     return v;
 }
 
-// Order-preserving integer of a float: -inf is the smallest that occurs and maps to 0; -0 counts as +0.
+// Order-preserving integer of a float: kDead for -inf, larger for every other number; -0 counts as +0.
 __device__ __forceinline__ uint32_t key_of(float v)
 {
-    const uint32_t b = __float_as_uint(v + 0.f);
-    return v == -INFINITY ? 0u : (b & 0x80000000u) ? ~b : b | 0x80000000u;
+    const int b = __float_as_int(v + 0.f);
+    return (uint32_t)(b ^ ((b >> 31) | 0x80000000));
 }
 __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k); }
 
-// exp(-l) overflows below -88; there the sigmoid is exp(l) to the last bit (0 for -inf)
-__device__ __forceinline__ float sigmoid(float l) { return l < -80.f ? expf(l) : 1.f / (1.f + expf(-l)); }
+// A score of every expert of a row, to 2^-20: two or four instructions a value where the functions to the last bit take forty. They
+// feed sums, and choose who may be among the picks; a pick's own score, and what decides between picks, is exact_score.
+__device__ __forceinline__ float rough_score(bool soft, float l, float top)
+{
+    return soft ? __expf(l - top) : __fdividef(1.f, 1.f + __expf(-l));
+}
+
+// The score (softmax: before the division by the row's sum) of one expert. exp(-l) overflows below -88; there the sigmoid is exp(l)
+// to the last bit.
+__device__ __forceinline__ float exact_score(bool soft, float l, float top)
+{
+    const bool low = l < -80.f;
+    const float e = expf(soft ? l - top : low ? l : -l);
+    return soft || low ? e : 1.f / (1.f + e);
+}
+
+// K rounds of "the largest key, and of its holders the lowest id": lane k gets the k-th's id. `N` keys a lane, of ids that ascend
+// with the position in the lane.
+template <int N, class Id>
+__device__ __forceinline__ int pick_rounds(uint32_t (&key)[N], Id id_of, int K, int lane)
+{
+    int id = -1;
+    for (int k = 0; k < K; ++k) {
+        uint32_t best = key[0];
+        int at = 0;
+#pragma unroll
+        for (int j = 1; j < N; ++j)
+            if (key[j] > best) best = key[j], at = j;
+        const uint32_t m = __reduce_max_sync(kFullMask, best);
+        if (m <= kDead) break;                                                // no expert left
+        const int e = __reduce_min_sync(kFullMask, best == m ? id_of(at) : 0x7fffffff);
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (id_of(j) == e) key[j] = 0u;
+        if (lane == k) id = e;
+    }
+    return id;
+}
+
+// The same for one key a lane, ids ascending with the lane: the lowest lane that holds the maximum holds the lowest id.
+__device__ __forceinline__ void pick_listed(uint32_t key, int e, float q, int K, int lane, int &id, float &got)
+{
+    const int rounds = min(K, __popc(__ballot_sync(kFullMask, key > kDead)));
+    int from = 0;
+    for (int k = 0; k < rounds; ++k) {
+        const uint32_t m = __reduce_max_sync(kFullMask, key);
+        const int src = __ffs(__ballot_sync(kFullMask, key == m)) - 1;
+        if (lane == src) key = 0u;
+        if (lane == k) from = src;
+    }
+    got = __shfl_sync(kFullMask, q, from);
+    e = __shfl_sync(kFullMask, e, from);
+    id = lane < rounds ? e : -1;
+}
+
+// Lane k's pick out of a row: its id (-1: none left). `rough` holds a value per expert that is off by at most `slack` of 1 + itself from
+// what orders them; exact(logit, id, q) gives that value's key and in q what the caller wants of the pick, which comes back in
+// `got`. `list`: 2 kListed words of shared memory of this warp.
+constexpr int kListed = 64;
+
+template <int NV, class T, class Exact>
+__device__ __forceinline__ int pick(const float (&l)[NV], const float (&rough)[NV], float slack, Exact exact, const T *row, int E, int K, int lane,
+                                    uint32_t *list, float &got)
+{
+    int id = -1;
+    if (NV == 1) {                                                            // a key per lane is what the list below would be
+        float q;
+        pick_listed(l[0] > -INFINITY ? exact(l[0], lane, q) : 0u, lane, q, K, lane, id, got);
+        return id;
+    }
+    // the warp in at least K groups of lanes: the least of the groups' maxima is reached by K values
+    float best = rough[0];
+#pragma unroll
+    for (int j = 1; j < NV; ++j) best = fmaxf(best, rough[j]);
+    float bound;
+    if (K <= 8 && NV <= 8) {
+        best = fmaxf(best, __shfl_xor_sync(kFullMask, best, 1));
+        best = fmaxf(best, __shfl_xor_sync(kFullMask, best, 2));              // 8 groups of 4
+        if (K <= 4) best = fmaxf(best, __shfl_xor_sync(kFullMask, best, 4));  // 4 groups of 8
+        if (K <= 2) best = fmaxf(best, __shfl_xor_sync(kFullMask, best, 8));  // 2 groups of 16
+        bound = of_key(__reduce_min_sync(kFullMask, key_of(best)));
+    } else {                                                                  // the K-th largest of the lanes' maxima: closer
+        uint32_t top = key_of(best), m = 0u;
+        for (int k = 0; k < K; ++k) {
+            m = __reduce_max_sync(kFullMask, top);
+            if (m <= kDead) break;
+            if (lane == __ffs(__ballot_sync(kFullMask, top == m)) - 1) top = 0u;
+        }
+        bound = of_key(max(m, kDead));
+    }
+    bound -= slack * (1.f + fabsf(bound));
+    bound = fmaxf(bound, -3.4028235e38f);                                     // where a group is empty: every value that may be picked
+    // what reaches it, in the order of the ids
+    int count = 0;
+    constexpr int kStep = NV < 4 ? 1 : 4;                                     // a lane's neighbouring experts
+#pragma unroll
+    for (int j = 0; j < NV; j += kStep) {
+        if (NV > 8) {
+            float most = rough[j];
+#pragma unroll
+            for (int c = 1; c < kStep; ++c) most = fmaxf(most, rough[(j + c) % NV]);
+            if (!__any_sync(kFullMask, most >= bound)) continue;
+        }
+        int at = count;
+#pragma unroll
+        for (int c = 0; c < kStep; ++c) {
+            const unsigned who = __ballot_sync(kFullMask, rough[j + c] >= bound);
+            at += __popc(who & lanemask_lt());
+            count += __popc(who);
+        }
+#pragma unroll
+        for (int c = 0; c < kStep; ++c)
+            if (rough[j + c] >= bound) {
+                if (at < kListed) list[at] = __float_as_uint(l[j + c]), list[kListed + at] = expert_of<NV>(j + c, lane);
+                ++at;
+            }
+    }
+    __syncwarp();
+    if (count <= 32) {
+        const bool in = lane < count;
+        const int e = in ? (int)list[kListed + lane] : 0;
+        float q = 0.f;
+        pick_listed(in ? exact(__uint_as_float(list[lane]), e, q) : 0u, e, q, K, lane, id, got);
+    } else {
+        float q;
+        if (count <= kListed) {
+            const int e0 = (int)list[kListed + lane], e1 = lane + 32 < count ? (int)list[kListed + 32 + lane] : 0x7ffffffe;
+            uint32_t two[2] = {exact(__uint_as_float(list[lane]), e0, q),
+                               lane + 32 < count ? exact(__uint_as_float(list[lane + 32]), e1, q) : 0u};
+            id = pick_rounds<2>(two, [&](int j) { return j ? e1 : e0; }, K, lane);
+        } else if (NV <= 8) {
+            uint32_t key[NV];
+#pragma unroll
+            for (int j = 0; j < NV; ++j) key[j] = l[j] > -INFINITY ? exact(l[j], expert_of<NV>(j, lane), q) : kDead;
+            id = pick_rounds<NV>(key, [&](int j) { return expert_of<NV>(j, lane); }, K, lane);
+        } else {                                                              // the row again, once per pick: what follows the pick before
+            uint32_t last_key = 0xffffffffu;
+            int last_e = -1;
+            for (int k = 0; k < K; ++k) {
+                uint32_t best = kDead;
+                int at = 0x7fffffff;
+#pragma unroll 1
+                for (int e = lane; e < E; e += 32) {
+                    const float x = value(row, e);
+                    const uint32_t o = x < INFINITY && x > -INFINITY ? exact(x, e, q) : kDead;
+                    const bool after = o < last_key || (o == last_key && e > last_e);
+                    if (after && o > best) best = o, at = e;
+                }
+                const uint32_t m = __reduce_max_sync(kFullMask, best);
+                if (m <= kDead) break;
+                last_key = m;
+                last_e = __reduce_min_sync(kFullMask, best == m ? at : 0x7fffffff);
+                if (lane == k) id = last_e;
+            }
+        }
+        if (id >= 0) exact(value(row, id), id, got);
+    }
+    __syncwarp();                                                             // the list is free again
+    return id;
+}
+
+// Warps per CTA. With a balance loss one CTA fills an SM as far as the registers allow.
+__host__ __device__ constexpr int route_warps(int nv, bool balance)
+{
+    return nv > 32 ? 4 : !balance ? 8 : nv <= 8 ? 32 : nv == 16 ? 16 : 8;
+}
 
 template <class T, int NV, int MODE>
-__global__ void __launch_bounds__(NV <= 32 ? 256 : 128)
+__global__ void __launch_bounds__(route_warps(NV, MODE != kRoute) * 32)
 route_kernel(const RouteArgs a)
 {
     extern __shared__ float shared[];
     constexpr bool kBal = MODE != kRoute;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    const int padded = NV * 32;
-    float *mine = shared + (size_t)warp * padded;                             // this warp's sums, in the order of its lanes' values
-    int *counts = reinterpret_cast<int *>(shared + (size_t)warps * padded);   // [E + 1]
+    constexpr int kWarps = route_warps(NV, kBal), kPadded = NV * 32;
+    constexpr bool kInRegisters = NV <= 16;                                   // where a warp keeps its sums of probabilities
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    uint32_t *list = reinterpret_cast<uint32_t *>(shared) + warp * 2 * kListed;
+    float *sums = shared + kWarps * 2 * kListed;                                       // [warp][value of a lane][lane]
+    float *mine = sums + (size_t)warp * kPadded;
+    int *counts = reinterpret_cast<int *>(sums + (size_t)kWarps * kPadded);   // [E + 1], and at least [kWarps]
+    float psum[kInRegisters ? NV : 1];
     if (kBal) {
-        for (int i = lane; i < padded; i += 32) mine[i] = 0.f;
+        if (kInRegisters) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) psum[j % (kInRegisters ? NV : 1)] = 0.f;
+        } else {
+            for (int i = lane; i < kPadded; i += 32) mine[i] = 0.f;
+        }
         for (int i = threadIdx.x; i <= a.E; i += blockDim.x) counts[i] = 0;
         __syncthreads();
     }
+    const bool soft = a.scoring == EP_SCORE_SOFTMAX;
+    const bool all = kBal || a.bias || (soft && !a.renormalize);              // are scores needed beyond the picked ones?
     int tokens = 0;
     bool bad = false, bad_index = false;
-    for (int t = blockIdx.x * warps + warp; t < a.T; t += gridDim.x * warps) {
+    for (int t = blockIdx.x * kWarps + warp; t < a.T; t += gridDim.x * kWarps) {
         const T *row = static_cast<const T *>(a.logits) + (size_t)t * a.E;
         float l[NV];
-        bad |= load_row<NV>(row, a.E, lane, a.vec, l);
+        load_row<NV>(row, a.E, lane, a.vec, l);
+        bad |= clean_row<NV>(l);
         float top = l[0];
 #pragma unroll
         for (int j = 1; j < NV; ++j) top = fmaxf(top, l[j]);
-        top = warp_max(top);
-        const bool live = top > -INFINITY;                                    // does the token have an expert at all?
+        const bool live = __any_sync(kFullMask, top > -INFINITY);             // does the token have an expert at all?
+        if (soft) top = warp_max(top);
         int id = -1;
         if (MODE == kBalance && lane < a.K) {
             id = __ldg(a.topk_idx + (size_t)t * a.K + lane);
@@ -146,62 +337,52 @@ route_kernel(const RouteArgs a)
         }
         const bool counted = live && (MODE != kBalance || __any_sync(kFullMask, id >= 0));
 
-        // ---- probabilities
-        const bool soft = a.scoring == EP_SCORE_SOFTMAX;
-        const bool all = kBal || a.bias || (soft && !a.renormalize);          // are scores needed beyond the picked ones?
+        // ---- scores
         float s[NV], sum = 1.f;
         if (all && live) {
-            sum = 0.f;
 #pragma unroll
-            for (int j = 0; j < NV; ++j) {
-                s[j] = soft ? expf(l[j] - top) : sigmoid(l[j]);
-                sum += s[j];
+            for (int j = 0; j < NV; ++j) s[j] = rough_score(soft, l[j], top);
+            if (kBal || soft) {
+                sum = 0.f;
+#pragma unroll
+                for (int j = 0; j < NV; ++j) sum += s[j];
+                sum = warp_sum(sum);
             }
-            sum = warp_sum(sum);
             if (kBal && counted) {
-                const float inv = sum > 0.f ? 1.f / sum : 0.f;                // sigmoids of very negative logits can all be 0
+                const float inv = sum > 0.f ? __fdividef(1.f, sum) : 0.f;     // sigmoids of very negative logits can all be 0
 #pragma unroll
-                for (int j = 0; j < NV; ++j) mine[j * 32 + lane] += s[j] * inv;
-                if (lane == 0) ++tokens;
+                for (int j = 0; j < NV; ++j) {
+                    if (kInRegisters) psum[j % (kInRegisters ? NV : 1)] += s[j] * inv;
+                    else mine[j * 32 + lane] += s[j] * inv;
+                }
+                ++tokens;
             }
         }
         if (MODE != kBalance) {
-            // ---- picks: lane k ends up with the k-th
-            uint32_t key[NV];
+            float w = 0.f;                                                    // the pick's score
+            if (live && a.bias) {
+                float rough[NV];
+                load_row<NV>(a.bias, a.E, lane, a.vec_bias, rough);           // -inf past E
+                const float inv = soft ? __fdividef(1.f, sum) : 1.f;
 #pragma unroll
-            for (int j = 0; j < NV; ++j) {
-                const int e = expert_of<NV>(j, lane);
-                float v = l[j];
-                if (a.bias && e < a.E && v > -INFINITY) {
-                    v = (soft ? s[j] / sum : s[j]) + __ldg(a.bias + e);
-                    if (!(v < INFINITY)) bad = true, v = -INFINITY;
-                }
-                key[j] = key_of(v);
+                for (int j = 0; j < NV; ++j) rough[j] = l[j] > -INFINITY ? s[j] * inv + rough[j] : -INFINITY;
+                bad |= clean_row<NV>(rough);
+                id = pick<NV>(l, rough, 0x1p-18f, [&](float x, int e, float &q) {
+                    q = exact_score(soft, x, top);
+                    const float o = (soft ? q / sum : q) + __ldg(a.bias + e);
+                    return o < INFINITY ? key_of(o) : kDead;
+                }, row, a.E, a.K, lane, list, w);
+            } else if (live) {
+                id = pick<NV>(l, l, 0.f, [](float x, int, float &q) { q = x; return key_of(x); }, row, a.E, a.K, lane, list, w);
+                w = exact_score(soft, w, top);
             }
-            uint32_t my_key = 0u;
-            for (int k = 0; k < a.K; ++k) {
-                uint32_t best = key[0];
-                int at = 0;
-#pragma unroll
-                for (int j = 1; j < NV; ++j)
-                    if (key[j] > best) best = key[j], at = j;                 // ids ascend with j
-                const uint32_t m = __reduce_max_sync(kFullMask, best);
-                if (m == 0u) break;                                           // no expert left
-                const int e = __reduce_min_sync(kFullMask, best == m ? expert_of<NV>(at, lane) : 0x7fffffff);
-#pragma unroll
-                for (int j = 0; j < NV; ++j)
-                    if (expert_of<NV>(j, lane) == e) key[j] = 0u;
-                if (lane == k) id = e, my_key = m;
+            if (id < 0) w = 0.f;
+            if (a.renormalize) {
+                const float picked = warp_sum(w);
+                w = picked > 0.f ? w / picked : 0.f;
+            } else if (soft) {
+                w /= sum;
             }
-            // ---- weights of the picks
-            float w = 0.f;
-            if (id >= 0) {
-                const float v = a.bias ? value(row, id) : of_key(my_key);
-                w = soft ? expf(v - top) : sigmoid(v);
-            }
-            const float picked = warp_sum(w);
-            if (a.renormalize) w = picked > 0.f ? w / picked : 0.f;
-            else if (soft) w /= sum;
             if (lane < a.K) {
                 a.topk_idx[(size_t)t * a.K + lane] = id;
                 a.topk_weights[(size_t)t * a.K + lane] = w * a.scale;
@@ -214,85 +395,66 @@ route_kernel(const RouteArgs a)
         if (bad_index) atomicOr(a.status, EP_STATUS_BAD_INDEX);
     }
     if (kBal) {
+        __shared__ bool last;
+        if (kInRegisters) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) mine[j * 32 + lane] = psum[j % (kInRegisters ? NV : 1)];
+        }
         if (lane == 0 && tokens) atomicAdd(counts + a.E, tokens);
         __syncthreads();
-        for (int i = threadIdx.x; i < padded; i += blockDim.x) {
+        for (int i = threadIdx.x; i < kPadded; i += blockDim.x) {
             const int e = expert_of<NV>(i >> 5, i & 31);
             if (e < a.E) {
                 float v = 0.f;
-                for (int w = 0; w < warps; ++w) v += shared[(size_t)w * padded + i];
-                a.partial[(size_t)blockIdx.x * a.E + e] = v;
-            }
-        }
-        for (int i = threadIdx.x; i <= a.E; i += blockDim.x) a.partial_counts[(size_t)blockIdx.x * (a.E + 1) + i] = counts[i];
-    }
-}
-
-// Adds the CTAs' rows: counts, mean probabilities, loss. One cluster; each CTA owns a run of experts, eight warps split the rows.
-__global__ void __launch_bounds__(kFinishThreads) __cluster_dims__(kFinishCtas, 1, 1)
-balance_finish_kernel(const float *partial, const int32_t *partial_counts, int ctas, int E, float coef, int32_t *expert_counts,
-                      int32_t *tokens_out, float *mean_probs, float *loss)
-{
-    namespace cg = cooperative_groups;
-    constexpr int kWarps = kFinishThreads / 32;
-    __shared__ float psum[kWarps][32];
-    __shared__ int csum[kWarps][32];
-    __shared__ float share_dot;
-    __shared__ int share_count, share_tokens;
-    cg::cluster_group cluster = cg::this_cluster();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rank = cluster.block_rank();
-    pdl_wait();
-    if (threadIdx.x == 0) share_tokens = 0;
-    __syncthreads();
-    int n = 0;
-    for (int c = threadIdx.x; c < ctas; c += kFinishThreads) n += partial_counts[(size_t)c * (E + 1) + E];
-    n = __reduce_add_sync(kFullMask, n);
-    if (lane == 0 && n) atomicAdd(&share_tokens, n);
-    __syncthreads();
-    const int tokens = share_tokens;
-    const float inv = tokens ? 1.f / (float)tokens : 0.f;
-    float dot = 0.f;                                                          // warp 0: sum of count * (sum of probabilities)
-    int count = 0;
-    for (int base = rank * 32; base < E; base += kFinishCtas * 32) {
-        const int e = base + lane;
-        float p = 0.f;
-        int k = 0;
-        if (e < E) {
 #pragma unroll 8
-            for (int c = warp; c < ctas; c += kWarps) {
-                p += partial[(size_t)c * E + e];
-                k += partial_counts[(size_t)c * (E + 1) + e];
+                for (int w = 0; w < kWarps; ++w) v += sums[(size_t)w * kPadded + i];
+                const size_t at = (size_t)(blockIdx.x % kRows) * a.E + e;
+                if (v > 0.f) atomicAdd(a.sums + at, __float2ull_rn(ldexpf(v, a.shift)));
+                if (counts[e]) atomicAdd(a.sum_counts + at, counts[e]);
             }
         }
-        psum[warp][lane] = p;
-        csum[warp][lane] = k;
+        int32_t *total = a.sum_counts + (size_t)kRows * a.E;                  // tokens, CTAs
+        if (threadIdx.x == 0 && counts[a.E]) atomicAdd(total, counts[a.E]);
+        __threadfence();
+        __syncthreads();
+        if (threadIdx.x == 0) last = atomicAdd(total + 1, 1) == (int)gridDim.x - 1;
+        __syncthreads();
+        if (!last) return;
+        __threadfence();
+        const int n = __ldcg(total);
+        const float unit = n ? ldexpf(1.f, -a.shift) / (float)n : 0.f;
+        float dot = 0.f;                                                      // sum of count * (mean probability)
+        int picks = 0;
+        for (int e = threadIdx.x; e < a.E; e += blockDim.x) {
+            unsigned long long p[kRows];
+            int k[kRows];
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) p[r] = __ldcg(a.sums + (size_t)r * a.E + e), k[r] = __ldcg(a.sum_counts + (size_t)r * a.E + e);
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) a.sums[(size_t)r * a.E + e] = 0ull, a.sum_counts[(size_t)r * a.E + e] = 0;
+#pragma unroll
+            for (int r = 1; r < kRows; ++r) p[0] += p[r], k[0] += k[r];
+            const float mean = __ull2float_rn(p[0]) * unit;
+            a.mean_probs[e] = mean;
+            a.expert_counts[e] = k[0];
+            dot += (float)k[0] * mean;
+            picks += k[0];
+        }
+        dot = warp_sum(dot);
+        picks = __reduce_add_sync(kFullMask, picks);
+        __syncthreads();
+        if (lane == 0) shared[warp] = dot, counts[warp] = picks;
         __syncthreads();
         if (warp == 0) {
-#pragma unroll
-            for (int w = 1; w < kWarps; ++w) p += psum[w][lane], k += csum[w][lane];
-            if (e < E) {
-                expert_counts[e] = k;
-                mean_probs[e] = p * inv;
-                dot += (float)k * (p * inv);
-                count += k;
+            dot = warp_sum(lane < kWarps ? shared[lane] : 0.f);
+            picks = __reduce_add_sync(kFullMask, lane < kWarps ? counts[lane] : 0);
+            if (lane == 0) {
+                *a.loss = picks ? a.coef * (float)a.E / (float)picks * dot : 0.f;
+                *a.tokens = n;
+                total[0] = total[1] = 0;
             }
         }
-        __syncthreads();
     }
-    if (warp == 0) {
-        dot = warp_sum(dot);
-        count = __reduce_add_sync(kFullMask, count);
-        if (lane == 0) share_dot = dot, share_count = count;
-    }
-    cluster.sync();
-    if (rank == 0 && threadIdx.x == 0) {
-        float d = 0.f;
-        int c = 0;
-        for (int r = 0; r < kFinishCtas; ++r) d += *cluster.map_shared_rank(&share_dot, r), c += *cluster.map_shared_rank(&share_count, r);
-        *loss = c ? coef * (float)E / (float)c * d : 0.f;
-        *tokens_out = tokens;
-    }
-    cluster.sync();                                                           // the other CTAs' words stay until they are read
 }
 
 // ---- gradient ----------------------------------------------------------------------------------------------------
@@ -308,20 +470,26 @@ struct RouteGradArgs {
     float scale, coef;
 };
 
+// One warp per token; the row, its scores and the gradient of the probabilities (the same for every token) stay in registers.
+// Bound by memory at large batches: a row is read and a row is written.
+constexpr int route_grad_ctas(int nv) { return nv <= 8 ? 5 : nv == 16 ? 3 : 2; }   // per SM
+
 template <class T, int NV>
-__global__ void __launch_bounds__(NV <= 32 ? 256 : 128)
+__global__ void __launch_bounds__(NV <= 32 ? 256 : 128, route_grad_ctas(NV))
 route_grad_kernel(const RouteGradArgs a)
 {
-    extern __shared__ float shared[];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    const int padded = NV * 32;
-    float *at_pick = shared + (size_t)warp * padded;                          // gradient of the picked scores, 0 elsewhere
-    float *f = shared + (size_t)warps * padded;                               // gradient of the probabilities, in the order of the lanes' values
+    extern __shared__ float4 shared4[];
+    constexpr int kWarps = NV <= 32 ? 8 : 4, kPadded = NV * 32 < 128 ? 128 : NV * 32;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    float *at_pick = reinterpret_cast<float *>(shared4) + (size_t)warp * kPadded;   // gradient of the picked scores, 0 elsewhere
     __shared__ int total;
     const bool soft = a.scoring == EP_SCORE_SOFTMAX, balance = a.counts != nullptr;
-    for (int i = lane; i < padded; i += 32) at_pick[i] = 0.f;
+    for (int i = lane; i < kPadded; i += 32) at_pick[i] = 0.f;
     if (threadIdx.x == 0) total = 0;
     __syncthreads();
+    float f[NV];                                                              // gradient of the probabilities
+#pragma unroll
+    for (int j = 0; j < NV; ++j) f[j] = 0.f;
     if (balance) {
         int n = 0;
         for (int e = threadIdx.x; e < a.E; e += blockDim.x) n += __ldg(a.counts + e);
@@ -330,44 +498,59 @@ route_grad_kernel(const RouteGradArgs a)
         __syncthreads();
         const int tokens = __ldg(a.tokens);
         const float unit = total && tokens ? __ldg(a.d_loss) * a.coef / (float)tokens * ((float)a.E / (float)total) : 0.f;
-        for (int i = threadIdx.x; i < padded; i += blockDim.x) {
-            const int e = expert_of<NV>(i >> 5, i & 31);
-            f[i] = e < a.E ? unit * (float)__ldg(a.counts + e) : 0.f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int e = expert_of<NV>(j, lane);
+            if (e < a.E) f[j] = unit * (float)__ldg(a.counts + e);
         }
-        __syncthreads();
     }
-    for (int t = blockIdx.x * warps + warp; t < a.T; t += gridDim.x * warps) {
+    // the next token's row, picks and gradients are requested before this one's are used
+    constexpr bool kAhead = NV <= 8;
+    float l_next[kAhead ? NV : 1], dw_next = 0.f;
+    int id_next = -1;
+    const auto fetch = [&](int t, float (&l)[kAhead ? NV : 1], int &id, float &dw) {
+        if (kAhead) load_row<NV>(static_cast<const T *>(a.logits) + (size_t)t * a.E, a.E, lane, a.vec, reinterpret_cast<float (&)[NV]>(l));
+        id = lane < a.K ? __ldg(a.topk_idx + (size_t)t * a.K + lane) : -1;
+        dw = lane < a.K && a.d_weights ? __ldg(a.d_weights + (size_t)t * a.K + lane) : 0.f;
+    };
+    const int first = blockIdx.x * kWarps + warp, stride = gridDim.x * kWarps;
+    if (first < a.T) fetch(first, l_next, id_next, dw_next);
+    for (int t = first; t < a.T; t += stride) {
         const T *row = static_cast<const T *>(a.logits) + (size_t)t * a.E;
         T *out = static_cast<T *>(a.dlogits) + (size_t)t * a.E;
         float l[NV];
-        load_row<NV>(row, a.E, lane, a.vec, l);
-        int id = -1;
-        float dw = 0.f;
-        if (lane < a.K) {
-            id = __ldg(a.topk_idx + (size_t)t * a.K + lane);
-            if (id < 0 || id >= a.E) id = -1;
-            if (id >= 0 && a.d_weights) dw = a.scale * __ldg(a.d_weights + (size_t)t * a.K + lane);
+        if (kAhead) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) l[j] = l_next[j % (kAhead ? NV : 1)];
+        } else {
+            load_row<NV>(row, a.E, lane, a.vec, l);
         }
+        int id = id_next >= 0 && id_next < a.E ? id_next : -1;
+        const float dw = id >= 0 ? a.scale * dw_next : 0.f;
+        if (t + stride < a.T) fetch(t + stride, l_next, id_next, dw_next);
+        clean_row<NV>(l);
         float top = l[0];
 #pragma unroll
         for (int j = 1; j < NV; ++j) top = fmaxf(top, l[j]);
-        top = warp_max(top);
-        const bool counted = top > -INFINITY && __any_sync(kFullMask, id >= 0);
-        float s[NV], sum = 0.f;
+        if (soft) top = warp_max(top);
+        const bool counted = __any_sync(kFullMask, top > -INFINITY) && __any_sync(kFullMask, id >= 0);
+        float s[NV], sum = 0.f, inv = 0.f;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            s[j] = !counted ? 0.f : soft ? expf(l[j] - top) : sigmoid(l[j]);
+            s[j] = counted ? rough_score(soft, l[j], top) : 0.f;
             sum += s[j];
         }
-        sum = warp_sum(sum);
-        const float inv = sum > 0.f ? 1.f / sum : 0.f;
+        if (soft || balance) {
+            sum = warp_sum(sum);
+            inv = sum > 0.f ? __fdividef(1.f, sum) : 0.f;
+        }
         // gradient with respect to the picked scores
         float mine = 0.f, picked_dot = 0.f;
         if (a.d_weights) {
             float v = 0.f;
             if (id >= 0 && counted) {
                 v = value(row, id);
-                v = !(v < INFINITY) || v == -INFINITY ? 0.f : soft ? expf(v - top) * inv : sigmoid(v);
+                v = !(v < INFINITY) || v == -INFINITY ? 0.f : exact_score(soft, v, top) * (soft ? inv : 1.f);
             }
             if (a.renormalize) {
                 const float picked = warp_sum(v), dot = warp_sum(dw * v);
@@ -375,26 +558,40 @@ route_grad_kernel(const RouteGradArgs a)
             } else {
                 mine = dw;
             }
-            picked_dot = warp_sum(mine * v);
+            if (soft) picked_dot = warp_sum(mine * v);
             if (id >= 0) at_pick[id] = mine;                                  // a token's picks are distinct
             __syncwarp();
         }
         float dot = 0.f;
         if (balance) {
 #pragma unroll
-            for (int j = 0; j < NV; ++j) dot += s[j] * f[j * 32 + lane];
+            for (int j = 0; j < NV; ++j) dot += s[j] * f[j];
             dot = warp_sum(dot) * inv;
         }
         float d[NV];
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const int e = expert_of<NV>(j, lane);
-            const float p = s[j] * inv, g = balance ? f[j * 32 + lane] - dot : 0.f, k = a.d_weights ? at_pick[e] : 0.f;
-            d[j] = soft ? p * (g + (k - picked_dot)) : (p * g + s[j] * k) * (1.f - s[j]);
+        for (int j = 0; j < NV; j += NV < 4 ? 1 : 4) {
+            float k[4] = {0.f, 0.f, 0.f, 0.f};
+            if (a.d_weights) {
+                if (NV < 4) {
+                    k[0] = at_pick[expert_of<NV>(j, lane)];
+                } else {
+                    const float4 q = *reinterpret_cast<const float4 *>(at_pick + expert_of<NV>(j, lane));
+                    k[0] = q.x, k[1] = q.y, k[2] = q.z, k[3] = q.w;
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < (NV < 4 ? 1 : 4); ++c) {
+                const int i = (j + c) % NV;
+                const float p = s[i] * inv, g = balance ? f[i] - dot : 0.f;
+                d[i] = soft ? p * (g + (k[c] - picked_dot)) : (p * g + s[i] * k[c]) * (1.f - s[i]);
+            }
         }
-        __syncwarp();
-        if (a.d_weights && id >= 0) at_pick[id] = 0.f;
-        __syncwarp();
+        if (a.d_weights) {
+            __syncwarp();
+            if (id >= 0) at_pick[id] = 0.f;
+            __syncwarp();
+        }
         if (NV >= 4 && a.vec) {
 #pragma unroll
             for (int j = 0; j < NV; j += 4) {
@@ -430,19 +627,17 @@ int check_router(const ep_router_t *r)
     return EP_OK;
 }
 
-int route_warps(int E) { return E <= 1024 ? 8 : 4; }
-
-int route_ctas(const ep_router_t &r)
-{
-    const int want = ceil_div(r.num_tokens, route_warps(r.num_experts));
-    return want < kMaxRouteCtas ? (want < 1 ? 1 : want) : kMaxRouteCtas;
-}
-
 int values_per_lane(int E)
 {
     int nv = 1;
     while (nv * 32 < E) nv *= 2;
     return nv;
+}
+
+int balance_ctas(const ep_router_t &r)
+{
+    const int want = ceil_div(r.num_tokens, route_warps(values_per_lane(r.num_experts), true));
+    return want < kBalanceCtas ? (want < 1 ? 1 : want) : kBalanceCtas;
 }
 
 bool rows_of_vectors(const ep_router_t &r, const void *p)   // may a lane load four neighbouring logits at once?
@@ -460,11 +655,12 @@ int allow_smem(Kernel kernel, size_t bytes)
 template <class T, int NV, int MODE>
 int launch_route(const RouteArgs &a, int ctas, cudaStream_t stream)
 {
-    const int warps = route_warps(a.E);
-    const size_t smem = MODE == kRoute ? 0 : ((size_t)warps * NV * 32 + a.E + 1) * 4;
+    constexpr int kWarps = route_warps(NV, MODE != kRoute);
+    if (MODE == kRoute) ctas = ceil_div(a.T, kWarps);
+    const size_t smem = ((size_t)kWarps * 2 * kListed + (MODE == kRoute ? 0 : (size_t)kWarps * NV * 32 + a.E + 1 + kWarps)) * 4;
     const int rc = allow_smem(route_kernel<T, NV, MODE>, smem);
     if (rc != EP_OK) return rc;
-    route_kernel<T, NV, MODE><<<ctas, warps * 32, smem, stream>>>(a);
+    route_kernel<T, NV, MODE><<<ctas, kWarps * 32, smem, stream>>>(a);
     EP_LAUNCH_CHECK(1);
     return EP_OK;
 }
@@ -472,13 +668,13 @@ int launch_route(const RouteArgs &a, int ctas, cudaStream_t stream)
 template <class T, int NV>
 int launch_route_grad(const RouteGradArgs &a, cudaStream_t stream)
 {
-    const int warps = route_warps(a.E);
-    const size_t smem = ((size_t)warps + 1) * NV * 32 * 4;
+    constexpr int kWarps = NV <= 32 ? 8 : 4, kPadded = NV * 32 < 128 ? 128 : NV * 32;
+    const size_t smem = (size_t)kWarps * kPadded * 4;
     const int rc = allow_smem(route_grad_kernel<T, NV>, smem);
     if (rc != EP_OK) return rc;
-    int ctas = ceil_div(a.T, warps);
-    if (ctas > 4 * 148) ctas = 4 * 148;
-    route_grad_kernel<T, NV><<<ctas, warps * 32, smem, stream>>>(a);
+    int ctas = ceil_div(a.T, kWarps);
+    if (ctas > route_grad_ctas(NV) * 148) ctas = route_grad_ctas(NV) * 148;   // one wave
+    route_grad_kernel<T, NV><<<ctas, kWarps * 32, smem, stream>>>(a);
     EP_LAUNCH_CHECK(1);
     return EP_OK;
 }
@@ -514,29 +710,27 @@ int check_balance(const ep_balance_t *b)
     return b->expert_counts && b->tokens && b->mean_probs && b->loss ? EP_OK : EP_ERR_NULL;
 }
 
-// The route kernel in the given mode, then (with a balance) the cluster that adds up.
 int run_route(const ep_router_t &r, RouteArgs &a, const ep_balance_t *b, bool pick, void *workspace, size_t workspace_bytes,
               cudaStream_t stream)
 {
     a.T = r.num_tokens, a.E = r.num_experts, a.K = r.top_k, a.scoring = r.scoring, a.renormalize = r.renormalize, a.scale = r.scale;
     a.vec = rows_of_vectors(r, a.logits);
-    int ctas = route_ctas(r);
+    a.vec_bias = r.num_experts % 4 == 0 && aligned16(a.bias);
     if (!b) {
         if (r.num_tokens == 0) return EP_OK;
-        return for_router(r, RunRoute<kRoute>{a, ceil_div(a.T, route_warps(a.E)), stream});
+        return for_router(r, RunRoute<kRoute>{a, 0, stream});
     }
     if (!workspace) return EP_ERR_NULL;
     if (!aligned16(workspace)) return EP_ERR_INVALID_ARG;
     if (workspace_bytes < ep_route_workspace_bytes(&r)) return EP_ERR_CAPACITY;
-    a.partial = static_cast<float *>(workspace);
-    a.partial_counts = reinterpret_cast<int32_t *>(a.partial + (size_t)ctas * a.E);
-    const int rc = pick ? for_router(r, RunRoute<kRouteBalance>{a, ctas, stream}) : for_router(r, RunRoute<kBalance>{a, ctas, stream});
-    if (rc != EP_OK) return rc;
-    EP_CUDA_TRY(launch_pdl(balance_finish_kernel, dim3(kFinishCtas), dim3(kFinishThreads), 0, stream, (const float *)a.partial,
-                           (const int32_t *)a.partial_counts, ctas, a.E, r.balance_coef, b->expert_counts, b->tokens, b->mean_probs,
-                           b->loss));
-    EP_LAUNCH_CHECK(1);
-    return EP_OK;
+    a.sums = static_cast<unsigned long long *>(workspace);
+    a.sum_counts = reinterpret_cast<int32_t *>(a.sums + (size_t)kRows * a.E);
+    a.shift = 62;                                                             // T probabilities of at most 1 and a little fit 63 bits
+    for (int64_t t = a.T; t > 0; t >>= 1) --a.shift;
+    a.expert_counts = b->expert_counts, a.tokens = b->tokens, a.mean_probs = b->mean_probs, a.loss = b->loss;
+    a.coef = r.balance_coef;
+    const int ctas = balance_ctas(r);
+    return pick ? for_router(r, RunRoute<kRouteBalance>{a, ctas, stream}) : for_router(r, RunRoute<kBalance>{a, ctas, stream});
 }
 
 }  // namespace
@@ -546,7 +740,7 @@ extern "C" size_t ep_route_workspace_bytes(const ep_router_t *r)
 {
     using namespace ep;
     if (check_router(r) != EP_OK) return 0;
-    return ((size_t)route_ctas(*r) * (2 * (size_t)r->num_experts + 1) * 4 + 15) & ~size_t(15);
+    return ((size_t)kRows * r->num_experts * 12 + 8 + 15) & ~size_t(15);
 }
 
 extern "C" int ep_route(const ep_router_t *r, const void *logits, const float *bias, int32_t *topk_idx, float *topk_weights,

@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from dataclasses import dataclass
+from dataclasses import dataclass, field
 
 import torch
 
@@ -160,6 +160,24 @@ def _want(t, dtype, name):
 
 def _stream():
     return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+
+
+def _at(t, shape, dtype, name):
+    """Address of a contiguous tensor of this shape and type; None stays None."""
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: the EP library needs contiguous tensors")
+    return t.data_ptr()
+
+
+def _stream_of(t):
+    """The current stream of the tensor's device, as an address."""
+    return torch._C._cuda_getCurrentRawStream(t.get_device())
 
 
 def _check(rc: int, where: str):
@@ -458,14 +476,25 @@ class Router:
     renormalize: bool = True
     scale: float = 1.0
     balance_coef: float = 0.0
+    _structs: dict = field(default_factory=dict, init=False, repr=False, compare=False)   # by batch size and type
 
-    def _struct(self, logits) -> _Router:
-        if logits.dtype not in (torch.float32, torch.bfloat16):
-            raise TypeError(f"logits must be float32 or bfloat16, got {logits.dtype}")
-        if logits.dim() != 2 or logits.shape[1] != self.num_experts:
-            raise ValueError(f"logits must be [T, {self.num_experts}], got {list(logits.shape)}")
-        return _Router(logits.shape[0], self.num_experts, self.top_k, DTYPE_F32 if logits.dtype == torch.float32 else DTYPE_BF16,
-                       int(self.scoring), int(bool(self.renormalize)), float(self.scale), float(self.balance_coef))
+    def _struct(self, logits):
+        """(a pointer to ep_router_t, T) for these logits."""
+        shape = logits.shape
+        if len(shape) != 2 or shape[1] != self.num_experts:
+            raise ValueError(f"logits must be [T, {self.num_experts}], got {list(shape)}")
+        key = (shape[0], logits.dtype)
+        st = self._structs.get(key)
+        if st is None:
+            if logits.dtype not in (torch.float32, torch.bfloat16):
+                raise TypeError(f"logits must be float32 or bfloat16, got {logits.dtype}")
+            if len(self._structs) >= 64:
+                self._structs.clear()
+            st = ctypes.pointer(_Router(shape[0], self.num_experts, self.top_k,
+                                        DTYPE_F32 if logits.dtype == torch.float32 else DTYPE_BF16, int(self.scoring),
+                                        int(bool(self.renormalize)), float(self.scale), float(self.balance_coef)))
+            self._structs[key] = st
+        return st, shape[0]
 
 
 @dataclass
@@ -480,10 +509,12 @@ class Routing:
     loss: torch.Tensor = None            # [1] fp32
     workspace: torch.Tensor = None
 
-    def _balance(self):
+    def _balance(self, E):
+        """A pointer to ep_balance_t, or None."""
         if self.expert_counts is None:
             return None
-        return ctypes.byref(_Balance(*[getattr(self, f).data_ptr() for f in _BALANCE_FIELDS]))
+        return ctypes.byref(_Balance(_at(self.expert_counts, (E,), torch.int32, "expert_counts"), _at(self.tokens, (1,), torch.int32, "tokens"),
+                                     _at(self.mean_probs, (E,), torch.float32, "mean_probs"), _at(self.loss, (1,), torch.float32, "loss")))
 
 
 def ep_route_workspace_bytes(T, K, E) -> int:
@@ -499,50 +530,36 @@ def alloc_routing(T, E, K, balance=False, topk_idx=None, device="cuda") -> Routi
     if balance:
         r.expert_counts, r.tokens = mk(torch.int32, E), mk(torch.int32, 1)
         r.mean_probs, r.loss = mk(torch.float32, E), mk(torch.float32, 1)
-        r.workspace = mk(torch.uint8, max(16, ep_route_workspace_bytes(T, K, E)))
+        r.workspace = torch.zeros(max(16, ep_route_workspace_bytes(T, K, E)), dtype=torch.uint8, device=device)   # zero between calls
     return r
-
-
-def _want_table(t, shape, dtype, name):
-    if t is not None:
-        _want(t, dtype, name)
-        if tuple(t.shape) != shape:
-            raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
-
-
-def _check_routing(r: Routing, T, E, K, weights=True):
-    _want_table(r.topk_idx, (T, K), torch.int32, "topk_idx"), _want_table(r.status, (1,), torch.int32, "status")
-    if weights:
-        _want_table(r.topk_weights, (T, K), torch.float32, "topk_weights")
-    _want_table(r.expert_counts, (E,), torch.int32, "expert_counts"), _want_table(r.tokens, (1,), torch.int32, "tokens")
-    _want_table(r.mean_probs, (E,), torch.float32, "mean_probs"), _want_table(r.loss, (1,), torch.float32, "loss")
 
 
 def ep_route(logits: torch.Tensor, router: Router, bias: torch.Tensor = None, out: Routing = None) -> Routing:
     """topk_idx and topk_weights [T, K] of logits [T, E] (fp32 or bf16); with an `out` that has them, expert counts, mean
     probabilities and the balance loss too. bias [E] (fp32) takes part in the selection only."""
-    st = router._struct(logits)
-    T, E, K = st.num_tokens, st.num_experts, st.top_k
+    st, T = router._struct(logits)
+    E, K = router.num_experts, router.top_k
     if out is None:
         out = alloc_routing(T, E, K, balance=router.balance_coef != 0.0, device=logits.device)
-    _check_routing(out, T, E, K), _want_table(bias, (E,), torch.float32, "bias")
-    _check(lib().ep_route(ctypes.byref(st), _ptr(logits), _ptr(bias), _ptr(out.topk_idx), _ptr(out.topk_weights), out._balance(),
-                          _ptr(out.status), _ptr(out.workspace), 0 if out.workspace is None else out.workspace.numel(),
-                          _stream()), "ep_route")
+    ws = out.workspace
+    _check(lib().ep_route(st, _at(logits, (T, E), logits.dtype, "logits"), _at(bias, (E,), torch.float32, "bias"),
+                          _at(out.topk_idx, (T, K), torch.int32, "topk_idx"), _at(out.topk_weights, (T, K), torch.float32, "topk_weights"),
+                          out._balance(E), _at(out.status, (1,), torch.int32, "status"), None if ws is None else _ptr(ws),
+                          0 if ws is None else ws.numel(), _stream_of(logits)), "ep_route")
     return out
 
 
 def ep_balance_loss(logits: torch.Tensor, router: Router, topk_idx: torch.Tensor, out: Routing = None) -> Routing:
     """Expert counts, mean probabilities and the balance loss for a routing table that is already there."""
-    st = router._struct(logits)
-    T, E, K = st.num_tokens, st.num_experts, st.top_k
+    st, T = router._struct(logits)
+    E, K = router.num_experts, router.top_k
     if out is None:
         out = alloc_routing(T, E, K, balance=True, topk_idx=topk_idx, device=logits.device)
-    _want_table(topk_idx, (T, K), torch.int32, "topk_idx"), _check_routing(out, T, E, K, weights=False)
     if out.expert_counts is None:
         raise ValueError("ep_balance_loss needs a Routing allocated with balance=True")
-    _check(lib().ep_balance_loss(ctypes.byref(st), _ptr(logits), _ptr(topk_idx), out._balance(), _ptr(out.status),
-                                 _ptr(out.workspace), out.workspace.numel(), _stream()), "ep_balance_loss")
+    _check(lib().ep_balance_loss(st, _at(logits, (T, E), logits.dtype, "logits"), _at(topk_idx, (T, K), torch.int32, "topk_idx"),
+                                 out._balance(E), _at(out.status, (1,), torch.int32, "status"), _ptr(out.workspace),
+                                 out.workspace.numel(), _stream_of(logits)), "ep_balance_loss")
     return out
 
 
@@ -550,48 +567,37 @@ def ep_route_backward(logits: torch.Tensor, router: Router, routing: Routing, d_
                       d_loss: torch.Tensor = None, dlogits: torch.Tensor = None) -> torch.Tensor:
     """Gradient of the weights (for d_weights [T, K]) and of the balance loss (for d_loss [1]), either or both, with respect
     to the logits; in the logits' type."""
-    st = router._struct(logits)
-    T, E, K = st.num_tokens, st.num_experts, st.top_k
+    st, T = router._struct(logits)
+    E, K = router.num_experts, router.top_k
     if dlogits is None:
         dlogits = torch.empty_like(logits)
-    _check_routing(routing, T, E, K, weights=False), _want_table(d_weights, (T, K), torch.float32, "d_weights")
-    _want_table(d_loss, (1,), torch.float32, "d_loss"), _want_table(dlogits, (T, E), logits.dtype, "dlogits")
     if d_loss is not None and routing.expert_counts is None:
         raise ValueError("the gradient of the balance loss needs the Routing that holds its counts")
-    _check(lib().ep_route_backward(ctypes.byref(st), _ptr(logits), _ptr(routing.topk_idx), _ptr(d_weights),
-                                   routing._balance() if d_loss is not None else None, _ptr(d_loss), _ptr(dlogits), _stream()),
-           "ep_route_backward")
+    _check(lib().ep_route_backward(st, _at(logits, (T, E), logits.dtype, "logits"), _at(routing.topk_idx, (T, K), torch.int32, "topk_idx"),
+                                   _at(d_weights, (T, K), torch.float32, "d_weights"),
+                                   None if d_loss is None else routing._balance(E), _at(d_loss, (1,), torch.float32, "d_loss"),
+                                   _at(dlogits, (T, E), logits.dtype, "dlogits"), _stream_of(logits)), "ep_route_backward")
     return dlogits
 
 
-def _matmul_args(rows, weight, expert_offsets, activation, operand_op) -> _Matmul:
-    _want(weight, torch.bfloat16, "weight"), _want(expert_offsets, torch.int32, "expert_offsets")
+def _matmul_args(rows, weight, expert_offsets, activation, operand_op):
+    """(ep_matmul_t, rows, experts, out features, in features)"""
     E, N, H = weight.shape
-    if expert_offsets.numel() != E + 1:
-        raise ValueError(f"expert_offsets must hold {E + 1} entries for {E} experts, got {expert_offsets.numel()}")
-    return _Matmul(int(rows), int(H), int(N), int(E), int(activation), int(operand_op))
-
-
-def _want_rows(t, rows, cols, name):
-    """A [rows, cols] bf16 tensor, or None."""
-    if t is not None:
-        _want(t, torch.bfloat16, name)
-        if tuple(t.shape) != (rows, cols):
-            raise ValueError(f"{name} must be [{rows}, {cols}], got {list(t.shape)}")
+    return _Matmul(rows, H, N, E, activation, operand_op), E, N, H
 
 
 def ep_expert_matmul(x, expert_offsets, weight, bias=None, activation=ACT_NONE, operand=None, operand_op=OPERAND_ADD, y=None,
                      pre=None, status=None):
     """y[p] = act(x[p] weight[e]^T + bias[e]) (+ or *) operand[p] for the rows p of expert e's segment of the pair space.
     x [rows, in], weight [experts, out, in], bias [experts, out], operand, y and pre [rows, out], all bf16."""
-    m = _matmul_args(x.shape[0], weight, expert_offsets, activation, operand_op)
-    E, N, H = weight.shape
-    _want_rows(x, m.rows, H, "x"), _want_rows(operand, m.rows, N, "operand"), _want_rows(bias, E, N, "bias")
+    bf, P = torch.bfloat16, x.shape[0]
+    m, E, N, H = _matmul_args(P, weight, expert_offsets, activation, operand_op)
     if y is None:
-        y = torch.empty(m.rows, N, dtype=torch.bfloat16, device=x.device)
-    _want_rows(y, m.rows, N, "y"), _want_rows(pre, m.rows, N, "pre")
-    _check(lib().ep_expert_matmul(ctypes.byref(m), _ptr(x), _ptr(expert_offsets), _ptr(weight), _ptr(bias), _ptr(operand), _ptr(y),
-                                  _ptr(pre), _ptr(status), _stream()), "ep_expert_matmul")
+        y = torch.empty(P, N, dtype=bf, device=x.device)
+    _check(lib().ep_expert_matmul(ctypes.byref(m), _at(x, (P, H), bf, "x"), _at(expert_offsets, (E + 1,), torch.int32, "expert_offsets"),
+                                  _at(weight, (E, N, H), bf, "weight"), _at(bias, (E, N), bf, "bias"), _at(operand, (P, N), bf, "operand"),
+                                  _at(y, (P, N), bf, "y"), _at(pre, (P, N), bf, "pre"), _at(status, (1,), torch.int32, "status"),
+                                  _stream_of(x)), "ep_expert_matmul")
     return y
 
 
@@ -625,24 +631,17 @@ def ep_expert_matmul_backward(dy, x, expert_offsets, weight, pre=None, activatio
                               grads: ExpertGrads = None, status=None) -> ExpertGrads:
     """The gradients of `ep_expert_matmul` for dy, written to the tensors that `grads` has (default: dx and dweight).
     `pre` is what the forward call wrote; the gradient of an added operand is dy itself."""
-    m = _matmul_args(dy.shape[0], weight, expert_offsets, activation, operand_op)
-    E, N, H = weight.shape
+    bf, P = torch.bfloat16, dy.shape[0]
+    m, E, N, H = _matmul_args(P, weight, expert_offsets, activation, operand_op)
     if grads is None:
-        grads = alloc_expert_grads(m.rows, H, N, E, device=dy.device)
-    _want_rows(dy, m.rows, N, "dy"), _want_rows(x, m.rows, H, "x"), _want_rows(pre, m.rows, N, "pre")
-    _want_rows(operand, m.rows, N, "operand"), _want_rows(grads.dx, m.rows, H, "dx"), _want_rows(grads.doperand, m.rows, N, "doperand")
-    if grads.dweight is not None:
-        _want(grads.dweight, torch.bfloat16, "dweight")
-        if grads.dweight.shape != weight.shape:
-            raise ValueError(f"dweight must be {list(weight.shape)}, got {list(grads.dweight.shape)}")
-    if grads.dbias is not None:
-        _want(grads.dbias, torch.float32, "dbias")
-        if tuple(grads.dbias.shape) != (E, N):
-            raise ValueError(f"dbias must be [{E}, {N}], got {list(grads.dbias.shape)}")
+        grads = alloc_expert_grads(P, H, N, E, device=dy.device)
     _check(lib().ep_expert_matmul_backward(
-        ctypes.byref(m), _ptr(dy), _ptr(x), _ptr(expert_offsets), _ptr(weight), _ptr(pre), _ptr(operand), _ptr(grads.dx),
-        _ptr(grads.dweight), _ptr(grads.dbias), _ptr(grads.doperand), _ptr(status), _ptr(grads.workspace),
-        grads.workspace.numel(), _stream()), "ep_expert_matmul_backward")
+        ctypes.byref(m), _at(dy, (P, N), bf, "dy"), _at(x, (P, H), bf, "x"),
+        _at(expert_offsets, (E + 1,), torch.int32, "expert_offsets"), _at(weight, (E, N, H), bf, "weight"), _at(pre, (P, N), bf, "pre"),
+        _at(operand, (P, N), bf, "operand"), _at(grads.dx, (P, H), bf, "dx"), _at(grads.dweight, (E, N, H), bf, "dweight"),
+        _at(grads.dbias, (E, N), torch.float32, "dbias"), _at(grads.doperand, (P, N), bf, "doperand"),
+        _at(status, (1,), torch.int32, "status"), _ptr(grads.workspace), grads.workspace.numel(), _stream_of(dy)),
+        "ep_expert_matmul_backward")
     return grads
 
 

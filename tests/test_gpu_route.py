@@ -278,19 +278,21 @@ def test_outputs_stay_inside_their_buffers():
     nws = ep.ep_route_workspace_bytes(T, K, E)
     whole = {}
 
-    def carve(name, dtype, *shape):
+    def carve(name, dtype, *shape, fill=77):
         n = math.prod(shape)
         whole[name] = torch.full((n + 32,), 77, dtype=dtype, device="cuda")
+        whole[name][16:16 + n] = fill
         return whole[name][16:16 + n].view(*shape)
 
     out = ep.Routing(carve("idx", torch.int32, T, K), carve("w", torch.float32, T, K), torch.zeros(1, dtype=torch.int32, device="cuda"),
                      carve("counts", torch.int32, E), carve("tokens", torch.int32, 1), carve("mean", torch.float32, E),
-                     carve("loss", torch.float32, 1), carve("ws", torch.uint8, nws))
+                     carve("loss", torch.float32, 1), carve("ws", torch.uint8, nws, fill=0))
     ep.ep_route(logits, router, out=out)
     grad = carve("grad", torch.bfloat16, T, E)
     ep.ep_route_backward(logits, router, out, d_weights=torch.ones(T, K, device="cuda"), d_loss=torch.ones(1, device="cuda"), dlogits=grad)
     for name, t in whole.items():
         assert (t[:16] == 77).all() and (t[-16:] == 77).all(), name
+    assert (out.workspace == 0).all()                           # left for the next call as it was found
 
 
 def test_a_large_table_agrees_with_its_parts():
