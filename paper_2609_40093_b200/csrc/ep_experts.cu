@@ -14,6 +14,9 @@
 //   dx        in features     rows            out features     W, MN-major              dz, K-major
 //   dweight   in features     out features    rows             x, MN-major              dz, MN-major
 //
+// Where there are fewer tiles than SMs, tiles get narrower (down to 64 columns), and then up to eight CTAs of a cluster share a
+// tile, each with a part of the contracted axis, and add their accumulators through each other's shared memory in a fixed order.
+//
 // One persistent CTA per SM. A warp keeps a ring of shared-memory stages full by TMA (64 of the contracted axis each), one
 // thread issues the products, four warps empty the accumulators, of which there are two of 256 columns, so that a tile's
 // epilogue runs under the next tile's products. Rows behind a segment's end that a box brings along only feed columns that
@@ -35,6 +38,8 @@ constexpr int kAccColumns = 256;          // columns of one of the two accumulat
 constexpr int kBytesA = kTileM * kTileK * 2;
 constexpr int kStageLd = 36, kStageWords = 16 * kStageLd;      // an epilogue warp's buffer: 16 columns of 32 lanes
 constexpr int kStageBytes = kEpilogueWarps * kStageWords * 4;
+constexpr int kSplitColumns = 64, kExchangeLd = kTileM + 4;    // a shared tile's accumulators as its CTAs exchange them
+constexpr int kExchangeBytes = kSplitColumns * kExchangeLd * 4;
 constexpr int kMaxStages = 12;
 constexpr int kSmemLimit = 227 * 1024;
 
@@ -46,6 +51,7 @@ struct ProductArgs {
     int E;
     int columns;                          // columns per tile at most
     int stages;
+    int split;                            // CTAs that share a tile
     uint16_t *out;
     const CUtensorMap *segment_maps;      // dweight: [E][2]
     // forward epilogue
@@ -106,15 +112,15 @@ __device__ __forceinline__ void act_both(int act, float z, float &value, float &
 // Tiles are dealt out to the CTAs (pairs) round by round, an expert's row pieces next to each other, then its feature tiles: what
 // runs at the same time shares rows and weights in L2. Neither experts sorted by cost nor a shared counter was faster, with
 // segments of even and of Zipf-distributed lengths (counter: 3 to 6 % slower; order: within 2 % either way).
-template <int MODE, int CG>
+template <int MODE, int CG, bool SPLIT>
 struct Walk {
     const ProductArgs &a;
     const int *first_tile;   // [E+1] shared memory: tiles of the experts before e (forward, dx)
     const int *bound;        // [E+1] the segments' bounds, clamped
-    int m_tiles, n_tiles, total, tile, step;
+    int m_tiles, n_tiles, total, tile, step, part;
 
-    __device__ Walk(const ProductArgs &args, const int *first, const int *b, int start, int stride)
-        : a(args), first_tile(first), bound(b), tile(start), step(stride)
+    __device__ Walk(const ProductArgs &args, const int *first, const int *b, int start, int stride, int which)
+        : a(args), first_tile(first), bound(b), tile(start), step(stride), part(which)
     {
         m_tiles = (a.M + kTileM * CG - 1) / (kTileM * CG);
         n_tiles = MODE == kDweight ? (a.N + a.columns - 1) / a.columns : 0;
@@ -152,6 +158,11 @@ struct Walk {
             t.nk = (a.K + kTileK - 1) / kTileK;
         }
         t.n = max(kStep, (t.cols + kStep - 1) / kStep * kStep);
+        if (SPLIT) {                                     // this CTA's part of the contracted axis (may be empty)
+            const int from = t.nk * part / a.split, to = t.nk * (part + 1) / a.split;
+            t.k0 += from * kTileK;
+            t.nk = to - from;
+        }
         tile += step;
         return true;
     }
@@ -211,24 +222,43 @@ __device__ __forceinline__ void finish8(const ProductArgs &a, float (&z)[8], con
 
 // ---- the kernel --------------------------------------------------------------------------------------------------
 
-template <int MODE, int CG>
+// 8 features of a row: the mode's arithmetic and the store. operand: as loaded, if there is one.
+template <int MODE>
+__device__ __forceinline__ void finish_row(const ProductArgs &a, float (&z)[8], const float (&bias)[8], const uint4 &operand, size_t at)
+{
+    if (MODE == kForward) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) z[j] += bias[j];
+        switch (a.activation) {
+        case EP_ACT_RELU: finish8<EP_ACT_RELU>(a, z, operand, at); break;
+        case EP_ACT_SILU: finish8<EP_ACT_SILU>(a, z, operand, at); break;
+        case EP_ACT_GELU: finish8<EP_ACT_GELU>(a, z, operand, at); break;
+        default: finish8<EP_ACT_NONE>(a, z, operand, at); break;
+        }
+    } else {
+        *reinterpret_cast<uint4 *>(a.out + at) = pack8(z);
+    }
+}
+
+template <int MODE, int CG, bool SPLIT>
 __global__ void __launch_bounds__(kThreads, 1)
 product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ ColumnMaps map_b)
 {
     extern __shared__ char raw[];
-    __shared__ uint64_t full_[kMaxStages], empty_[kMaxStages], acc_full_[2], acc_empty_[2];
+    __shared__ uint64_t full_[kMaxStages], empty_[kMaxStages], acc_full_[2], acc_empty_[2], ex_full_;
     __shared__ uint32_t tmem_slot;
     __shared__ int gave_up_;
     __shared__ int warp_sum[kThreads / 32];
     volatile int *gave_up = &gave_up_;
 
     const int warp = __shfl_sync(kFullMask, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;   // uniform in the warp, and seen to be
-    const uint32_t rank = CG == 2 ? cluster_rank() : 0;
+    const uint32_t rank = CG == 2 ? cluster_rank() : 0, part = SPLIT ? cluster_rank() : 0;
+    const int split = SPLIT ? a.split : 1;
     const int b_bytes = max(32, a.columns / CG) * kTileK * 2;
     const int stage_bytes = kBytesA + b_bytes;
     const uint32_t ring_base = (smem_addr(raw) + 1023) & ~1023u;
     char *tables = raw + (ring_base - smem_addr(raw)) + (size_t)a.stages * stage_bytes;
-    int *first_tile = reinterpret_cast<int *>(tables + kStageBytes), *bound = first_tile + a.E + 1;   // the epilogue's buffers first
+    int *first_tile = reinterpret_cast<int *>(tables + (SPLIT ? kExchangeBytes : kStageBytes)), *bound = first_tile + a.E + 1;   // the epilogue's buffers first
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < a.stages; ++s) {
@@ -239,6 +269,7 @@ product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, c
             bar_init(smem_addr(&acc_full_[s]), 1);
             bar_init(smem_addr(&acc_empty_[s]), kEpilogueWarps * CG);
         }
+        if (SPLIT) bar_init(smem_addr(&ex_full_), split * kEpilogueWarps);
         gave_up_ = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -274,11 +305,12 @@ product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, c
         if (threadIdx.x == kThreads - 1) first_tile[a.E] = run;
     }
     tmem_fence_before();
-    if (CG == 2) cluster_sync();
+    if (CG == 2 || SPLIT) cluster_sync();
     __syncthreads();
     tmem_fence_after();
     const uint32_t tmem = tmem_slot;
-    Walk<MODE, CG> walk(a, first_tile, bound, blockIdx.x / CG, gridDim.x / CG);   // one per role
+    const int sharing = CG * split;
+    Walk<MODE, CG, SPLIT> walk(a, first_tile, bound, blockIdx.x / sharing, gridDim.x / sharing, part);   // one per role
     const uint32_t full0 = smem_addr(full_), empty0 = smem_addr(empty_), full0_leader = CG == 2 ? in_cta(full0, 0) : full0;
     constexpr bool kAMn = MODE != kForward, kBMn = MODE == kDweight;
     Tile t;
@@ -360,6 +392,50 @@ product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, c
             mma_commit<CG>(smem_addr(&acc_full_[acc]));
             ++used;
         }
+    } else if (SPLIT && warp >= 4) {
+        // ---- accumulators out, of a tile that `split` CTAs share: each writes its sums down, and finishes some of the columns
+        const int q = warp & 3, first = (warp - 4) / 4 * 32, thread = threadIdx.x - 128;
+        float *mine = reinterpret_cast<float *>(tables);
+        const size_t ld = a.M;
+        bool ok = walk.next(t);                                              // the grid has a cluster per tile: there is no second one
+        if (ok && t.nk) {
+            ok = bar_wait(smem_addr(&acc_full_[0]), 0, gave_up);
+            tmem_fence_after();
+        }
+        if (ok) {
+            if (first < t.cols) {
+                uint32_t v[32];
+                if (t.nk) {
+                    tmem_load32(tmem + (uint32_t(q * 32) << 16) + first, v);
+                } else {
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) v[c] = 0u;
+                }
+#pragma unroll
+                for (int c = 0; c < 32; ++c) mine[(first + c) * kExchangeLd + q * 32 + lane] = __uint_as_float(v[c]);
+            }
+            __syncwarp();
+            if (lane < split) bar_arrive_cluster_release(in_cta(smem_addr(&ex_full_), lane));
+            ok = bar_wait<true>(smem_addr(&ex_full_), 0, gave_up);
+        }
+        const int width = ok ? (t.cols + split - 1) / split : 0;
+        for (int i = thread; i < width * (kTileM / 8); i += 32 * kEpilogueWarps) {
+            const int c = part * width + i / (kTileM / 8), f = i % (kTileM / 8) * 8, feature = t.m0 + f;
+            if (c >= t.cols || feature >= a.M) continue;
+            const size_t at = ((MODE == kDweight ? (size_t)t.e * a.N + t.c0 : (size_t)t.c0) + c) * ld + feature;
+            float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, bias[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            uint4 operand = make_uint4(0u, 0u, 0u, 0u);
+            if (MODE == kForward) {
+                if (a.bias) unpack8(__ldg(reinterpret_cast<const uint4 *>(a.bias + (size_t)t.e * a.M + feature)), bias);
+                if (a.operand) operand = *reinterpret_cast<const uint4 *>(a.operand + at);
+            }
+            const uint32_t from = smem_addr(mine + c * kExchangeLd + f);
+            for (int s = 0; s < split; ++s) {
+                const float4 lo = load_cluster(in_cta(from, s)), hi = load_cluster(in_cta(from, s) + 16);
+                z[0] += lo.x, z[1] += lo.y, z[2] += lo.z, z[3] += lo.w, z[4] += hi.x, z[5] += hi.y, z[6] += hi.z, z[7] += hi.w;
+            }
+            finish_row<MODE>(a, z, bias, operand, at);
+        }
     } else if (warp >= 4) {
         // ---- accumulators out
         const int q = warp & 3, first = (warp - 4) / 4 * 32;                 // a warp reaches the lanes 32 (warp mod 4) .. + 31
@@ -419,18 +495,13 @@ product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, c
                                 const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
                                 float z[8];
 #pragma unroll
-                                for (int j = 0; j < 8; ++j) z[j] = __uint_as_float(w[j]) + bias[j];
+                                for (int j = 0; j < 8; ++j) z[j] = __uint_as_float(w[j]);
                                 const size_t at = corner + c * ld;
                                 const uint4 mine = r[2 * h + i];
                                 // the same columns of the warp's next block (the operand may be y itself: an ordinary load)
                                 if (a.operand && c + kStep < cols)
                                     r[2 * h + i] = *reinterpret_cast<const uint4 *>(a.operand + at + kStep * ld);
-                                switch (a.activation) {
-                                case EP_ACT_RELU: finish8<EP_ACT_RELU>(a, z, mine, at); break;
-                                case EP_ACT_SILU: finish8<EP_ACT_SILU>(a, z, mine, at); break;
-                                case EP_ACT_GELU: finish8<EP_ACT_GELU>(a, z, mine, at); break;
-                                default: finish8<EP_ACT_NONE>(a, z, mine, at); break;
-                                }
+                                finish_row<MODE>(a, z, bias, mine, at);
                             }
                         }
                     }
@@ -465,7 +536,7 @@ product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, c
     __syncwarp();
     tmem_fence_before();
     __syncthreads();
-    if (CG == 2) cluster_sync();                                             // the peer's signals land in this CTA's memory
+    if (CG == 2 || SPLIT) cluster_sync();                                    // the others' signals land in, and their reads come from, this CTA's memory
     tmem_fence_after();
     if (warp == 2) tmem_free<CG>(tmem, 2 * kAccColumns);
     if (threadIdx.x == 0 && gave_up_ && a.status) atomicOr(a.status, EP_STATUS_TIMEOUT);
@@ -630,37 +701,58 @@ int sm_count(int *n)
     return EP_OK;
 }
 
-template <int MODE, int CG>
+template <int MODE, int CG, bool SPLIT>
 int launch_product(ProductArgs a, const CUtensorMap &map_a, const ColumnMaps &map_b, int64_t max_tiles, cudaStream_t stream)
 {
     int sms = 0;
     const int rc = sm_count(&sms);
     if (rc != EP_OK) return rc;
     const int stage = kBytesA + (a.columns / CG < 32 ? 32 : a.columns / CG) * kTileK * 2;
-    const int tables = kStageBytes + 2 * (a.E + 1) * 4;
+    const int tables = (SPLIT ? kExchangeBytes : kStageBytes) + 2 * (a.E + 1) * 4;
     a.stages = (kSmemLimit - 2048 - tables) / stage;                         // 2048: alignment of the ring, static words
     if (a.stages > kMaxStages) a.stages = kMaxStages;
     int smem = 1024 + a.stages * stage + tables;
     if (smem < 120 * 1024) smem = 120 * 1024;                                // one CTA per SM: it holds all of the tensor memory
-    EP_CUDA_TRY(cudaFuncSetAttribute(product_kernel<MODE, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    int64_t pairs = sms / CG;
-    if (max_tiles < pairs) pairs = max_tiles;
+    EP_CUDA_TRY(cudaFuncSetAttribute(product_kernel<MODE, CG, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    const int sharing = SPLIT ? a.split : CG;
+    int64_t groups = sms / sharing;
+    if (max_tiles < groups || SPLIT) groups = max_tiles;                     // a shared tile has a cluster of its own
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(pairs * CG));
+    cfg.gridDim = dim3((unsigned)(groups * sharing));
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = CG;
+    attr[0].val.clusterDim.x = sharing;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    EP_CUDA_TRY(cudaLaunchKernelEx(&cfg, product_kernel<MODE, CG>, a, map_a, map_b));
+    EP_CUDA_TRY(cudaLaunchKernelEx(&cfg, product_kernel<MODE, CG, SPLIT>, a, map_a, map_b));
     EP_LAUNCH_CHECK(1);
     return EP_OK;
+}
+
+// Picks the launch for tiles of at most a.columns columns. `pieces(columns)`: column tiles over all experts; `stages`: 64-element
+// stages of the contracted axis of an average tile.
+template <int MODE, class Pieces>
+int launch_tiles(ProductArgs a, const CUtensorMap &map_a, const ColumnMaps &map_b, Pieces pieces, int64_t stages, cudaStream_t stream)
+{
+    const int64_t features = (a.M + kTileM - 1) / kTileM, pairs = (a.M + 2 * kTileM - 1) / (2 * kTileM);
+    // Pairs of CTAs (256 features per tile, each operand row fetched once for both) wherever there is work for all pairs; with few
+    // rows per expert the time is that of reading the weights and single CTAs spread it better. 128 experts of 1024 x 2048 on one
+    // box: 16 rows each 86.9 us single, 88.9 paired; 256 experts of 2048 x 7168, 256 rows each: 1989 single, 1728 paired.
+    if (a.columns >= 128 && pieces(a.columns) * pairs >= 74) return launch_product<MODE, 2, false>(a, map_a, map_b, pieces(a.columns) * pairs, stream);
+    // Fewer tiles than SMs: narrower tiles, then CTAs that share a tile (at least four stages each).
+    while (a.columns > kSplitColumns && pieces(a.columns) * features < 148) a.columns /= 2;
+    const int64_t tiles = pieces(a.columns) * features;
+    if (tiles >= (int64_t(1) << 31) - (1 << 20)) return EP_ERR_INVALID_ARG;
+    a.split = 1;
+    while (a.split < 8 && tiles * a.split * 2 <= 148 && stages >= 8 * a.split) a.split *= 2;
+    if (a.split > 1) return launch_product<MODE, 1, true>(a, map_a, map_b, tiles, stream);
+    return launch_product<MODE, 1, false>(a, map_a, map_b, tiles, stream);
 }
 
 int make_row_maps(TensorMapEncode encode, ColumnMaps *maps, const void *rows, int features, int64_t n)
@@ -681,18 +773,11 @@ int row_columns(int64_t rows, int E)
 }
 
 
-// Pairs of CTAs (256 features per tile, each operand row fetched once for both) wherever there is work for all pairs; with few
-// rows per expert the time is that of reading the weights and single CTAs spread it better. 128 experts of 1024 x 2048 on one
-// box: 16 rows each 86.9 us single, 88.9 paired; 256 experts of 2048 x 7168, 256 rows each: 1989 single, 1728 paired.
-constexpr int64_t kPairTiles = 74;
-
 template <int MODE>
 int launch_rows(const ProductArgs &a, const CUtensorMap &map_a, const ColumnMaps &map_b, cudaStream_t stream)
 {
-    const int64_t pieces = (a.rows < a.E ? a.rows : a.E) + a.rows / a.columns;    // at most
-    const int64_t single = pieces * ((a.M + kTileM - 1) / kTileM), paired = pieces * ((a.M + 2 * kTileM - 1) / (2 * kTileM));
-    if (a.columns >= 128 && paired >= kPairTiles) return launch_product<MODE, 2>(a, map_a, map_b, paired, stream);
-    return launch_product<MODE, 1>(a, map_a, map_b, single, stream);
+    const auto pieces = [&](int columns) { return (a.rows < a.E ? a.rows : a.E) + a.rows / columns; };   // at most
+    return launch_tiles<MODE>(a, map_a, map_b, pieces, (a.K + kTileK - 1) / kTileK, stream);
 }
 
 // Rows per run of the slope kernel: about 40 warps per SM (a warp is one run of 256 columns), runs of at least 8 rows, and no
@@ -868,11 +953,8 @@ extern "C" int ep_expert_matmul_backward(const ep_matmul_t *m, const void *dy, c
         a.out = static_cast<uint16_t *>(dweight);
         a.segment_maps = maps;
         a.columns = kAccColumns;
-        const int64_t per = (int64_t)E * ((a.N + a.columns - 1) / a.columns), tiles = per * ((a.M + kTileM - 1) / kTileM);
-        const int64_t pair_tiles = per * ((a.M + 2 * kTileM - 1) / (2 * kTileM));
-        if (tiles >= (int64_t(1) << 31) - (1 << 20)) return EP_ERR_INVALID_ARG;
-        rc = pair_tiles >= kPairTiles ? launch_product<kDweight, 2>(a, map_a, map_b, pair_tiles, stream)
-                                      : launch_product<kDweight, 1>(a, map_a, map_b, tiles, stream);
+        const auto pieces = [&](int columns) { return (int64_t)a.E * ((a.N + columns - 1) / columns); };
+        rc = launch_tiles<kDweight>(a, map_a, map_b, pieces, m->rows / m->num_experts / kTileK, stream);
         if (rc != EP_OK) return rc;
     }
     return EP_OK;

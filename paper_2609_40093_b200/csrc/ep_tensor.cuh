@@ -49,24 +49,34 @@ __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count)
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
 }
 
+// CLUSTER: what another CTA of the cluster released with its arrival is seen afterwards.
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity)
 {
     uint32_t ok;
-    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
-                 : "=r"(ok)
-                 : "r"(bar), "r"(parity)
-                 : "memory");
+    if (CLUSTER)
+        asm volatile(
+            "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+            : "=r"(ok)
+            : "r"(bar), "r"(parity)
+            : "memory");
+    else
+        asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+                     : "=r"(ok)
+                     : "r"(bar), "r"(parity)
+                     : "memory");
     return ok != 0;
 }
 
 // Waits for the phase of the given parity to end. False if it did not within the limit, or if another warp of the block
 // gave up before (*gave_up, shared memory): the caller then leaves its loop.
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *gave_up)
 {
-    if (bar_try(bar, parity)) return true;
+    if (bar_try<CLUSTER>(bar, parity)) return true;
     const long long start = clock64();
     for (;;) {
-        if (bar_try(bar, parity)) return true;
+        if (bar_try<CLUSTER>(bar, parity)) return true;
         if (*gave_up) return false;
         if (clock64() - start > kWaitCycles) {
             *gave_up = 1;
@@ -93,6 +103,19 @@ __device__ __forceinline__ uint32_t in_cta(uint32_t addr, uint32_t rank)
 __device__ __forceinline__ void bar_arrive_cluster(uint32_t bar)
 {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+// The same with release semantics: what this thread (and, after a __syncwarp, its warp) read and wrote before is done for who waits.
+__device__ __forceinline__ void bar_arrive_cluster_release(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+__device__ __forceinline__ float4 load_cluster(uint32_t addr)
+{
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
 }
 
 // --- TMA --------------------------------------------------------------------------------------------------------

@@ -115,23 +115,25 @@ def experts(x, offsets, weight, bias=None, name="none", operand=None, mul=False)
 
 
 def experts_gradient(dy, x, offsets, weight, pre, name="none", operand=None, mul=False):
-    """dx, dweight, dbias, doperand and, for the error bounds, the same sums over absolute values (all 64 bits)."""
+    """dx, dweight, dbias, doperand and, for the error bounds, the same sums over absolute values (all 64 bits); size["slope"] is
+    what an error of 1 in the slope of every row would do to dbias, weighted with 1 + |z|."""
     P = int(offsets[-1])
     E, N, H = weight.shape
     g = dy[:P].double()
     z = pre[:P].double() if pre is not None else torch.zeros_like(g)
-    dz = g * slope(z, name)
-    dop = None
+    dop = g * act(z, name) if mul else None
     if mul:
-        dop = g * act(z, name)
-        dz = dz * operand[:P].double()
+        g = g * operand[:P].double()
+    dz = g * slope(z, name)
     out = {"dx": torch.zeros(P, H, dtype=torch.float64, device=dy.device),
            "dweight": torch.zeros(E, N, H, dtype=torch.float64, device=dy.device),
            "dbias": torch.zeros(E, N, dtype=torch.float64, device=dy.device), "doperand": dop}
     size = {k: torch.zeros_like(v) for k, v in out.items() if k != "doperand"}
+    size["slope"] = torch.zeros_like(out["dbias"])
     for e, rows in enumerate(segments(offsets)):
         xe, we, de = x[rows].double(), weight[e].double(), dz[rows]
         out["dx"][rows], size["dx"][rows] = de @ we, de.abs() @ we.abs()
         out["dweight"][e], size["dweight"][e] = de.t() @ xe, de.t().abs() @ xe.abs()
         out["dbias"][e], size["dbias"][e] = de.sum(0), de.abs().sum(0)
+        size["slope"][e] = (g[rows].abs() * (1 + z[rows].abs())).sum(0)
     return out, size

@@ -133,7 +133,7 @@ def _check_backward(c, name="none", op="none", wanted=("dx", "dweight", "dbias",
         got = got[:P] if key == "dx" else got
         err = (got.double() - want[key]).abs()
         if key == "dbias":
-            tol = (n * 2.0 ** -23 + 2.0 ** -16) * size[key]
+            tol = (n * 2.0 ** -23 + 2.0 ** -16) * size[key] + 2.0 ** -18 * size["slope"]   # the slope's error is not relative: it has a zero
         else:
             tol = 2.0 ** -8 * want[key].abs() + (2.0 ** -8 + n * 2.0 ** -23) * size[key]
         assert (err <= tol + 1e-30).all(), (key, float((err - tol).max()))
@@ -250,6 +250,23 @@ def test_rows_past_four_gigabytes():
         assert ((y[p].double() - want).abs() <= 2.0 ** -8 * want.abs() + 1e-4).all(), p
         want, size = y[p].double() @ w[e].double(), y[p].double().abs() @ w[e].double().abs()
         assert ((dx[p].double() - want).abs() <= 2.0 ** -8 * want.abs() + N * 2.0 ** -23 * size).all(), p
+
+
+@pytest.mark.parametrize("counts,H,N", [([1], 4096, 64), ([5, 0, 40], 2048, 136), ([64, 1], 1032, 264), ([130], 520, 128), ([300, 20], 4104, 72)])
+def test_few_tiles_shared_by_several_blocks(counts, H, N):
+    """Long contracted axes and few tiles: the axis is cut into up to eight parts, of unequal length and with ragged ends."""
+    c = _case(counts, H, N, seed=H, slack=2)
+    for name, op in (("none", "none"), ("gelu", "add"), ("silu", "mul")):
+        _check_forward(c, name, True, op, pre=True)
+    again = [_check_forward(c, "silu", True, "mul") for _ in range(2)]
+    assert torch.equal(again[0][:c["P"]], again[1][:c["P"]])
+
+
+@pytest.mark.parametrize("counts,H,N", [([3000], 64, 72), ([1500, 0, 30], 136, 64), ([900, 1100], 72, 520), ([70, 2500, 1, 0], 128, 128)])
+def test_gradients_with_long_segments_and_few_tiles(counts, H, N):
+    """The rows are cut into parts; experts without rows, or with fewer rows than parts, among them."""
+    _check_backward(_case(counts, H, N, seed=N, slack=5), "silu", "mul")
+    _check_backward(_case(counts, N, H * 8, seed=N, slack=5), "gelu", "add")
 
 
 def test_many_experts():
