@@ -23,6 +23,8 @@
 // are not stored; in the dweight mode, where the rows are contracted, the operands are read through tensor maps that end
 // with the segment (one pair per expert, made on the device from the offsets), so that the rest of the last box is zero
 // whatever the neighbouring rows hold.
+#include <atomic>
+
 #include "ep_tensor.cuh"
 
 namespace ep {
@@ -693,27 +695,25 @@ int check_matmul(const ep_matmul_t *m)
     return EP_OK;
 }
 
-int sm_count(int *n)
-{
-    int dev = 0;
-    EP_CUDA_TRY(cudaGetDevice(&dev));
-    EP_CUDA_TRY(cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev));
-    return EP_OK;
-}
-
 template <int MODE, int CG, bool SPLIT>
 int launch_product(ProductArgs a, const CUtensorMap &map_a, const ColumnMaps &map_b, int64_t max_tiles, cudaStream_t stream)
 {
-    int sms = 0;
-    const int rc = sm_count(&sms);
-    if (rc != EP_OK) return rc;
+    static std::atomic<int> sm_counts[64] = {};                              // per device; set once the shared memory limit is raised
+    int dev = 0;
+    EP_CUDA_TRY(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= 64) return EP_ERR_INVALID_ARG;
+    int sms = sm_counts[dev].load();
+    if (sms == 0) {
+        EP_CUDA_TRY(cudaFuncSetAttribute(product_kernel<MODE, CG, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit - 1024));
+        EP_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+        sm_counts[dev].store(sms);
+    }
     const int stage = kBytesA + (a.columns / CG < 32 ? 32 : a.columns / CG) * kTileK * 2;
     const int tables = (SPLIT ? kExchangeBytes : kStageBytes) + 2 * (a.E + 1) * 4;
     a.stages = (kSmemLimit - 2048 - tables) / stage;                         // 2048: alignment of the ring, static words
     if (a.stages > kMaxStages) a.stages = kMaxStages;
     int smem = 1024 + a.stages * stage + tables;
     if (smem < 120 * 1024) smem = 120 * 1024;                                // one CTA per SM: it holds all of the tensor memory
-    EP_CUDA_TRY(cudaFuncSetAttribute(product_kernel<MODE, CG, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
     const int sharing = SPLIT ? a.split : CG;
     int64_t groups = sms / sharing;
     if (max_tiles < groups || SPLIT) groups = max_tiles;                     // a shared tile has a cluster of its own
