@@ -275,10 +275,10 @@ product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, c
         gave_up_ = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 2) tmem_alloc<CG>(smem_addr(&tmem_slot), 2 * kAccColumns);
-
-    pdl_trigger();
     pdl_wait();                                                              // nothing is read or written before this
+    // Tensor memory is taken after the kernels before are done and before the next one may come: a CTA that held it while it
+    // waited, beside one that needs some, could wait for good.
+    if (warp == 2) tmem_alloc<CG>(smem_addr(&tmem_slot), 2 * kAccColumns);
     // the segments' bounds and, where tiles follow the segments, the experts' first tiles
     for (int e = threadIdx.x; e <= a.E; e += kThreads) bound[e] = segment_bound(__ldg(a.offsets + e), a.rows);
     if (threadIdx.x == 0 && blockIdx.x == 0 && a.status && __ldg(a.offsets + a.E) > a.rows) atomicOr(a.status, EP_STATUS_CAPACITY);
@@ -310,6 +310,7 @@ product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, c
     if (CG == 2 || SPLIT) cluster_sync();
     __syncthreads();
     tmem_fence_after();
+    pdl_trigger();
     const uint32_t tmem = tmem_slot;
     const int sharing = CG * split;
     Walk<MODE, CG, SPLIT> walk(a, first_tile, bound, blockIdx.x / sharing, gridDim.x / sharing, part);   // one per role

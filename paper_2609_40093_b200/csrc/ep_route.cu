@@ -320,7 +320,7 @@ route_kernel(const RouteArgs a)
     const bool all = kBal || a.bias || (soft && !a.renormalize);              // are scores needed beyond the picked ones?
     int tokens = 0;
     bool bad = false, bad_index = false;
-    for (int t = blockIdx.x * kWarps + warp; t < a.T; t += gridDim.x * kWarps) {
+    for (unsigned t = blockIdx.x * kWarps + warp; t < (unsigned)a.T; t += gridDim.x * kWarps) {   // T < 2^31: no wrap
         const T *row = static_cast<const T *>(a.logits) + (size_t)t * a.E;
         float l[NV];
         load_row<NV>(row, a.E, lane, a.vec, l);
@@ -508,14 +508,14 @@ route_grad_kernel(const RouteGradArgs a)
     constexpr bool kAhead = NV <= 8;
     float l_next[kAhead ? NV : 1], dw_next = 0.f;
     int id_next = -1;
-    const auto fetch = [&](int t, float (&l)[kAhead ? NV : 1], int &id, float &dw) {
+    const auto fetch = [&](unsigned t, float (&l)[kAhead ? NV : 1], int &id, float &dw) {
         if (kAhead) load_row<NV>(static_cast<const T *>(a.logits) + (size_t)t * a.E, a.E, lane, a.vec, reinterpret_cast<float (&)[NV]>(l));
         id = lane < a.K ? __ldg(a.topk_idx + (size_t)t * a.K + lane) : -1;
         dw = lane < a.K && a.d_weights ? __ldg(a.d_weights + (size_t)t * a.K + lane) : 0.f;
     };
-    const int first = blockIdx.x * kWarps + warp, stride = gridDim.x * kWarps;
-    if (first < a.T) fetch(first, l_next, id_next, dw_next);
-    for (int t = first; t < a.T; t += stride) {
+    const unsigned first = blockIdx.x * kWarps + warp, stride = gridDim.x * kWarps, T_ = a.T;
+    if (first < T_) fetch(first, l_next, id_next, dw_next);
+    for (unsigned t = first; t < T_; t += stride) {
         const T *row = static_cast<const T *>(a.logits) + (size_t)t * a.E;
         T *out = static_cast<T *>(a.dlogits) + (size_t)t * a.E;
         float l[NV];
@@ -527,7 +527,7 @@ route_grad_kernel(const RouteGradArgs a)
         }
         int id = id_next >= 0 && id_next < a.E ? id_next : -1;
         const float dw = id >= 0 ? a.scale * dw_next : 0.f;
-        if (t + stride < a.T) fetch(t + stride, l_next, id_next, dw_next);
+        if (t + stride < T_) fetch(t + stride, l_next, id_next, dw_next);
         clean_row<NV>(l);
         float top = l[0];
 #pragma unroll

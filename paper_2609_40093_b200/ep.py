@@ -175,9 +175,15 @@ def _at(t, shape, dtype, name):
     return t.data_ptr()
 
 
-def _stream_of(t):
-    """The current stream of the tensor's device, as an address."""
-    return torch._C._cuda_getCurrentRawStream(t.get_device())
+def _stream_of(first, *others):
+    """The current stream, as an address, of the CUDA device on which all these tensors (or None) have to be."""
+    dev = first.get_device()
+    if dev < 0:
+        raise ValueError("the EP library needs CUDA tensors")
+    for t in others:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"the EP library needs its tensors on one CUDA device, got {first.device} and {t.device}")
+    return torch._C._cuda_getCurrentRawStream(dev)
 
 
 def _check(rc: int, where: str):
@@ -509,6 +515,9 @@ class Routing:
     loss: torch.Tensor = None            # [1] fp32
     workspace: torch.Tensor = None
 
+    def _loss_tensors(self):
+        return self.expert_counts, self.tokens, self.mean_probs, self.loss
+
     def _balance(self, E):
         """A pointer to ep_balance_t, or None."""
         if self.expert_counts is None:
@@ -545,7 +554,8 @@ def ep_route(logits: torch.Tensor, router: Router, bias: torch.Tensor = None, ou
     _check(lib().ep_route(st, _at(logits, (T, E), logits.dtype, "logits"), _at(bias, (E,), torch.float32, "bias"),
                           _at(out.topk_idx, (T, K), torch.int32, "topk_idx"), _at(out.topk_weights, (T, K), torch.float32, "topk_weights"),
                           out._balance(E), _at(out.status, (1,), torch.int32, "status"), None if ws is None else _ptr(ws),
-                          0 if ws is None else ws.numel(), _stream_of(logits)), "ep_route")
+                          0 if ws is None else ws.numel(),
+                          _stream_of(logits, bias, out.topk_idx, out.topk_weights, out.status, ws, *out._loss_tensors())), "ep_route")
     return out
 
 
@@ -559,7 +569,8 @@ def ep_balance_loss(logits: torch.Tensor, router: Router, topk_idx: torch.Tensor
         raise ValueError("ep_balance_loss needs a Routing allocated with balance=True")
     _check(lib().ep_balance_loss(st, _at(logits, (T, E), logits.dtype, "logits"), _at(topk_idx, (T, K), torch.int32, "topk_idx"),
                                  out._balance(E), _at(out.status, (1,), torch.int32, "status"), _ptr(out.workspace),
-                                 out.workspace.numel(), _stream_of(logits)), "ep_balance_loss")
+                                 out.workspace.numel(), _stream_of(logits, topk_idx, out.status, out.workspace, *out._loss_tensors())),
+           "ep_balance_loss")
     return out
 
 
@@ -576,7 +587,9 @@ def ep_route_backward(logits: torch.Tensor, router: Router, routing: Routing, d_
     _check(lib().ep_route_backward(st, _at(logits, (T, E), logits.dtype, "logits"), _at(routing.topk_idx, (T, K), torch.int32, "topk_idx"),
                                    _at(d_weights, (T, K), torch.float32, "d_weights"),
                                    None if d_loss is None else routing._balance(E), _at(d_loss, (1,), torch.float32, "d_loss"),
-                                   _at(dlogits, (T, E), logits.dtype, "dlogits"), _stream_of(logits)), "ep_route_backward")
+                                   _at(dlogits, (T, E), logits.dtype, "dlogits"),
+                                   _stream_of(logits, routing.topk_idx, d_weights, d_loss, dlogits, routing.expert_counts, routing.tokens)),
+           "ep_route_backward")
     return dlogits
 
 
@@ -597,7 +610,7 @@ def ep_expert_matmul(x, expert_offsets, weight, bias=None, activation=ACT_NONE, 
     _check(lib().ep_expert_matmul(ctypes.byref(m), _at(x, (P, H), bf, "x"), _at(expert_offsets, (E + 1,), torch.int32, "expert_offsets"),
                                   _at(weight, (E, N, H), bf, "weight"), _at(bias, (E, N), bf, "bias"), _at(operand, (P, N), bf, "operand"),
                                   _at(y, (P, N), bf, "y"), _at(pre, (P, N), bf, "pre"), _at(status, (1,), torch.int32, "status"),
-                                  _stream_of(x)), "ep_expert_matmul")
+                                  _stream_of(x, expert_offsets, weight, bias, operand, y, pre, status)), "ep_expert_matmul")
     return y
 
 
@@ -640,8 +653,9 @@ def ep_expert_matmul_backward(dy, x, expert_offsets, weight, pre=None, activatio
         _at(expert_offsets, (E + 1,), torch.int32, "expert_offsets"), _at(weight, (E, N, H), bf, "weight"), _at(pre, (P, N), bf, "pre"),
         _at(operand, (P, N), bf, "operand"), _at(grads.dx, (P, H), bf, "dx"), _at(grads.dweight, (E, N, H), bf, "dweight"),
         _at(grads.dbias, (E, N), torch.float32, "dbias"), _at(grads.doperand, (P, N), bf, "doperand"),
-        _at(status, (1,), torch.int32, "status"), _ptr(grads.workspace), grads.workspace.numel(), _stream_of(dy)),
-        "ep_expert_matmul_backward")
+        _at(status, (1,), torch.int32, "status"), _ptr(grads.workspace), grads.workspace.numel(),
+        _stream_of(dy, x, expert_offsets, weight, pre, operand, grads.dx, grads.dweight, grads.dbias, grads.doperand, status,
+                   grads.workspace)), "ep_expert_matmul_backward")
     return grads
 
 

@@ -111,3 +111,26 @@ def test_binding_refuses_types_shapes_and_strides():
         ep.ep_expert_matmul(torch.zeros(6, 32, dtype=bf)[:, ::2], off, w)
     with pytest.raises(ValueError, match="dy"):
         ep.ep_expert_matmul_backward(torch.zeros(6, 16, dtype=bf), x, off, w, grads=ep.alloc_expert_grads(6, 16, 8, 2, device="cpu"))
+
+
+def test_binding_refuses_host_tensors():
+    """An address of host memory would fault on the GPU: every tensor has to be on the first one's CUDA device."""
+    with pytest.raises(ValueError, match="CUDA"):
+        ep.ep_route(torch.zeros(4, 8), ep.Router(8, 2), out=ep.alloc_routing(4, 8, 2, device="cpu"))
+    bf = torch.bfloat16
+    x, off, w = torch.zeros(6, 16, dtype=bf), torch.zeros(3, dtype=torch.int32), torch.zeros(2, 8, 16, dtype=bf)
+    with pytest.raises(ValueError, match="CUDA"):
+        ep.ep_expert_matmul(x, off, w)
+    with pytest.raises(ValueError, match="CUDA"):
+        ep.ep_expert_matmul_backward(torch.zeros(6, 8, dtype=bf), x, off, w, grads=ep.alloc_expert_grads(6, 16, 8, 2, device="cpu"))
+
+
+@pytest.mark.gpu
+def test_binding_refuses_a_mix_of_devices():
+    with pytest.raises(ValueError, match="one CUDA device"):
+        ep.ep_route(torch.zeros(4, 8, device="cuda"), ep.Router(8, 2), out=ep.alloc_routing(4, 8, 2, device="cpu"))
+    with pytest.raises(ValueError, match="one CUDA device"):
+        ep.ep_route(torch.zeros(4, 8, device="cuda"), ep.Router(8, 2), bias=torch.zeros(8))
+    bf = torch.bfloat16
+    with pytest.raises(ValueError, match="one CUDA device"):
+        ep.ep_expert_matmul(torch.zeros(6, 16, dtype=bf, device="cuda"), torch.zeros(3, dtype=torch.int32), torch.zeros(2, 8, 16, dtype=bf, device="cuda"))
