@@ -163,27 +163,32 @@ def _stream():
 
 
 def _at(t, shape, dtype, name):
-    """Address of a contiguous tensor of this shape and type; None stays None."""
+    """Address of a contiguous tensor of this shape (None: any) and type; None stays None."""
     if t is None:
         return None
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.shape != shape:
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
     if not t.is_contiguous():
         raise ValueError(f"{name}: the EP library needs contiguous tensors")
     return t.data_ptr()
 
 
+def _on_device(device, *tensors):
+    """Every tensor (or None) has to be on this CUDA device."""
+    if device < 0:
+        raise ValueError("the EP library needs CUDA tensors")
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"the EP library needs its tensors on one CUDA device, got cuda:{device} and {t.device}")
+
+
 def _stream_of(first, *others):
     """The current stream, as an address, of the CUDA device on which all these tensors (or None) have to be."""
-    dev = first.get_device()
-    if dev < 0:
-        raise ValueError("the EP library needs CUDA tensors")
-    for t in others:
-        if t is not None and t.get_device() != dev:
-            raise ValueError(f"the EP library needs its tensors on one CUDA device, got {first.device} and {t.device}")
-    return torch._C._cuda_getCurrentRawStream(dev)
+    device = first.get_device()
+    _on_device(device, *others)
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
 def _check(rc: int, where: str):
@@ -515,15 +520,30 @@ class Routing:
     loss: torch.Tensor = None            # [1] fp32
     workspace: torch.Tensor = None
 
-    def _loss_tensors(self):
-        return self.expert_counts, self.tokens, self.mean_probs, self.loss
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        object.__setattr__(self, "_checked", None)
 
-    def _balance(self, E):
-        """A pointer to ep_balance_t, or None."""
-        if self.expert_counts is None:
-            return None
-        return ctypes.byref(_Balance(_at(self.expert_counts, (E,), torch.int32, "expert_counts"), _at(self.tokens, (1,), torch.int32, "tokens"),
-                                     _at(self.mean_probs, (E,), torch.float32, "mean_probs"), _at(self.loss, (1,), torch.float32, "loss")))
+    def _args(self, T, E, K, device):
+        """(topk_idx, topk_weights, a pointer to ep_balance_t or None, status, workspace, its bytes) as the library takes them.
+        Types, shapes and devices are checked when a tensor is new or its memory has moved."""
+        tensors = (self.topk_idx, self.topk_weights, self.status, self.expert_counts, self.tokens, self.mean_probs, self.loss, self.workspace)
+        key = (T, E, K, device, *[None if t is None else t.data_ptr() for t in tensors])
+        known = self._checked
+        if known is not None and known[0] == key:
+            return known[1]
+        idx, w, status = (_at(self.topk_idx, (T, K), torch.int32, "topk_idx"), _at(self.topk_weights, (T, K), torch.float32, "topk_weights"),
+                          _at(self.status, (1,), torch.int32, "status"))
+        balance = None
+        if self.expert_counts is not None:
+            balance = ctypes.pointer(_Balance(
+                _at(self.expert_counts, (E,), torch.int32, "expert_counts"), _at(self.tokens, (1,), torch.int32, "tokens"),
+                _at(self.mean_probs, (E,), torch.float32, "mean_probs"), _at(self.loss, (1,), torch.float32, "loss")))
+        ws, nbytes = (None, 0) if self.workspace is None else (_ptr(self.workspace), self.workspace.numel() * self.workspace.element_size())
+        _on_device(device, *tensors)
+        args = (idx, w, balance, status, ws, nbytes)
+        object.__setattr__(self, "_checked", (key, args))
+        return args
 
 
 def ep_route_workspace_bytes(T, K, E) -> int:
@@ -550,12 +570,9 @@ def ep_route(logits: torch.Tensor, router: Router, bias: torch.Tensor = None, ou
     E, K = router.num_experts, router.top_k
     if out is None:
         out = alloc_routing(T, E, K, balance=router.balance_coef != 0.0, device=logits.device)
-    ws = out.workspace
-    _check(lib().ep_route(st, _at(logits, (T, E), logits.dtype, "logits"), _at(bias, (E,), torch.float32, "bias"),
-                          _at(out.topk_idx, (T, K), torch.int32, "topk_idx"), _at(out.topk_weights, (T, K), torch.float32, "topk_weights"),
-                          out._balance(E), _at(out.status, (1,), torch.int32, "status"), None if ws is None else _ptr(ws),
-                          0 if ws is None else ws.numel(),
-                          _stream_of(logits, bias, out.topk_idx, out.topk_weights, out.status, ws, *out._loss_tensors())), "ep_route")
+    x, b = _at(logits, None, logits.dtype, "logits"), _at(bias, (E,), torch.float32, "bias")
+    idx, w, balance, status, ws, nbytes = out._args(T, E, K, logits.get_device())
+    _check(lib().ep_route(st, x, b, idx, w, balance, status, ws, nbytes, _stream_of(logits, bias)), "ep_route")
     return out
 
 
@@ -567,10 +584,9 @@ def ep_balance_loss(logits: torch.Tensor, router: Router, topk_idx: torch.Tensor
         out = alloc_routing(T, E, K, balance=True, topk_idx=topk_idx, device=logits.device)
     if out.expert_counts is None:
         raise ValueError("ep_balance_loss needs a Routing allocated with balance=True")
-    _check(lib().ep_balance_loss(st, _at(logits, (T, E), logits.dtype, "logits"), _at(topk_idx, (T, K), torch.int32, "topk_idx"),
-                                 out._balance(E), _at(out.status, (1,), torch.int32, "status"), _ptr(out.workspace),
-                                 out.workspace.numel(), _stream_of(logits, topk_idx, out.status, out.workspace, *out._loss_tensors())),
-           "ep_balance_loss")
+    x, idx = _at(logits, None, logits.dtype, "logits"), _at(topk_idx, (T, K), torch.int32, "topk_idx")
+    _, _, balance, status, ws, nbytes = out._args(T, E, K, logits.get_device())
+    _check(lib().ep_balance_loss(st, x, idx, balance, status, ws, nbytes, _stream_of(logits, topk_idx)), "ep_balance_loss")
     return out
 
 
@@ -584,12 +600,11 @@ def ep_route_backward(logits: torch.Tensor, router: Router, routing: Routing, d_
         dlogits = torch.empty_like(logits)
     if d_loss is not None and routing.expert_counts is None:
         raise ValueError("the gradient of the balance loss needs the Routing that holds its counts")
-    _check(lib().ep_route_backward(st, _at(logits, (T, E), logits.dtype, "logits"), _at(routing.topk_idx, (T, K), torch.int32, "topk_idx"),
-                                   _at(d_weights, (T, K), torch.float32, "d_weights"),
-                                   None if d_loss is None else routing._balance(E), _at(d_loss, (1,), torch.float32, "d_loss"),
-                                   _at(dlogits, (T, E), logits.dtype, "dlogits"),
-                                   _stream_of(logits, routing.topk_idx, d_weights, d_loss, dlogits, routing.expert_counts, routing.tokens)),
-           "ep_route_backward")
+    x, dw = _at(logits, None, logits.dtype, "logits"), _at(d_weights, (T, K), torch.float32, "d_weights")
+    dl, out = _at(d_loss, (1,), torch.float32, "d_loss"), _at(dlogits, (T, E), logits.dtype, "dlogits")
+    idx, _, balance, _, _, _ = routing._args(T, E, K, logits.get_device())
+    _check(lib().ep_route_backward(st, x, idx, dw, None if d_loss is None else balance, dl, out,
+                                   _stream_of(logits, d_weights, d_loss, dlogits)), "ep_route_backward")
     return dlogits
 
 

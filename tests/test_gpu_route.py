@@ -308,3 +308,22 @@ def test_a_large_table_agrees_with_its_parts():
     assert torch.equal(whole.expert_counts, sum(p.expert_counts for p in parts)) and int(whole.expert_counts.sum()) == T * K
     mean = sum(p.mean_probs.double() for p in parts) / 4
     assert ((whole.mean_probs.double() - mean).abs() <= WEIGHT * mean).all()
+
+
+def test_tensors_of_a_routing_may_be_exchanged_between_calls():
+    """What a Routing remembers of its tensors is forgotten when one is replaced or moves."""
+    T, E, K = 40, 16, 2
+    router, logits = ep.Router(E, K, balance_coef=0.1), _logits(40, 16, torch.float32, 3).cuda()
+    out = ep.ep_route(logits, router)
+    idx = out.topk_idx.clone()
+    fresh = torch.full_like(idx, -7)
+    out.topk_idx = fresh
+    ep.ep_route(logits, router, out=out)
+    assert torch.equal(fresh, idx)
+    out.topk_idx = torch.zeros(T, K, dtype=torch.int64, device="cuda")
+    with pytest.raises(TypeError, match="topk_idx"):
+        ep.ep_route(logits, router, out=out)
+    out.topk_idx = fresh
+    out.mean_probs.resize_(4 * E)                               # other memory behind the same tensor, of another shape
+    with pytest.raises(ValueError, match="mean_probs"):
+        ep.ep_route(logits, router, out=out)
