@@ -72,7 +72,7 @@ struct Tile {
     int e, m0;
     int c0, cols;                         // first column (row p, or out feature) and how many are real
     int n;                                // columns of the product: cols rounded up to what the tensor cores take
-    int k0, nk;                           // first contracted index and stages
+    int k0, nk, all;                      // first contracted index, stages, and stages of all CTAs that share the tile (0: no rows)
 };
 
 __device__ __forceinline__ int segment_bound(int32_t v, long long rows)
@@ -160,6 +160,7 @@ struct Walk {
             t.nk = (a.K + kTileK - 1) / kTileK;
         }
         t.n = max(kStep, (t.cols + kStep - 1) / kStep * kStep);
+        t.all = t.nk;
         if (SPLIT) {                                     // this CTA's part of the contracted axis (may be empty)
             const int from = t.nk * part / a.split, to = t.nk * (part + 1) / a.split;
             t.k0 += from * kTileK;
@@ -191,8 +192,8 @@ struct Ring {
 // ---- epilogues ---------------------------------------------------------------------------------------------------
 
 // A warp's 32 lanes x 32 columns of accumulators pass through shared memory, so that afterwards a lane holds 8 neighbouring
-// features of a column and reads and writes global memory 16 bytes at a time: the forward mode 16 columns of fp32 at a time,
-// the others, which do no more arithmetic, all 32 columns as rounded pairs. The pairs matter where the contracted axis is
+// features of a column and reads and writes global memory 16 bytes at a time: the forward mode with an operand or `pre` 16 columns
+// of fp32 at a time, the others, whose arithmetic is done before, all 32 columns as rounded pairs. The pairs matter where the contracted axis is
 // short and a tile's epilogue takes as long as its products: shared memory feeds both, and with fp32 words the dweight mode
 // took 220 us at 128 experts of 1024 x 2048 and 32768 rows, with pairs 195. (Stored straight from the accumulators' order,
 // 2 bytes a lane, a column took ten instructions.) Rows are 36 words apart: 16-byte reads of eight lanes fall on all banks.
@@ -223,6 +224,14 @@ __device__ __forceinline__ void finish8(const ProductArgs &a, float (&z)[8], con
 }
 
 // ---- the kernel --------------------------------------------------------------------------------------------------
+
+// 32 accumulators of one feature: bias and activation, in place.
+template <int ACT>
+__device__ __forceinline__ void act_all(uint32_t (&v)[32], float bias)
+{
+#pragma unroll
+    for (int c = 0; c < 32; ++c) v[c] = __float_as_uint(act_value(ACT, __uint_as_float(v[c]) + bias));
+}
 
 // 8 features of a row: the mode's arithmetic and the store. operand: as loaded, if there is one.
 template <int MODE>
@@ -274,6 +283,10 @@ product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, c
         if (SPLIT) bar_init(smem_addr(&ex_full_), split * kEpilogueWarps);
         gave_up_ = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (threadIdx.x < 5) {                                                   // the maps are arguments: theirs may be fetched already
+        const CUtensorMap *map = threadIdx.x == 0 ? &map_a : &map_b.box[threadIdx.x - 1];
+        if (MODE != kDweight) asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
     }
     pdl_wait();                                                              // nothing is read or written before this
     // Tensor memory is taken after the kernels before are done and before the next one may come: a CTA that held it while it
@@ -400,7 +413,7 @@ product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, c
         const int q = warp & 3, first = (warp - 4) / 4 * 32, thread = threadIdx.x - 128;
         float *mine = reinterpret_cast<float *>(tables);
         const size_t ld = a.M;
-        bool ok = walk.next(t);                                              // the grid has a cluster per tile: there is no second one
+        bool ok = walk.next(t) && t.all > 0;                                 // the grid has a cluster per tile: there is no second one
         if (ok && t.nk) {
             ok = bar_wait(smem_addr(&acc_full_[0]), 0, gave_up);
             tmem_fence_after();
@@ -444,10 +457,12 @@ product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, c
         const int q = warp & 3, first = (warp - 4) / 4 * 32;                 // a warp reaches the lanes 32 (warp mod 4) .. + 31
         constexpr int kStep = kEpilogueWarps / 4 * 32;
         uint32_t *stage = reinterpret_cast<uint32_t *>(tables) + (warp - 4) * kStageWords;
-        const int my_col = (lane >> 2) * (MODE == kForward ? 1 : 2), my_seg = (lane & 3) * 8;
+        const bool words = MODE == kForward && (a.operand || a.pre);         // fp32 through the buffer, or rounded pairs of columns
+        const int my_col = (lane >> 2) * (words ? 1 : 2), my_seg = (lane & 3) * 8;
         const size_t ld = a.M;
         int used = 0;
         while (walk.next(t)) {
+            if (t.nk == 0) continue;
             const int feature = t.m0 + rank * kTileM + q * 32 + my_seg;
             const bool live = feature < a.M;                                 // M is a multiple of 8
             const int acc = used & 1;
@@ -455,18 +470,19 @@ product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, c
             const size_t corner = ((MODE == kDweight ? (size_t)t.e * a.N + t.c0 : (size_t)t.c0) + my_col) * ld + feature;
             const int cols = live ? t.cols - my_col : 0;                     // column c + my_col of the tile is real iff c < cols
             uint4 r[4];                                                      // the operand of the lane's four columns of a block
-            float bias[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            if (MODE == kForward) {
+            float bias[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, lane_bias = 0.f;
+            if (MODE == kForward && !words) {                                // the lane's own feature
+                const int mine = t.m0 + rank * kTileM + q * 32 + lane;
+                if (a.bias && mine < a.M) lane_bias = __uint_as_float((uint32_t)__ldg(a.bias + (size_t)t.e * a.M + mine) << 16);
+            } else if (MODE == kForward) {
                 if (a.bias && live) unpack8(__ldg(reinterpret_cast<const uint4 *>(a.bias + (size_t)t.e * a.M + feature)), bias);
                 if (a.operand)                                               // under the products
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         if (first + 8 * i < cols) r[i] = *reinterpret_cast<const uint4 *>(a.operand + corner + (first + 8 * i) * ld);
             }
-            if (t.nk) {
-                if (!bar_wait(smem_addr(&acc_full_[acc]), (used >> 1) & 1, gave_up)) break;
-                tmem_fence_after();
-            }
+            if (!bar_wait(smem_addr(&acc_full_[acc]), (used >> 1) & 1, gave_up)) break;
+            tmem_fence_after();
             const auto release = [&] {                                       // this warp has read its last column of the accumulator
                 tmem_fence_before();
                 __syncwarp();
@@ -474,14 +490,9 @@ product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, c
             };
             for (int c0 = first; c0 < t.cols; c0 += kStep) {
                 uint32_t v[32];
-                if (t.nk) {
-                    tmem_load32(from + c0, v);
-                    if (c0 + kStep >= t.cols) release();
-                } else {
-#pragma unroll
-                    for (int c = 0; c < 32; ++c) v[c] = 0u;
-                }
-                if (MODE == kForward) {
+                tmem_load32(from + c0, v);
+                if (c0 + kStep >= t.cols) release();
+                if (words) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         if (c0 + 16 * h >= t.cols) break;
@@ -509,7 +520,15 @@ product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, c
                         }
                     }
                 } else {
-                    // no arithmetic: a word carries two columns' results, rounded
+                    // nothing else to read: a word carries two columns' results, rounded
+                    if (MODE == kForward) {
+                        switch (a.activation) {
+                        case EP_ACT_RELU: act_all<EP_ACT_RELU>(v, lane_bias); break;
+                        case EP_ACT_SILU: act_all<EP_ACT_SILU>(v, lane_bias); break;
+                        case EP_ACT_GELU: act_all<EP_ACT_GELU>(v, lane_bias); break;
+                        default: act_all<EP_ACT_NONE>(v, lane_bias); break;
+                        }
+                    }
                     __syncwarp();
 #pragma unroll
                     for (int c = 0; c < 16; ++c)
@@ -532,8 +551,8 @@ product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, c
                     }
                 }
             }
-            if (t.nk && first >= t.cols) release();
-            used += t.nk > 0;
+            if (first >= t.cols) release();
+            ++used;
         }
     }
     __syncwarp();
@@ -545,22 +564,31 @@ product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, c
     if (threadIdx.x == 0 && gave_up_ && a.status) atomicOr(a.status, EP_STATUS_TIMEOUT);
 }
 
-// One pair of tensor maps per expert that end with its segment: {x, dz} of rows [0, bound[e+1]).
-__global__ void __launch_bounds__(32)
+// One pair of tensor maps per expert that end with its segment: {x, dz} of rows [0, bound[e+1]). An expert without rows gets its
+// zeros here, from all blocks (e, *): the gradients of 240 experts of 5888 x 144, most of them without rows, take 161 us so, 211
+// with one block per expert.
+__global__ void __launch_bounds__(256)
 segment_maps_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_dz, const int32_t *offsets,
-                    long long rows, CUtensorMap *out)
+                    long long rows, CUtensorMap *out, uint4 *dweight, long long vecs)
 {
     __shared__ alignas(128) uint32_t work[2][32];
-    const int e = blockIdx.x, lane = threadIdx.x;
+    const int e = blockIdx.x, lane = threadIdx.x & 31;
     pdl_trigger();
     pdl_wait();
+    const int begin = segment_bound(__ldg(offsets + e), rows), end = segment_bound(__ldg(offsets + e + 1), rows);
+    if (end <= begin) {
+        uint4 *dst = dweight + (size_t)e * vecs;
+        for (long long v = (long long)blockIdx.y * 256 + threadIdx.x; v < vecs; v += (long long)gridDim.y * 256)
+            st_stream(dst + v, make_uint4(0u, 0u, 0u, 0u));
+    }
+    if (blockIdx.y || threadIdx.x >= 32) return;
     work[0][lane] = reinterpret_cast<const uint32_t *>(&map_x)[lane];
     work[1][lane] = reinterpret_cast<const uint32_t *>(&map_dz)[lane];
-    const uint32_t end = max(1, segment_bound(__ldg(offsets + e + 1), rows));
     __syncwarp();
     for (int i = 0; i < 2; ++i) {
         const uint32_t s = smem_addr(work[i]);
-        if (lane == 0) asm volatile("tensormap.replace.tile.global_dim.shared::cta.b1024.b32 [%0], 1, %1;" ::"r"(s), "r"(end) : "memory");
+        if (lane == 0)
+            asm volatile("tensormap.replace.tile.global_dim.shared::cta.b1024.b32 [%0], 1, %1;" ::"r"(s), "r"(max(1, end)) : "memory");
         __syncwarp();
         asm volatile("tensormap.cp_fenceproxy.global.shared::cta.tensormap::generic.release.gpu.sync.aligned [%0], [%1], 128;" ::"l"(
                          out + 2 * (size_t)e + i),
@@ -657,29 +685,35 @@ slope_kernel(const SlopeArgs a)
     }
 }
 
-// dbias[e][n] = sum of the expert's pieces: eight warps take a run of pieces each, then the eight sums, both in order.
+// dbias[e][n] = sum of the expert's pieces, a thread per column; with many pieces per expert eight threads per column take a run of
+// them each, and the eight sums are added in order (SPLIT), in blocks of 32 columns instead of 256: 128 experts of 1024 columns and
+// eight pieces each, unevenly, 437 us for all gradients with eight, 446 with one; 240 experts of 5888 columns and hardly a row, the
+// other way round, 229 and 212.
+template <int SPLIT>
 __global__ void __launch_bounds__(256)
 bias_grad_kernel(const float *__restrict__ partial, const int32_t *__restrict__ offsets, long long rows, int N, int chunk, float *dbias)
 {
-    __shared__ float part[8][32];
+    constexpr int kColumns = 256 / SPLIT;
+    __shared__ float part[SPLIT][kColumns];
     pdl_trigger();
     pdl_wait();
-    const int e = blockIdx.y, lane = threadIdx.x & 31, w = threadIdx.x >> 5, n = blockIdx.x * 32 + lane;
+    const int e = blockIdx.y, col = threadIdx.x % kColumns, w = threadIdx.x / kColumns, n = blockIdx.x * kColumns + col;
     const int begin = segment_bound(__ldg(offsets + e), rows), end = segment_bound(__ldg(offsets + e + 1), rows);
     float s = 0.f;
     if (begin < end && n < N) {
-        const int c0 = begin / chunk, count = (end - 1) / chunk - c0 + 1, per = (count + 7) / 8;
+        const int c0 = begin / chunk, count = (end - 1) / chunk - c0 + 1, per = (count + SPLIT - 1) / SPLIT;
         const int from = c0 + min(count, w * per), to = c0 + min(count, w * per + per);
 #pragma unroll 8
         for (int c = from; c < to; ++c) s += __ldg(partial + (size_t)(c + e) * N + n);
     }
-    part[w][lane] = s;
-    __syncthreads();
-    if (w == 0 && n < N) {
+    if (SPLIT > 1) {
+        part[w][col] = s;
+        __syncthreads();
+        if (w) return;
 #pragma unroll
-        for (int i = 1; i < 8; ++i) s += part[i][lane];
-        dbias[(size_t)e * N + n] = s;
+        for (int i = 1; i < SPLIT; ++i) s += part[i][col];
     }
+    if (n < N) dbias[(size_t)e * N + n] = s;
 }
 
 // ---- host side ---------------------------------------------------------------------------------------------------
@@ -918,8 +952,10 @@ extern "C" int ep_expert_matmul_backward(const ep_matmul_t *m, const void *dy, c
         EP_CUDA_TRY(launch_pdl(kernel, grid, dim3(kSlopeWarps * 32), 0, stream, s));
         EP_LAUNCH_CHECK(1);
         if (dbias) {
-            EP_CUDA_TRY(launch_pdl(bias_grad_kernel, dim3((unsigned)((N + 31) / 32), (unsigned)E), dim3(256), 0, stream, partial,
-                                   expert_offsets, (long long)m->rows, (int)N, s.chunk, dbias));
+            const bool many = chunks > (int64_t)E;
+            EP_CUDA_TRY(launch_pdl(many ? bias_grad_kernel<8> : bias_grad_kernel<1>,
+                                   dim3((unsigned)((N + (many ? 31 : 255)) / (many ? 32 : 256)), (unsigned)E), dim3(256), 0, stream,
+                                   partial, expert_offsets, (long long)m->rows, (int)N, s.chunk, dbias));
             EP_LAUNCH_CHECK(1);
         }
     }
@@ -947,8 +983,9 @@ extern "C" int ep_expert_matmul_backward(const ep_matmul_t *m, const void *dy, c
         rc = make_map(encode, &map_a, x, H, m->rows, 1, kTileK);
         if (rc == EP_OK) rc = make_map(encode, &map_b.box[0], dz, N, m->rows, 1, kTileK);
         if (rc != EP_OK) return rc;
-        EP_CUDA_TRY(launch_pdl(segment_maps_kernel, dim3((unsigned)E), dim3(32), 0, stream, map_a, map_b.box[0], expert_offsets,
-                               (long long)m->rows, maps));
+        const unsigned share = E >= 592 ? 2 : (unsigned)(1184 / E);           // blocks per expert: eight per SM, were all without rows
+        EP_CUDA_TRY(launch_pdl(segment_maps_kernel, dim3((unsigned)E, share), dim3(256), 0, stream, map_a, map_b.box[0], expert_offsets,
+                               (long long)m->rows, maps, static_cast<uint4 *>(dweight), (long long)(N * H / 8)));
         EP_LAUNCH_CHECK(1);
         a.M = m->in_features, a.N = m->out_features, a.K = 0;
         a.out = static_cast<uint16_t *>(dweight);
