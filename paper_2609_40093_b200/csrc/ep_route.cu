@@ -286,6 +286,69 @@ __device__ __forceinline__ int pick(const float (&l)[NV], const float (&rough)[N
     return id;
 }
 
+// The end of a kernel with a balance loss: `sums` holds the warps' sums of probabilities, [warp][value of a lane][lane], `counts` the
+// CTA's picks and, at E, its tokens. All threads call it; `shared` (the start of the dynamic shared memory) is free.
+template <int NV, int kWarps>
+__device__ __forceinline__ void finish_balance(const RouteArgs &a, float *shared, const float *sums, int *counts)
+{
+    constexpr int kPadded = NV * 32;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    __shared__ bool last;
+    __syncthreads();
+    for (int i = threadIdx.x; i < kPadded; i += blockDim.x) {
+        const int e = expert_of<NV>(i >> 5, i & 31);
+        if (e < a.E) {
+            float v = 0.f;
+#pragma unroll 8
+            for (int w = 0; w < kWarps; ++w) v += sums[(size_t)w * kPadded + i];
+            const size_t at = (size_t)(blockIdx.x % kRows) * a.E + e;
+            if (v > 0.f) atomicAdd(a.sums + at, __float2ull_rn(ldexpf(v, a.shift)));
+            if (counts[e]) atomicAdd(a.sum_counts + at, counts[e]);
+        }
+    }
+    int32_t *total = a.sum_counts + (size_t)kRows * a.E;                  // tokens, CTAs
+    if (threadIdx.x == 0 && counts[a.E]) atomicAdd(total, counts[a.E]);
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) last = atomicAdd(total + 1, 1) == (int)gridDim.x - 1;
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    const int n = __ldcg(total);
+    const float unit = n ? ldexpf(1.f, -a.shift) / (float)n : 0.f;
+    float dot = 0.f;                                                      // sum of count * (mean probability)
+    int picks = 0;
+    for (int e = threadIdx.x; e < a.E; e += blockDim.x) {
+        unsigned long long p[kRows];
+        int k[kRows];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) p[r] = __ldcg(a.sums + (size_t)r * a.E + e), k[r] = __ldcg(a.sum_counts + (size_t)r * a.E + e);
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) a.sums[(size_t)r * a.E + e] = 0ull, a.sum_counts[(size_t)r * a.E + e] = 0;
+#pragma unroll
+        for (int r = 1; r < kRows; ++r) p[0] += p[r], k[0] += k[r];
+        const float mean = __ull2float_rn(p[0]) * unit;
+        a.mean_probs[e] = mean;
+        a.expert_counts[e] = k[0];
+        dot += (float)k[0] * mean;
+        picks += k[0];
+    }
+    dot = warp_sum(dot);
+    picks = __reduce_add_sync(kFullMask, picks);
+    __syncthreads();
+    if (lane == 0) shared[warp] = dot, counts[warp] = picks;
+    __syncthreads();
+    if (warp == 0) {
+        dot = warp_sum(lane < kWarps ? shared[lane] : 0.f);
+        picks = __reduce_add_sync(kFullMask, lane < kWarps ? counts[lane] : 0);
+        if (lane == 0) {
+            *a.loss = picks ? a.coef * (float)a.E / (float)picks * dot : 0.f;
+            *a.tokens = n;
+            total[0] = total[1] = 0;
+        }
+    }
+}
+
 // Warps per CTA. With a balance loss one CTA fills an SM as far as the registers allow.
 __host__ __device__ constexpr int route_warps(int nv, bool balance)
 {
@@ -335,7 +398,7 @@ route_kernel(const RouteArgs a)
             id = __ldg(a.topk_idx + (size_t)t * a.K + lane);
             if (id < -1 || id >= a.E) bad_index = true, id = -1;
         }
-        const bool counted = live && (MODE != kBalance || __any_sync(kFullMask, id >= 0));
+        bool counted = live && (MODE != kBalance || __any_sync(kFullMask, id >= 0));
 
         // ---- scores
         float s[NV], sum = 1.f;
@@ -348,26 +411,33 @@ route_kernel(const RouteArgs a)
                 for (int j = 0; j < NV; ++j) sum += s[j];
                 sum = warp_sum(sum);
             }
-            if (kBal && counted) {
-                const float inv = sum > 0.f ? __fdividef(1.f, sum) : 0.f;     // sigmoids of very negative logits can all be 0
+        }
+        float rough[MODE != kBalance ? NV : 1];                               // what orders the picks, where there is a bias
+        if (MODE != kBalance && a.bias && live) {
+            float(&v)[NV] = reinterpret_cast<float(&)[NV]>(rough);
+            load_row<NV>(a.bias, a.E, lane, a.vec_bias, v);                   // -inf past E
+            const float inv = soft ? __fdividef(1.f, sum) : 1.f;
+            float most = -INFINITY;
 #pragma unroll
-                for (int j = 0; j < NV; ++j) {
-                    if (kInRegisters) psum[j % (kInRegisters ? NV : 1)] += s[j] * inv;
-                    else mine[j * 32 + lane] += s[j] * inv;
-                }
-                ++tokens;
+            for (int j = 0; j < NV; ++j) v[j] = l[j] > -INFINITY ? s[j] * inv + v[j] : -INFINITY;
+            bad |= clean_row<NV>(v);
+#pragma unroll
+            for (int j = 0; j < NV; ++j) most = fmaxf(most, v[j]);
+            counted = __any_sync(kFullMask, most > -INFINITY);                // a bias of -inf masks too
+        }
+        if (kBal && counted) {
+            const float inv = sum > 0.f ? __fdividef(1.f, sum) : 0.f;         // sigmoids of very negative logits can all be 0
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                if (kInRegisters) psum[j % (kInRegisters ? NV : 1)] += s[j] * inv;
+                else mine[j * 32 + lane] += s[j] * inv;
             }
+            ++tokens;
         }
         if (MODE != kBalance) {
             float w = 0.f;                                                    // the pick's score
             if (live && a.bias) {
-                float rough[NV];
-                load_row<NV>(a.bias, a.E, lane, a.vec_bias, rough);           // -inf past E
-                const float inv = soft ? __fdividef(1.f, sum) : 1.f;
-#pragma unroll
-                for (int j = 0; j < NV; ++j) rough[j] = l[j] > -INFINITY ? s[j] * inv + rough[j] : -INFINITY;
-                bad |= clean_row<NV>(rough);
-                id = pick<NV>(l, rough, 0x1p-18f, [&](float x, int e, float &q) {
+                id = pick<NV>(l, reinterpret_cast<float(&)[NV]>(rough), 0x1p-18f, [&](float x, int e, float &q) {
                     q = exact_score(soft, x, top);
                     const float o = (soft ? q / sum : q) + __ldg(a.bias + e);
                     return o < INFINITY ? key_of(o) : kDead;
@@ -395,65 +465,165 @@ route_kernel(const RouteArgs a)
         if (bad_index) atomicOr(a.status, EP_STATUS_BAD_INDEX);
     }
     if (kBal) {
-        __shared__ bool last;
         if (kInRegisters) {
 #pragma unroll
             for (int j = 0; j < NV; ++j) mine[j * 32 + lane] = psum[j % (kInRegisters ? NV : 1)];
         }
         if (lane == 0 && tokens) atomicAdd(counts + a.E, tokens);
+        finish_balance<NV, kWarps>(a, shared, sums, counts);
+    }
+}
+
+// ---- few experts -------------------------------------------------------------------------------------------------
+// Up to 16 experts and many tokens: a thread per token, its row in registers, the picks by plain scans over them. A warp per token
+// leaves most lanes idle there, but its chain is shorter: us with a warp -> a thread per token, forward / with the loss / gradient,
+//   8 experts, top 2:    4096 tokens 2.8 -> 2.4 / 6.6 -> 7.5 / 3.8 -> 3.6     16384 5.8 -> 2.4 / 10.9 -> 7.7 / 8.0 -> 3.7
+//   16, sigmoid + bias, top 8: 16384 7.8 -> 9.0 / 13.2 -> 20.8 / 7.8 -> 7.7   65536 24.9 -> 11.6 / 32.2 -> 23.3 / 22.4 -> 9.8
+// hence from 2048 tokens per expert on.
+
+constexpr int kFew = 16, kFewWarps = 8, kFewCtas = 4 * 148;
+
+template <int NE, class T>
+__device__ __forceinline__ void load_few(const T *row, int E, int vec, float (&l)[NE])
+{
+#pragma unroll
+    for (int j = 0; j < NE; j += 4) {
+        float v[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        if (vec) {
+            if (j < E) value4(row, j, v);
+        } else {
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                if (j + c < E) v[c] = value(row, j + c);
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) l[j + c] = v[c];
+    }
+}
+
+// Cleans the row; the largest logit (-inf: no expert), the scores (softmax: before the division by their sum) and their sum.
+template <int NE>
+__device__ __forceinline__ float score_few(float (&l)[NE], bool soft, float (&s)[NE], float &sum, bool &bad)
+{
+    float top = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < NE; ++j) {
+        if (!(l[j] < INFINITY)) bad = true, l[j] = -INFINITY;
+        top = fmaxf(top, l[j]);
+    }
+    sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < NE; ++j) {
+        s[j] = top == -INFINITY ? 0.f : rough_score(soft, l[j], top);
+        sum += s[j];
+    }
+    return top;
+}
+
+template <class T, int NE, int MODE>
+__global__ void __launch_bounds__(kFewWarps * 32)
+route_few_kernel(const RouteArgs a)
+{
+    constexpr bool kBal = MODE != kRoute;
+    __shared__ float shared[kFewWarps * 64], sums[kFewWarps * 32];
+    __shared__ int counts[kFew + 1 > kFewWarps ? kFew + 1 : kFewWarps];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const bool soft = a.scoring == EP_SCORE_SOFTMAX;
+    float psum[NE];
+    int cnt[NE], tokens = 0;
+    if (kBal) {
+#pragma unroll
+        for (int j = 0; j < NE; ++j) psum[j] = 0.f, cnt[j] = 0;
+        if (threadIdx.x <= a.E) counts[threadIdx.x] = 0;
         __syncthreads();
-        for (int i = threadIdx.x; i < kPadded; i += blockDim.x) {
-            const int e = expert_of<NV>(i >> 5, i & 31);
-            if (e < a.E) {
-                float v = 0.f;
-#pragma unroll 8
-                for (int w = 0; w < kWarps; ++w) v += sums[(size_t)w * kPadded + i];
-                const size_t at = (size_t)(blockIdx.x % kRows) * a.E + e;
-                if (v > 0.f) atomicAdd(a.sums + at, __float2ull_rn(ldexpf(v, a.shift)));
-                if (counts[e]) atomicAdd(a.sum_counts + at, counts[e]);
+    }
+    bool bad = false, bad_index = false;
+    for (unsigned t = blockIdx.x * blockDim.x + threadIdx.x; t < (unsigned)a.T; t += gridDim.x * blockDim.x) {
+        float l[NE], s[NE], sum;
+        load_few<NE>(static_cast<const T *>(a.logits) + (size_t)t * a.E, a.E, a.vec, l);
+        const float top = score_few<NE>(l, soft, s, sum, bad);
+        bool counted = top > -INFINITY;
+        if (MODE == kBalance) {
+            bool any = false;
+            for (int k = 0; k < a.K; ++k) {
+                const int id = __ldg(a.topk_idx + (size_t)t * a.K + k);
+                bad_index |= id < -1 || id >= a.E;
+                any |= id >= 0 && id < a.E;
+#pragma unroll
+                for (int j = 0; j < NE; ++j) cnt[j] += id == j && j < a.E;
+            }
+            counted &= any;
+        } else {
+            uint32_t key[NE];
+            if (a.bias) {
+#pragma unroll
+                for (int j = 0; j < NE; ++j) {
+                    float v = -INFINITY;
+                    if (l[j] > -INFINITY) {
+                        v = exact_score(soft, l[j], top);
+                        v = (soft ? v / sum : v) + __ldg(a.bias + j);
+                        if (!(v < INFINITY)) bad = true, v = -INFINITY;
+                    }
+                    key[j] = key_of(v);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < NE; ++j) key[j] = key_of(l[j]);
+            }
+            float w[kFew], picked = 0.f;
+            int32_t *ids = a.topk_idx + (size_t)t * a.K;
+            float *weights = a.topk_weights + (size_t)t * a.K;
+            const int rounds = min(a.K, kFew);
+#pragma unroll 1
+            for (int k = 0; k < rounds; ++k) {                                // rolled: sixteen copies outgrew the instruction cache
+                uint32_t best = kDead;
+                int at = -1;
+                float x = 0.f;
+#pragma unroll
+                for (int j = 0; j < NE; ++j)
+                    if (key[j] > best) best = key[j], at = j, x = l[j];       // the lowest id of equal keys
+#pragma unroll
+                for (int j = 0; j < NE; ++j)
+                    if (at == j) {
+                        key[j] = 0u;
+                        if (kBal) ++cnt[j];
+                    }
+                if (k == 0) counted = at >= 0;                                // a bias may mask what the logits did not
+                w[k] = at >= 0 ? exact_score(soft, x, top) : 0.f;
+                picked += w[k];
+                ids[k] = at;
+            }
+            const float by = a.renormalize ? picked : soft ? sum : 1.f;
+#pragma unroll 1
+            for (int k = 0; k < a.K; ++k) {
+                if (k >= rounds) ids[k] = -1;
+                weights[k] = k < rounds && by > 0.f ? w[k] / by * a.scale : 0.f;
             }
         }
-        int32_t *total = a.sum_counts + (size_t)kRows * a.E;                  // tokens, CTAs
-        if (threadIdx.x == 0 && counts[a.E]) atomicAdd(total, counts[a.E]);
-        __threadfence();
-        __syncthreads();
-        if (threadIdx.x == 0) last = atomicAdd(total + 1, 1) == (int)gridDim.x - 1;
-        __syncthreads();
-        if (!last) return;
-        __threadfence();
-        const int n = __ldcg(total);
-        const float unit = n ? ldexpf(1.f, -a.shift) / (float)n : 0.f;
-        float dot = 0.f;                                                      // sum of count * (mean probability)
-        int picks = 0;
-        for (int e = threadIdx.x; e < a.E; e += blockDim.x) {
-            unsigned long long p[kRows];
-            int k[kRows];
+        if (kBal && counted) {
+            const float inv = sum > 0.f ? 1.f / sum : 0.f;
 #pragma unroll
-            for (int r = 0; r < kRows; ++r) p[r] = __ldcg(a.sums + (size_t)r * a.E + e), k[r] = __ldcg(a.sum_counts + (size_t)r * a.E + e);
-#pragma unroll
-            for (int r = 0; r < kRows; ++r) a.sums[(size_t)r * a.E + e] = 0ull, a.sum_counts[(size_t)r * a.E + e] = 0;
-#pragma unroll
-            for (int r = 1; r < kRows; ++r) p[0] += p[r], k[0] += k[r];
-            const float mean = __ull2float_rn(p[0]) * unit;
-            a.mean_probs[e] = mean;
-            a.expert_counts[e] = k[0];
-            dot += (float)k[0] * mean;
-            picks += k[0];
+            for (int j = 0; j < NE; ++j) psum[j] += s[j] * inv;
+            ++tokens;
         }
-        dot = warp_sum(dot);
-        picks = __reduce_add_sync(kFullMask, picks);
-        __syncthreads();
-        if (lane == 0) shared[warp] = dot, counts[warp] = picks;
-        __syncthreads();
-        if (warp == 0) {
-            dot = warp_sum(lane < kWarps ? shared[lane] : 0.f);
-            picks = __reduce_add_sync(kFullMask, lane < kWarps ? counts[lane] : 0);
+    }
+    if (a.status) {
+        if (bad) atomicOr(a.status, EP_STATUS_BAD_LOGIT);
+        if (bad_index) atomicOr(a.status, EP_STATUS_BAD_INDEX);
+    }
+    if (kBal) {
+#pragma unroll
+        for (int j = 0; j < NE; ++j) {
+            const float p = warp_sum(psum[j]);
+            const int c = __reduce_add_sync(kFullMask, cnt[j]);
             if (lane == 0) {
-                *a.loss = picks ? a.coef * (float)a.E / (float)picks * dot : 0.f;
-                *a.tokens = n;
-                total[0] = total[1] = 0;
+                sums[warp * 32 + j] = p;
+                if (j < a.E && c) atomicAdd(counts + j, c);
             }
         }
+        tokens = __reduce_add_sync(kFullMask, tokens);
+        if (lane == 0 && tokens) atomicAdd(counts + a.E, tokens);
+        finish_balance<1, kFewWarps>(a, shared, sums, counts);
     }
 }
 
@@ -615,6 +785,97 @@ route_grad_kernel(const RouteGradArgs a)
     }
 }
 
+template <class T, int NE>
+__global__ void __launch_bounds__(kFewWarps * 32)
+route_few_grad_kernel(const RouteGradArgs a)
+{
+    const bool soft = a.scoring == EP_SCORE_SOFTMAX, balance = a.counts != nullptr;
+    float f[NE];                                                              // gradient of the probabilities
+#pragma unroll
+    for (int j = 0; j < NE; ++j) f[j] = 0.f;
+    if (balance) {
+        int total = 0;
+#pragma unroll
+        for (int j = 0; j < NE; ++j)
+            if (j < a.E) {
+                const int c = __ldg(a.counts + j);
+                total += c;
+                f[j] = (float)c;
+            }
+        const int tokens = __ldg(a.tokens);
+        const float unit = total && tokens ? __ldg(a.d_loss) * a.coef / (float)tokens * ((float)a.E / (float)total) : 0.f;
+#pragma unroll
+        for (int j = 0; j < NE; ++j) f[j] *= unit;
+    }
+    for (unsigned t = blockIdx.x * blockDim.x + threadIdx.x; t < (unsigned)a.T; t += gridDim.x * blockDim.x) {
+        float l[NE], s[NE], sum;
+        bool bad = false;
+        load_few<NE>(static_cast<const T *>(a.logits) + (size_t)t * a.E, a.E, a.vec, l);
+        const float top = score_few<NE>(l, soft, s, sum, bad);
+        const float inv = sum > 0.f ? 1.f / sum : 0.f;
+        float k_grad[NE], v[NE] /* of the picks */, picked = 0.f, dot = 0.f, picked_dot = 0.f;
+        bool any = false;
+#pragma unroll
+        for (int j = 0; j < NE; ++j) k_grad[j] = 0.f, v[j] = 0.f;
+        unsigned chosen = 0u;
+#pragma unroll 1
+        for (int k = 0; k < a.K; ++k) {
+            const int id = __ldg(a.topk_idx + (size_t)t * a.K + k);
+            if (id < 0 || id >= a.E) continue;
+            any = true;
+            chosen |= 1u << id;
+            if (!a.d_weights) continue;
+            const float dw = a.scale * __ldg(a.d_weights + (size_t)t * a.K + k);
+            float x = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < NE; ++j)
+                if (id == j) x = l[j];
+            const float score = x > -INFINITY ? exact_score(soft, x, top) * (soft ? inv : 1.f) : 0.f;
+#pragma unroll
+            for (int j = 0; j < NE; ++j)
+                if (id == j) k_grad[j] = dw, v[j] = score;                    // a token's picks are distinct
+            picked += score;
+            dot += dw * score;
+        }
+        const bool counted = top > -INFINITY && any;
+        if (a.d_weights) {
+            const float mean = a.renormalize && picked > 0.f ? dot / picked : 0.f;
+#pragma unroll
+            for (int j = 0; j < NE; ++j) {
+                if (a.renormalize) k_grad[j] = picked > 0.f && ((chosen >> j) & 1u) ? (k_grad[j] - mean) / picked : 0.f;
+                picked_dot += k_grad[j] * v[j];
+            }
+        }
+        float p_dot = 0.f;
+#pragma unroll
+        for (int j = 0; j < NE; ++j) p_dot += s[j] * f[j];
+        p_dot *= inv;
+        T *out = static_cast<T *>(a.dlogits) + (size_t)t * a.E;
+        float d[NE];
+#pragma unroll
+        for (int j = 0; j < NE; ++j) {
+            const float p = s[j] * inv, g = balance ? f[j] - p_dot : 0.f;
+            d[j] = !counted ? 0.f : soft ? p * (g + (k_grad[j] - picked_dot)) : (p * g + s[j] * k_grad[j]) * (1.f - s[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < NE; j += 4) {
+            if (a.vec) {
+                if (j < a.E) {
+                    if (sizeof(T) == 4)
+                        *reinterpret_cast<float4 *>(reinterpret_cast<float *>(out) + j) = make_float4(d[j], d[j + 1], d[j + 2], d[j + 3]);
+                    else
+                        *reinterpret_cast<uint2 *>(reinterpret_cast<uint16_t *>(out) + j) =
+                            make_uint2(pack_bf16x2(d[j], d[j + 1]), pack_bf16x2(d[j + 2], d[j + 3]));
+                }
+            } else {
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (j + c < a.E) out[j + c] = (T)d[j + c];
+            }
+        }
+    }
+}
+
 // ---- host side ---------------------------------------------------------------------------------------------------
 
 int check_router(const ep_router_t *r)
@@ -634,10 +895,14 @@ int values_per_lane(int E)
     return nv;
 }
 
+bool thread_per_token(const ep_router_t &r) { return r.num_experts <= kFew && r.num_tokens >= 2048 * r.num_experts; }
+
 int balance_ctas(const ep_router_t &r)
 {
-    const int want = ceil_div(r.num_tokens, route_warps(values_per_lane(r.num_experts), true));
-    return want < kBalanceCtas ? (want < 1 ? 1 : want) : kBalanceCtas;
+    const bool few = thread_per_token(r);
+    const int want = ceil_div(r.num_tokens, few ? kFewWarps * 32 : route_warps(values_per_lane(r.num_experts), true));
+    const int most = few ? kFewCtas : kBalanceCtas;
+    return want < most ? (want < 1 ? 1 : want) : most;
 }
 
 bool rows_of_vectors(const ep_router_t &r, const void *p)   // may a lane load four neighbouring logits at once?
@@ -679,11 +944,13 @@ int launch_route_grad(const RouteGradArgs &a, cudaStream_t stream)
     return EP_OK;
 }
 
-// Calls f.template operator()<T, NV>() for the router's type and size.
+// Calls f.run<T, values per lane>() or, with few experts, f.few<T, values per thread>() for the router's type and size.
 template <class F>
 int for_router(const ep_router_t &r, F f)
 {
     const bool f32 = r.logits_dtype == EP_DTYPE_F32;
+    if (thread_per_token(r) && r.num_experts <= 8) return f32 ? f.template few<float, 8>() : f.template few<__nv_bfloat16, 8>();
+    if (thread_per_token(r)) return f32 ? f.template few<float, kFew>() : f.template few<__nv_bfloat16, kFew>();
     switch (values_per_lane(r.num_experts)) {
 #define EP_CASE(nv) case nv: return f32 ? f.template run<float, nv>() : f.template run<__nv_bfloat16, nv>();
         EP_CASE(1) EP_CASE(2) EP_CASE(4) EP_CASE(8) EP_CASE(16) EP_CASE(32) EP_CASE(64)
@@ -692,17 +959,37 @@ int for_router(const ep_router_t &r, F f)
     }
 }
 
+template <class T, int NE, int MODE>
+int launch_few(const RouteArgs &a, int ctas, cudaStream_t stream)
+{
+    if (MODE == kRoute) ctas = ceil_div(a.T, kFewWarps * 32);
+    route_few_kernel<T, NE, MODE><<<ctas, kFewWarps * 32, 0, stream>>>(a);
+    EP_LAUNCH_CHECK(1);
+    return EP_OK;
+}
+
+template <class T, int NE>
+int launch_few_grad(const RouteGradArgs &a, cudaStream_t stream)
+{
+    const int ctas = ceil_div(a.T, kFewWarps * 32);
+    route_few_grad_kernel<T, NE><<<ctas < kFewCtas ? ctas : kFewCtas, kFewWarps * 32, 0, stream>>>(a);
+    EP_LAUNCH_CHECK(1);
+    return EP_OK;
+}
+
 template <int MODE>
 struct RunRoute {
     const RouteArgs &a;
     int ctas;
     cudaStream_t stream;
     template <class T, int NV> int run() const { return launch_route<T, NV, MODE>(a, ctas, stream); }
+    template <class T, int NE> int few() const { return launch_few<T, NE, MODE>(a, ctas, stream); }
 };
 struct RunRouteGrad {
     const RouteGradArgs &a;
     cudaStream_t stream;
     template <class T, int NV> int run() const { return launch_route_grad<T, NV>(a, stream); }
+    template <class T, int NE> int few() const { return launch_few_grad<T, NE>(a, stream); }
 };
 
 int check_balance(const ep_balance_t *b)

@@ -18,7 +18,7 @@ def scores(logits, sigmoid):
     l, dead = logits.double(), masked(logits)
     safe = torch.where(dead, 0.0, l)
     if sigmoid:
-        s = torch.where(dead, 0.0, 1.0 / (1.0 + torch.exp(-safe)))
+        s = torch.where(dead, 0.0, torch.sigmoid(safe))            # (written out, its derivative is inf * 0 for the lowest logits)
         total = s.sum(1, keepdim=True)
         return s, s / torch.where(total == 0, 1.0, total)
     top = torch.where(dead, -math.inf, l).amax(1, keepdim=True)
@@ -35,14 +35,15 @@ def route(logits, K, sigmoid=False, bias=None, renormalize=True, scale=1.0, orde
     v = order_by if order_by is not None else (logits.double() if bias is None else s + bias.double())
     v = torch.where(dead, -math.inf, v.double())
     T, E = logits.shape
+    order = torch.sort(v, dim=1, descending=True, stable=True)          # equal values stay in the order of their ids
+    n = min(K, E)
+    some = order.values[:, :n] > -math.inf
     idx = torch.full((T, K), -1, dtype=torch.int32)
     w = torch.zeros(T, K, dtype=torch.float64)
-    for t in range(T):
-        picks = sorted((e for e in range(E) if v[t, e] > -math.inf), key=lambda e: (-float(v[t, e]), e))[:K]
-        total = sum(float(s[t, e]) for e in picks) if renormalize else 1.0
-        for k, e in enumerate(picks):
-            idx[t, k] = e
-            w[t, k] = scale * float(s[t, e]) / total if total > 0 else 0.0
+    idx[:, :n] = torch.where(some, order.indices[:, :n], -1).to(torch.int32)
+    picked = torch.where(some, torch.gather(s, 1, order.indices[:, :n]), 0.0)
+    total = picked.sum(1, keepdim=True) if renormalize else torch.ones(T, 1, dtype=torch.float64)
+    w[:, :n] = torch.where(total > 0, scale * picked / torch.where(total > 0, total, 1.0), 0.0)
     return idx, w
 
 

@@ -33,7 +33,7 @@ def _compare_route(logits, router, bias=None, order_by=None):
     return got, idx
 
 
-SIZES = [(1, 1, 1), (1, 8, 2), (3, 4, 4), (64, 8, 2), (5, 31, 3), (4, 32, 32), (9, 33, 5), (7, 60, 6), (17, 64, 8), (33, 127, 7),
+SIZES = [(1, 1, 1), (1, 8, 2), (300, 8, 8), (5, 7, 9), (257, 13, 4), (40, 16, 16), (31, 16, 3), (40, 17, 5), (3, 4, 4), (64, 8, 2), (5, 31, 3), (4, 32, 32), (9, 33, 5), (7, 60, 6), (17, 64, 8), (33, 127, 7),
          (20, 128, 8), (257, 256, 8), (13, 257, 4), (6, 510, 10), (8, 512, 10), (3, 1000, 8), (2, 1025, 3), (3, 2044, 9), (2, 4096, 32)]
 
 
@@ -44,6 +44,50 @@ def test_picks_and_weights(T, E, K, dtype, sigmoid):
     logits = _logits(T, E, dtype, T * E + K)
     for renormalize, scale in ((True, 1.0), (False, 2.5)):
         _compare_route(logits, ep.Router(E, K, scoring=int(sigmoid), renormalize=renormalize, scale=scale))
+
+
+@pytest.mark.parametrize("T,E,K", [(2048, 1, 1), (6200, 3, 3), (10241, 5, 7), (16384, 8, 2), (16500, 8, 8), (23000, 11, 3), (26700, 13, 1), (32769, 16, 16)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("renormalize", [False, True])
+def test_many_tokens_on_few_experts(T, E, K, dtype, sigmoid, renormalize):
+    """Picks, weights, loss and gradient where a thread takes a token: masked tokens and experts, NaN, ties (coarse logits)."""
+    logits = _logits(T, E, torch.float32, T + E)
+    logits[::3] = (logits[::3] * 2).round() / 2
+    logits[torch.rand(T, generator=torch.Generator().manual_seed(E)) < 0.05] = -math.inf
+    logits[5, 0] = math.nan
+    logits[7, E - 1] = math.inf
+    logits[9] = torch.finfo(torch.float32).min if dtype == torch.float32 else -1e38
+    logits = logits.to(dtype)
+    router = ep.Router(E, K, scoring=int(sigmoid), renormalize=renormalize, scale=1.5, balance_coef=0.4)
+    got, idx = _compare_route(logits, router)
+    assert int(got.status) == ep.STATUS_BAD_LOGIT
+    _compare_balance(got, logits, idx, sigmoid, 0.4)
+    plain_call = ep.ep_route(logits.cuda(), router, out=ep.alloc_routing(T, E, K))
+    assert torch.equal(plain_call.topk_idx, got.topk_idx) and torch.equal(plain_call.topk_weights, got.topk_weights)
+    table = idx.clone()
+    table[11] = -1
+    alone = ep.ep_balance_loss(logits.cuda(), router, table.cuda())
+    _compare_balance(alone, logits, table, sigmoid, 0.4)
+    dw, dl = torch.randn(T, K, generator=torch.Generator().manual_seed(1)), 700.0
+    grad = ep.ep_route_backward(logits.cuda(), router, got, d_weights=dw.cuda(), d_loss=torch.full((1,), dl, device="cuda"))
+    want = plain.route_gradient(logits, idx, dw, sigmoid, renormalize, 1.5, 0.4, dl)
+    s = plain.scores(logits, sigmoid)[0]
+    picked = torch.where(idx >= 0, torch.gather(s, 1, idx.clamp(min=0).long()), 0.0)
+    unit = 1.5 / (picked.sum(1, keepdim=True).clamp(min=1e-300) if renormalize else torch.ones(T, 1, dtype=torch.float64))
+    largest = (dw.double().abs() * unit * picked).amax(1, keepdim=True)
+    counts = got.expert_counts.cpu().double()
+    share = dl * 0.4 / int(got.tokens) * E * counts.max() / counts.sum()
+    tol = 2.0 ** -14 * (largest + share) + 1e-30 + (2.0 ** -8 * want.abs() if dtype == torch.bfloat16 else 0.0)
+    assert ((grad.cpu().double() - want).abs() <= tol).all()
+    bias = (torch.randint(-8, 9, (E,), generator=torch.Generator().manual_seed(2)).float() * 4)    # outweighs every score: orders alone
+    biased = ep.ep_route(logits.cuda(), router, bias=bias.cuda(), out=ep.alloc_routing(T, E, K, balance=True))
+    ids = biased.topk_idx.cpu()
+    order = torch.where(plain.masked(logits), -math.inf, (s + bias.double()))
+    ranked = torch.gather(order, 1, ids.clamp(min=0).long())
+    assert (ranked[:, :-1] >= ranked[:, 1:] - 1e-6).masked_fill(ids[:, 1:] < 0, True).all()
+    assert torch.equal((ids >= 0).sum(1), (order > -math.inf).sum(1).clamp(max=K))
+    _compare_balance(biased, logits, ids, sigmoid, 0.4)
 
 
 def test_equal_logits_go_to_the_lowest_expert():
@@ -122,7 +166,7 @@ def test_selection_bias_orders_but_does_not_weigh(T, E, K, sigmoid):
     assert not (got.topk_idx == 1 % E).any() and int(got.status) == 0
 
 
-BALANCE = [(1, 8, 2), (64, 8, 2), (300, 60, 6), (1000, 128, 8), (97, 257, 4), (2500, 256, 8), (40, 1030, 8), (9, 4096, 32)]
+BALANCE = [(1, 8, 2), (64, 8, 2), (700, 5, 2), (3000, 16, 4), (333, 11, 3), (50, 17, 3), (300, 60, 6), (1000, 128, 8), (97, 257, 4), (2500, 256, 8), (40, 1030, 8), (9, 4096, 32)]
 
 
 def _compare_balance(got, logits, idx, sigmoid, coef):
@@ -170,7 +214,7 @@ def test_balance_of_nothing_is_zero():
         assert d.shape == (T, 16) and d.abs().sum() == 0
 
 
-@pytest.mark.parametrize("T,E,K", [(1, 8, 2), (64, 8, 8), (50, 60, 6), (200, 128, 8), (33, 257, 4), (300, 256, 8), (12, 1030, 8), (4, 4096, 32)])
+@pytest.mark.parametrize("T,E,K", [(1, 8, 2), (64, 8, 8), (300, 5, 2), (77, 16, 5), (30, 11, 11), (50, 60, 6), (200, 128, 8), (33, 257, 4), (300, 256, 8), (12, 1030, 8), (4, 4096, 32)])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("sigmoid", [False, True])
 @pytest.mark.parametrize("renormalize", [False, True])
@@ -269,6 +313,22 @@ def test_unaligned_rows_other_streams_and_graphs():
         fresh = ep.ep_route(static, router)
         assert torch.equal(out.topk_idx, fresh.topk_idx) and torch.equal(out.loss, fresh.loss)
         assert torch.equal(grad, ep.ep_route_backward(static, router, fresh, d_weights=dw, d_loss=dl))
+
+
+@pytest.mark.parametrize("E", [8, 13, 24, 256])
+def test_tokens_that_a_bias_leaves_without_an_expert_are_not_counted(E):
+    T, K = 20, 3
+    logits = _logits(T, E, torch.float32, 2)
+    logits[:7, 4:] = -math.inf                                  # seven tokens know only experts 0 to 3 ...
+    bias = torch.zeros(E)
+    bias[:4] = -math.inf                                        # ... which are shut
+    router = ep.Router(E, K, scoring=ep.SCORE_SIGMOID, balance_coef=0.3)
+    got = ep.ep_route(logits.cuda(), router, bias=bias.cuda(), out=ep.alloc_routing(T, E, K, balance=True))
+    idx = got.topk_idx.cpu()
+    assert (idx[:7] == -1).all() and (idx[7:] >= 4).all()
+    _compare_balance(got, logits, idx, True, 0.3)
+    d = ep.ep_route_backward(logits.cuda(), router, got, d_weights=torch.ones(T, K, device="cuda"), d_loss=torch.ones(1, device="cuda"))
+    assert d[:7].abs().sum() == 0 and torch.isfinite(d).all()
 
 
 def test_outputs_stay_inside_their_buffers():
