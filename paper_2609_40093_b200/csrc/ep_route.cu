@@ -352,7 +352,7 @@ __device__ __forceinline__ void finish_balance(const RouteArgs &a, float *shared
 // Warps per CTA. With a balance loss one CTA fills an SM as far as the registers allow.
 __host__ __device__ constexpr int route_warps(int nv, bool balance)
 {
-    return nv > 32 ? 4 : !balance ? 8 : nv <= 8 ? 32 : nv == 16 ? 16 : 8;
+    return !balance ? (nv > 32 ? 4 : 8) : nv <= 8 ? 32 : nv <= 16 ? 24 : nv <= 32 ? 16 : 8;
 }
 
 template <class T, int NV, int MODE>
@@ -642,7 +642,7 @@ struct RouteGradArgs {
 
 // One warp per token; the row, its scores and the gradient of the probabilities (the same for every token) stay in registers.
 // Bound by memory at large batches: a row is read and a row is written.
-constexpr int route_grad_ctas(int nv) { return nv <= 8 ? 5 : nv == 16 ? 3 : 2; }   // per SM
+constexpr int route_grad_ctas(int nv) { return nv <= 8 ? 5 : nv <= 12 ? 4 : nv <= 16 ? 3 : 2; }   // per SM
 
 template <class T, int NV>
 __global__ void __launch_bounds__(NV <= 32 ? 256 : 128, route_grad_ctas(NV))
@@ -890,9 +890,9 @@ int check_router(const ep_router_t *r)
 
 int values_per_lane(int E)
 {
-    int nv = 1;
-    while (nv * 32 < E) nv *= 2;
-    return nv;
+    for (const int nv : {1, 2, 4, 8, 12, 16, 24, 32, 64})
+        if (nv * 32 >= E) return nv;
+    return 128;
 }
 
 bool thread_per_token(const ep_router_t &r) { return r.num_experts <= kFew && r.num_tokens >= 2048 * r.num_experts; }
@@ -953,7 +953,7 @@ int for_router(const ep_router_t &r, F f)
     if (thread_per_token(r)) return f32 ? f.template few<float, kFew>() : f.template few<__nv_bfloat16, kFew>();
     switch (values_per_lane(r.num_experts)) {
 #define EP_CASE(nv) case nv: return f32 ? f.template run<float, nv>() : f.template run<__nv_bfloat16, nv>();
-        EP_CASE(1) EP_CASE(2) EP_CASE(4) EP_CASE(8) EP_CASE(16) EP_CASE(32) EP_CASE(64)
+        EP_CASE(1) EP_CASE(2) EP_CASE(4) EP_CASE(8) EP_CASE(12) EP_CASE(16) EP_CASE(24) EP_CASE(32) EP_CASE(64)
     default: return f32 ? f.template run<float, 128>() : f.template run<__nv_bfloat16, 128>();
 #undef EP_CASE
     }
