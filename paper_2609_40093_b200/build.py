@@ -14,7 +14,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libep_b200.so")
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-         "--shared", "-Xcompiler", "-fPIC", "-cudart", "static"]
+         "--threads", "0", "--shared", "-Xcompiler", "-fPIC", "-cudart", "static"]
 
 
 def sources():
