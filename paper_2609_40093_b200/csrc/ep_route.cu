@@ -141,6 +141,12 @@ __device__ __forceinline__ float exact_score(bool soft, float l, float top)
     return soft || low ? e : 1.f / (1.f + e);
 }
 
+// Renormalised weights are ratios of the picked scores. Those of a softmax are ratios of exp(l), and so, below logits of -40 and to the last
+// bit, are those of sigmoids: there they come from the logits' differences to the largest pick, because the scores themselves
+// and the reciprocal of their sum leave fp32's normal range at -87 (for a softmax where a bias picks that far below the largest logit).
+// At kNoScore and below every sigmoid is 0 in fp32, and so are the weights.
+constexpr float kNoScore = -103.97f;
+
 // K rounds of "the largest key, and of its holders the lowest id": lane k gets the k-th's id. `N` keys a lane, of ids that ascend
 // with the position in the lane.
 template <int N, class Id>
@@ -651,7 +657,7 @@ route_grad_kernel(const RouteGradArgs a)
     extern __shared__ float4 shared4[];
     constexpr int kWarps = NV <= 32 ? 8 : 4, kPadded = NV * 32 < 128 ? 128 : NV * 32;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    float *at_pick = reinterpret_cast<float *>(shared4) + (size_t)warp * kPadded;   // gradient of the picked scores, 0 elsewhere
+    float *at_pick = reinterpret_cast<float *>(shared4) + (size_t)warp * kPadded;   // the weights' part at the picks, 0 elsewhere
     __shared__ int total;
     const bool soft = a.scoring == EP_SCORE_SOFTMAX, balance = a.counts != nullptr;
     for (int i = lane; i < kPadded; i += 32) at_pick[i] = 0.f;
@@ -714,22 +720,27 @@ route_grad_kernel(const RouteGradArgs a)
             sum = warp_sum(sum);
             inv = sum > 0.f ? __fdividef(1.f, sum) : 0.f;
         }
-        // gradient with respect to the picked scores
-        float mine = 0.f, picked_dot = 0.f;
+        // The weights' part: the gradient of a picked score times that score. Renormalised, with r = score / (sum of the picked), it
+        // is r (dw - sum r dw), which sums to 0; nothing is divided by the sum and multiplied by a score again, which would be
+        // inf * 0 where both are tiny, nor by a softmax's denominator, which cancels.
+        float picked_dot = 0.f;
         if (a.d_weights) {
-            float v = 0.f;
-            if (id >= 0 && counted) {
-                v = value(row, id);
-                v = !(v < INFINITY) || v == -INFINITY ? 0.f : exact_score(soft, v, top) * (soft ? inv : 1.f);
+            float x = id >= 0 && counted ? value(row, id) : -INFINITY, base = top, part;
+            if (!(x < INFINITY)) x = -INFINITY;
+            bool as_exp = soft;
+            if (a.renormalize && !__any_sync(kFullMask, x >= (soft ? top - 40.f : -40.f))) {      // hardly ever
+                base = warp_max(x);
+                as_exp = soft || base > kNoScore;
             }
+            const float v = x > -INFINITY ? exact_score(as_exp, x, base) : 0.f;
             if (a.renormalize) {
                 const float picked = warp_sum(v), dot = warp_sum(dw * v);
-                mine = picked > 0.f ? (dw - dot / picked) / picked : 0.f;
+                part = picked > 0.f ? (dw - dot / picked) * __fdividef(v, picked) : 0.f;
             } else {
-                mine = dw;
+                part = soft ? dw * v * inv : dw * v;
+                if (soft) picked_dot = warp_sum(part);
             }
-            if (soft) picked_dot = warp_sum(mine * v);
-            if (id >= 0) at_pick[id] = mine;                                  // a token's picks are distinct
+            if (id >= 0) at_pick[id] = part;                                  // a token's picks are distinct
             __syncwarp();
         }
         float dot = 0.f;
@@ -754,7 +765,7 @@ route_grad_kernel(const RouteGradArgs a)
             for (int c = 0; c < (NV < 4 ? 1 : 4); ++c) {
                 const int i = (j + c) % NV;
                 const float p = s[i] * inv, g = balance ? f[i] - dot : 0.f;
-                d[i] = soft ? p * (g + (k[c] - picked_dot)) : (p * g + s[i] * k[c]) * (1.f - s[i]);
+                d[i] = soft ? p * (g - picked_dot) + k[c] : (p * g + k[c]) * (1.f - s[i]);
             }
         }
         if (a.d_weights) {
@@ -813,7 +824,7 @@ route_few_grad_kernel(const RouteGradArgs a)
         load_few<NE>(static_cast<const T *>(a.logits) + (size_t)t * a.E, a.E, a.vec, l);
         const float top = score_few<NE>(l, soft, s, sum, bad);
         const float inv = sum > 0.f ? 1.f / sum : 0.f;
-        float k_grad[NE], v[NE] /* of the picks */, picked = 0.f, dot = 0.f, picked_dot = 0.f;
+        float k_grad[NE] /* at the picks: dw, then the weights' part */, v[NE] /* their scores */, picked = 0.f, dot = 0.f, picked_dot = 0.f;
         bool any = false;
 #pragma unroll
         for (int j = 0; j < NE; ++j) k_grad[j] = 0.f, v[j] = 0.f;
@@ -830,7 +841,7 @@ route_few_grad_kernel(const RouteGradArgs a)
 #pragma unroll
             for (int j = 0; j < NE; ++j)
                 if (id == j) x = l[j];
-            const float score = x > -INFINITY ? exact_score(soft, x, top) * (soft ? inv : 1.f) : 0.f;
+            const float score = x > -INFINITY ? exact_score(soft, x, top) * (soft && !a.renormalize ? inv : 1.f) : 0.f;
 #pragma unroll
             for (int j = 0; j < NE; ++j)
                 if (id == j) k_grad[j] = dw, v[j] = score;                    // a token's picks are distinct
@@ -838,12 +849,27 @@ route_few_grad_kernel(const RouteGradArgs a)
             dot += dw * score;
         }
         const bool counted = top > -INFINITY && any;
-        if (a.d_weights) {
-            const float mean = a.renormalize && picked > 0.f ? dot / picked : 0.f;
+        if (a.d_weights && a.renormalize) {                                   // as above
+            float most = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < NE; ++j)
+                if ((chosen >> j) & 1u) most = fmaxf(most, l[j]);
+            if (soft ? most < top - 40.f : most < -40.f && most > kNoScore) { // hardly ever: the scores above will do otherwise
+                picked = dot = 0.f;
+#pragma unroll
+                for (int j = 0; j < NE; ++j) {
+                    v[j] = ((chosen >> j) & 1u) && l[j] > -INFINITY ? expf(l[j] - most) : 0.f;
+                    picked += v[j], dot += k_grad[j] * v[j];
+                }
+            }
+            const float by = picked > 0.f ? 1.f / picked : 0.f, mean = picked > 0.f ? dot / picked : 0.f;
+#pragma unroll
+            for (int j = 0; j < NE; ++j) k_grad[j] = (k_grad[j] - mean) * (v[j] * by);
+        } else if (a.d_weights) {
 #pragma unroll
             for (int j = 0; j < NE; ++j) {
-                if (a.renormalize) k_grad[j] = picked > 0.f && ((chosen >> j) & 1u) ? (k_grad[j] - mean) / picked : 0.f;
-                picked_dot += k_grad[j] * v[j];
+                k_grad[j] *= v[j];
+                if (soft) picked_dot += k_grad[j];
             }
         }
         float p_dot = 0.f;
@@ -855,7 +881,7 @@ route_few_grad_kernel(const RouteGradArgs a)
 #pragma unroll
         for (int j = 0; j < NE; ++j) {
             const float p = s[j] * inv, g = balance ? f[j] - p_dot : 0.f;
-            d[j] = !counted ? 0.f : soft ? p * (g + (k_grad[j] - picked_dot)) : (p * g + s[j] * k_grad[j]) * (1.f - s[j]);
+            d[j] = !counted ? 0.f : soft ? p * (g - picked_dot) + k_grad[j] : (p * g + k_grad[j]) * (1.f - s[j]);
         }
 #pragma unroll
         for (int j = 0; j < NE; j += 4) {
