@@ -492,7 +492,8 @@ int ep_last_cuda_error(void);
  * balance (may be NULL): the balance loss over the same pass,
  *   f_e = E * expert_counts[e] / sum(expert_counts)
  *   mean_probs[e] = mean over the tokens with a pick of p_e (softmax: the score;
- *                   sigmoid: the score over the sum of the token's scores)
+ *                   sigmoid: the score over the sum of the token's scores; 0 where
+ *                   all of them are 0 in fp32, below logits of -103.9)
  *   loss = balance_coef * sum_e f_e * mean_probs[e]
  * with expert_counts the valid picks per expert and tokens the tokens with a pick
  * (all 0, and loss 0, where there is none). No sum depends on an order: the same

@@ -147,6 +147,18 @@ __device__ __forceinline__ float exact_score(bool soft, float l, float top)
 // At kNoScore and below every sigmoid is 0 in fp32, and so are the weights.
 constexpr float kNoScore = -103.97f;
 
+// The same for the probabilities of the balance loss, a sigmoid over the sum of its row: where that sum is below kSmallSum the scores
+// are taken as 2^-64 exp(l - most), whose ratios are theirs, and beside which 1 - score is 1 as it is beside theirs.
+constexpr float kSmallSum = 0x1p-57f;
+template <int N>
+__device__ __forceinline__ void scale_small_sigmoids(const float (&l)[N], float most, float (&s)[N])
+{
+    if (most > kNoScore) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) s[j] = 0x1p-64f * __expf(l[j] - most);
+    }
+}
+
 // K rounds of "the largest key, and of its holders the lowest id": lane k gets the k-th's id. `N` keys a lane, of ids that ascend
 // with the position in the lane.
 template <int N, class Id>
@@ -416,6 +428,13 @@ route_kernel(const RouteArgs a)
 #pragma unroll
                 for (int j = 0; j < NV; ++j) sum += s[j];
                 sum = warp_sum(sum);
+                if (kBal && !soft && sum < kSmallSum) {                       // hardly ever
+                    scale_small_sigmoids<NV>(l, warp_max(top), s);
+                    sum = 0.f;
+#pragma unroll
+                    for (int j = 0; j < NV; ++j) sum += s[j];
+                    sum = warp_sum(sum);
+                }
             }
         }
         float rough[MODE != kBalance ? NV : 1];                               // what orders the picks, where there is a bias
@@ -432,7 +451,7 @@ route_kernel(const RouteArgs a)
             counted = __any_sync(kFullMask, most > -INFINITY);                // a bias of -inf masks too
         }
         if (kBal && counted) {
-            const float inv = sum > 0.f ? __fdividef(1.f, sum) : 0.f;         // sigmoids of very negative logits can all be 0
+            const float inv = sum > 0.f ? __fdividef(1.f, sum) : 0.f;         // sigmoids of logits below -103.97 are 0
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
                 if (kInRegisters) psum[j % (kInRegisters ? NV : 1)] += s[j] * inv;
@@ -522,6 +541,12 @@ __device__ __forceinline__ float score_few(float (&l)[NE], bool soft, float (&s)
     for (int j = 0; j < NE; ++j) {
         s[j] = top == -INFINITY ? 0.f : rough_score(soft, l[j], top);
         sum += s[j];
+    }
+    if (!soft && sum < kSmallSum) {                                           // hardly ever
+        scale_small_sigmoids<NE>(l, top, s);
+        sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < NE; ++j) sum += s[j];
     }
     return top;
 }
@@ -710,13 +735,17 @@ route_grad_kernel(const RouteGradArgs a)
         for (int j = 1; j < NV; ++j) top = fmaxf(top, l[j]);
         if (soft) top = warp_max(top);
         const bool counted = __any_sync(kFullMask, top > -INFINITY) && __any_sync(kFullMask, id >= 0);
+        if (!soft && balance && !__any_sync(kFullMask, top >= -40.f)) {       // hardly ever: scale_small_sigmoids, in place
+            const float most = warp_max(top), shift = most > kNoScore ? most + 44.361420f : 0.f;
+#pragma unroll
+            for (int j = 0; j < NV; ++j) l[j] -= shift;
+        }
         float s[NV], sum = 0.f, inv = 0.f;
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            s[j] = counted ? rough_score(soft, l[j], top) : 0.f;
-            sum += s[j];
-        }
+        for (int j = 0; j < NV; ++j) s[j] = counted ? rough_score(soft, l[j], top) : 0.f;
         if (soft || balance) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) sum += s[j];
             sum = warp_sum(sum);
             inv = sum > 0.f ? __fdividef(1.f, sum) : 0.f;
         }

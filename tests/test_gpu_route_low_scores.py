@@ -84,3 +84,23 @@ def test_gradient_of_picks_that_a_bias_takes_from_far_below(T, E, K, sigmoid, re
     want = _compare_gradient(got, logits, idx, dw, sigmoid, renormalize, 1.5)
     if renormalize:
         assert (want[:6].abs().amax(1) > 1e-3).all()
+
+
+@pytest.mark.parametrize("T,E,K", SIZES)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_balance_loss_of_small_sigmoids(T, E, K, dtype):
+    """A token's probabilities are its scores over their sum, however small the sum is, with and without the picks."""
+    logits = _low_rows(T, E, T + E, dtype)
+    logits[1::4, E // 2:] -= 95.0                               # scores of a row far apart
+    router = ep.Router(E, K, scoring=ep.SCORE_SIGMOID, balance_coef=0.3)
+    dev = logits.cuda()
+    got = ep.ep_route(dev, router)
+    idx = got.topk_idx.cpu()
+    _compare_balance(got, logits, idx, True, 0.3)
+    table = torch.randint(0, E, (T, K), generator=torch.Generator().manual_seed(3), dtype=torch.int32)
+    alone = ep.ep_balance_loss(dev, router, table.cuda())
+    _compare_balance(alone, logits, table, True, 0.3)
+    d_loss = 50.0
+    for r, ids in ((got, idx), (alone, table)):
+        grad = ep.ep_route_backward(dev, router, r, d_loss=torch.full((1,), d_loss, device="cuda"))
+        _compare_gradient(grad, logits, ids, None, True, True, 1.0, 0.3, d_loss, int(r.tokens), r.expert_counts.cpu().double())
