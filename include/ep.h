@@ -483,7 +483,8 @@ int ep_last_cuda_error(void);
  *           score_e + bias_e; equal values by ascending expert id, -0 equal to +0;
  *           topk_idx[t][k] in descending order
  *   weight  scale * score of the pick (never with the bias), divided by the sum of
- *           the token's K picked scores if renormalize is set (0 if that sum is 0)
+ *           the token's K picked scores if renormalize is set (0 where these are
+ *           sigmoids that are all 0 in fp32, below logits of -103.9)
  * A logit of -inf masks an expert for that token. NaN and +inf mask it too and set
  * EP_STATUS_BAD_LOGIT in *status (device, may be NULL; bits are OR-ed in). Where
  * fewer than K experts are left, the rest of the row is -1 with weight 0, which

@@ -473,7 +473,14 @@ route_kernel(const RouteArgs a)
             }
             if (id < 0) w = 0.f;
             if (a.renormalize) {
-                const float picked = warp_sum(w);
+                float picked = warp_sum(w);
+                if (picked < kSmallSum) {                                     // hardly ever
+                    const float x = id >= 0 ? value(row, id) : -INFINITY, most = warp_max(x);
+                    if (soft || most > kNoScore) {
+                        w = id >= 0 ? expf(x - most) : 0.f;
+                        picked = warp_sum(w);
+                    }
+                }
                 w = picked > 0.f ? w / picked : 0.f;
             } else if (soft) {
                 w /= sum;
@@ -623,6 +630,21 @@ route_few_kernel(const RouteArgs a)
                 w[k] = at >= 0 ? exact_score(soft, x, top) : 0.f;
                 picked += w[k];
                 ids[k] = at;
+            }
+            if (a.renormalize && picked < kSmallSum) {                        // hardly ever
+                const T *row = static_cast<const T *>(a.logits) + (size_t)t * a.E;
+                float most = -INFINITY;
+#pragma unroll 1
+                for (int k = 0; k < rounds; ++k)
+                    if (ids[k] >= 0) most = fmaxf(most, value(row, ids[k]));
+                if (soft || most > kNoScore) {
+                    picked = 0.f;
+#pragma unroll 1
+                    for (int k = 0; k < rounds; ++k) {
+                        w[k] = ids[k] >= 0 ? expf(value(row, ids[k]) - most) : 0.f;
+                        picked += w[k];
+                    }
+                }
             }
             const float by = a.renormalize ? picked : soft ? sum : 1.f;
 #pragma unroll 1

@@ -104,3 +104,23 @@ def test_balance_loss_of_small_sigmoids(T, E, K, dtype):
     for r, ids in ((got, idx), (alone, table)):
         grad = ep.ep_route_backward(dev, router, r, d_loss=torch.full((1,), d_loss, device="cuda"))
         _compare_gradient(grad, logits, ids, None, True, True, 1.0, 0.3, d_loss, int(r.tokens), r.expert_counts.cpu().double())
+
+
+@pytest.mark.parametrize("T,E,K", SIZES)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_renormalised_weights_of_small_sigmoids(T, E, K, dtype):
+    logits = _low_rows(T, E, T + E, dtype)
+    got = ep.ep_route(logits.cuda(), ep.Router(E, K, scoring=ep.SCORE_SIGMOID, scale=2.5))
+    idx, w = plain.route(logits, K, True, None, True, 2.5)
+    assert torch.equal(got.topk_idx.cpu(), idx)
+    assert ((got.topk_weights.cpu().double() - w).abs() <= WEIGHT * w + TINY).all()
+
+
+@pytest.mark.parametrize("T,E,K", [(30, 8, 3), (30, 24, 4), (30, 60, 6), (24, 256, 8), (24, 300, 5), (16, 1030, 4), (16384, 8, 2), (32768, 16, 4)])
+@pytest.mark.parametrize("sigmoid", [False, True])
+def test_renormalised_weights_of_picks_that_a_bias_takes_from_far_below(T, E, K, sigmoid):
+    logits, bias = _far_picks(T, E, K)
+    got = ep.ep_route(logits.cuda(), ep.Router(E, K, scoring=int(sigmoid)), bias=bias.cuda())
+    idx, w = plain.route(logits, K, sigmoid, bias)
+    assert torch.equal(got.topk_idx.cpu(), idx)
+    assert ((got.topk_weights.cpu().double() - w).abs() <= WEIGHT * w + TINY).all()
