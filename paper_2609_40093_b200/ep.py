@@ -185,9 +185,11 @@ def _on_device(device, *tensors):
 
 
 def _stream_of(first, *others):
-    """The current stream, as an address, of the CUDA device on which all these tensors (or None) have to be."""
+    """The current stream, as an address. All these tensors (or None) have to be on the current CUDA device, where the library launches."""
     device = first.get_device()
     _on_device(device, *others)
+    if device != torch._C._cuda_getDevice():
+        raise ValueError(f"the EP library works on the current CUDA device, cuda:{torch._C._cuda_getDevice()}, got tensors on cuda:{device}")
     return torch._C._cuda_getCurrentRawStream(device)
 
 
