@@ -78,7 +78,7 @@ inline int check_shape(const ep_shape_t *s, bool need_hidden)
     return EP_OK;
 }
 
-inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
+inline int ceil_div(int a, int b) { return (int)(((int64_t)a + b - 1) / b); }   // a may lie just below 2^31
 
 // Launch through cudaLaunchKernelEx. pdl: with programmatic stream serialisation, i.e. the kernel's CTAs
 // may become resident while the previous kernel of the stream is still running; the kernel must execute
