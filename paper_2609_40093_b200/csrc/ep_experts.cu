@@ -80,6 +80,9 @@ __device__ __forceinline__ int segment_bound(int32_t v, long long rows)
     return v < 0 ? 0 : (v > rows ? (int)rows : v);
 }
 
+// a / b rounded up, for a up to 2^31 - 1
+__device__ __forceinline__ int quotient_up(int a, int b) { return (int)(((unsigned)a + (unsigned)b - 1u) / (unsigned)b); }
+
 __device__ __forceinline__ float act_value(int act, float z)
 {
     switch (act) {
@@ -142,7 +145,7 @@ struct Walk {
             t.c0 = (r - m * n_tiles) * a.columns;
             t.cols = min(a.columns, a.N - t.c0);
             t.k0 = bound[t.e];
-            t.nk = (max(0, bound[t.e + 1] - t.k0) + kTileK - 1) / kTileK;
+            t.nk = quotient_up(max(0, bound[t.e + 1] - t.k0), kTileK);
         } else {
             int lo = 0, hi = a.E;                        // the expert e with first_tile[e] <= tile < first_tile[e+1]
             while (hi - lo > 1) {
@@ -151,8 +154,8 @@ struct Walk {
             }
             t.e = lo;
             const int r = tile - first_tile[lo], begin = bound[lo], count = bound[lo + 1] - begin;
-            const int pieces = (count + a.columns - 1) / a.columns, m = r / pieces, piece = r - m * pieces;
-            const int width = ((count + pieces - 1) / pieces + kStep - 1) / kStep * kStep;   // equal pieces
+            const int pieces = quotient_up(count, a.columns), m = r / pieces, piece = r - m * pieces;
+            const int width = (quotient_up(count, pieces) + kStep - 1) / kStep * kStep;   // equal pieces
             t.m0 = m * kTileM * CG;
             t.c0 = begin + piece * width;
             t.cols = max(0, min(width, count - piece * width));
@@ -303,7 +306,7 @@ product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, c
         const int m_tiles = (a.M + kTileM * CG - 1) / (kTileM * CG);
         const int per = (a.E + kThreads - 1) / kThreads, from = min(a.E, (int)threadIdx.x * per), to = min(a.E, from + per);
         int sum = 0;
-        for (int e = from; e < to; ++e) sum += (max(0, bound[e + 1] - bound[e]) + a.columns - 1) / a.columns * m_tiles;
+        for (int e = from; e < to; ++e) sum += quotient_up(max(0, bound[e + 1] - bound[e]), a.columns) * m_tiles;
         int scan = sum;
         for (int d = 1; d < 32; d <<= 1) {
             const int v = __shfl_up_sync(kFullMask, scan, d);
@@ -315,7 +318,7 @@ product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, c
         for (int w = 0; w < warp; ++w) run += warp_sum[w];
         for (int e = from; e < to; ++e) {
             first_tile[e] = run;
-            run += (max(0, bound[e + 1] - bound[e]) + a.columns - 1) / a.columns * m_tiles;
+            run += quotient_up(max(0, bound[e + 1] - bound[e]), a.columns) * m_tiles;
         }
         if (threadIdx.x == kThreads - 1) first_tile[a.E] = run;
     }
@@ -364,7 +367,7 @@ product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, c
                     for (int b = 0; b < kAccColumns / CG / 64; ++b)
                         if (b < boxes) tma_load<CG>(sb + b * 8192, mb, c + b * 64, k, 0, full);
                 } else {
-                    int row = 0;
+                    unsigned row = 0;                                        // c + row may pass 2^31 - 1 where no row is left
                     if (CG == 1 && half >= 256) tma_load<CG>(sb, mb, k, c, 0, full), row = 128;
                     if (half - row >= 128) tma_load<CG>(sb + row * 128, mb, k, c + row, 0, full), row += 128;
 #pragma unroll

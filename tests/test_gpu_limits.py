@@ -1,4 +1,4 @@
-"""The ends of the documented ranges: token counts just below 2^31, where a rounded-up quotient in 32 bits would overflow."""
+"""The ends of the documented ranges: token and row counts just below 2^31, where a rounded-up quotient in 32 bits would overflow."""
 import pytest
 import torch
 
@@ -59,3 +59,22 @@ def test_most_tokens_on_some_experts():
     r = ep.ep_route(logits, ep.Router(17, 1, renormalize=False))
     assert all((p == 0).all() for p in _pieces(r.topk_idx))
     assert all(((p - 1 / 17).abs() < 1e-7).all() for p in _pieces(r.topk_weights))
+
+
+@pytest.mark.parametrize("cut", [[], [MOST - 300], [5, 2 ** 30, MOST - 1]], ids=str)
+def test_most_rows_of_the_experts_products(cut):
+    """2^31 - 1 rows of eight features, nearly all of them zero: every row is written, those next to the bounds are right."""
+    _room(75)
+    bounds = [0] + cut + [MOST]
+    E = len(bounds) - 1
+    x = torch.zeros(MOST, 8, dtype=torch.bfloat16, device="cuda")
+    y = torch.full((MOST, 8), 31.0, dtype=torch.bfloat16, device="cuda")
+    w = torch.stack([torch.eye(8) * (e + 2) for e in range(E)]).bfloat16().cuda()
+    marked = sorted({0, 1, 12345, 2 ** 30 + 7, MOST - 1, MOST - 2} | {b + d for b in cut for d in (-1, 0)})
+    for p in marked:
+        x[p] = torch.arange(8) + 1
+    ep.ep_expert_matmul(x, torch.tensor(bounds, dtype=torch.int32, device="cuda"), w, y=y)
+    for p in marked:
+        e = max(i for i in range(E) if bounds[i] <= p)
+        assert y[p].tolist() == [(e + 2.0) * (i + 1) for i in range(8)], p
+    assert sum(int(torch.count_nonzero(piece)) for piece in _pieces(y)) == 8 * len(marked)
