@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from dataclasses import dataclass, field
+from dataclasses import dataclass, fields
 
 import torch
 
@@ -489,7 +489,15 @@ class Router:
     renormalize: bool = True
     scale: float = 1.0
     balance_coef: float = 0.0
-    _structs: dict = field(default_factory=dict, init=False, repr=False, compare=False)   # by batch size and type
+
+    def __post_init__(self):
+        self.__setstate__(self.__getstate__())
+
+    def __getstate__(self):
+        return {f.name: getattr(self, f.name) for f in fields(self)}
+
+    def __setstate__(self, state):
+        self.__dict__.update(state, _structs={})          # the library's structs by batch size and type: no field, not copied
 
     def _struct(self, logits):
         """(a pointer to ep_router_t, T) for these logits."""
@@ -525,6 +533,9 @@ class Routing:
     def __setattr__(self, name, value):
         object.__setattr__(self, name, value)
         object.__setattr__(self, "_checked", None)
+
+    def __getstate__(self):
+        return dict(self.__dict__, _checked=None)
 
     def _args(self, T, E, K, device):
         """(topk_idx, topk_weights, a pointer to ep_balance_t or None, status, workspace, its bytes) as the library takes them.

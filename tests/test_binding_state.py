@@ -1,4 +1,8 @@
 """What the binding refuses, keeps and forgets, on the host alone."""
+import copy
+import dataclasses
+import pickle
+
 import pytest
 import torch
 
@@ -21,3 +25,32 @@ def test_tensors_on_another_device_than_the_current_one_are_refused(monkeypatch)
         ep._stream_of(_OnDevice(), _OnDevice(), None)
     monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1, raising=False)
     assert ep._stream_of(_OnDevice(), _OnDevice(), None) == 0
+
+
+@pytest.mark.parametrize("kind", ["copy", "deepcopy", "pickle", "asdict"])
+def test_a_router_that_was_used_can_be_copied_and_stored(kind):
+    """It is a description, kept in configurations and checkpoints; what a call remembers of it is not part of that."""
+    router = ep.Router(8, 2, scoring=ep.SCORE_SIGMOID, renormalize=False, scale=2.5, balance_coef=0.1)
+    router._struct(torch.zeros(4, 8))
+    if kind == "asdict":
+        fields = dataclasses.asdict(router)
+        assert fields == dict(num_experts=8, top_k=2, scoring=1, renormalize=False, scale=2.5, balance_coef=0.1)
+        other = ep.Router(**fields)
+    else:
+        other = {"copy": copy.copy, "deepcopy": copy.deepcopy, "pickle": lambda r: pickle.loads(pickle.dumps(r))}[kind](router)
+    assert other == router and hash(other) == hash(router) and repr(other) == repr(router)
+    st, T = other._struct(torch.zeros(5, 8))
+    assert T == st.contents.num_tokens == 5 and st.contents.scoring == 1 and router._struct(torch.zeros(4, 8))[0].contents.num_tokens == 4
+    assert dataclasses.replace(router, top_k=3)._struct(torch.zeros(4, 8))[0].contents.top_k == 3
+
+
+@pytest.mark.parametrize("kind", ["copy", "deepcopy", "pickle"])
+def test_a_routing_that_was_used_can_be_copied_and_stored(kind, monkeypatch):
+    monkeypatch.setattr(ep, "_on_device", lambda *a: None)
+    routing = ep.alloc_routing(4, 8, 2, balance=True, device="cpu")
+    first = routing._args(4, 8, 2, -1)
+    other = {"copy": copy.copy, "deepcopy": copy.deepcopy, "pickle": lambda r: pickle.loads(pickle.dumps(r))}[kind](routing)
+    args = other._args(4, 8, 2, -1)
+    assert args[0] == other.topk_idx.data_ptr() and args[3] == other.status.data_ptr()
+    assert (args[0] == first[0]) == (kind == "copy")
+    assert args[2].contents.loss == other.loss.data_ptr()
