@@ -184,6 +184,13 @@ def _on_device(device, *tensors):
             raise ValueError(f"the EP library needs its tensors on one CUDA device, got cuda:{device} and {t.device}")
 
 
+def _fit(*sizes):
+    """The library's structs hold 32-bit sizes and would cut larger ones."""
+    for n in sizes:
+        if n >= 1 << 31:
+            raise ValueError(f"the EP library takes sizes below 2^31, got {n}")
+
+
 def _stream_of(first, *others):
     """The current stream, as an address. All these tensors (or None) have to be on the current CUDA device, where the library launches."""
     device = first.get_device()
@@ -509,6 +516,7 @@ class Router:
         if st is None:
             if logits.dtype not in (torch.float32, torch.bfloat16):
                 raise TypeError(f"logits must be float32 or bfloat16, got {logits.dtype}")
+            _fit(shape[0], self.num_experts, self.top_k)
             if len(self._structs) >= 64:
                 self._structs.clear()
             st = ctypes.pointer(_Router(shape[0], self.num_experts, self.top_k,
@@ -560,6 +568,7 @@ class Routing:
 
 
 def ep_route_workspace_bytes(T, K, E) -> int:
+    _fit(T, E, K)
     return int(lib().ep_route_workspace_bytes(ctypes.byref(_Router(int(T), int(E), int(K), 0, 0, 0, 1.0, 0.0))))
 
 
@@ -624,6 +633,7 @@ def ep_route_backward(logits: torch.Tensor, router: Router, routing: Routing, d_
 def _matmul_args(rows, weight, expert_offsets, activation, operand_op):
     """(ep_matmul_t, rows, experts, out features, in features)"""
     E, N, H = weight.shape
+    _fit(E, N, H)
     return _Matmul(rows, H, N, E, activation, operand_op), E, N, H
 
 
@@ -653,6 +663,7 @@ class ExpertGrads:
 
 
 def ep_expert_matmul_backward_workspace_bytes(rows, in_features, out_features, num_experts) -> int:
+    _fit(in_features, out_features, num_experts)
     m = _Matmul(int(rows), int(in_features), int(out_features), int(num_experts), 0, 0)
     return int(lib().ep_expert_matmul_backward_workspace_bytes(ctypes.byref(m)))
 

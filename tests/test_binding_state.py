@@ -54,3 +54,19 @@ def test_a_routing_that_was_used_can_be_copied_and_stored(kind, monkeypatch):
     assert args[0] == other.topk_idx.data_ptr() and args[3] == other.status.data_ptr()
     assert (args[0] == first[0]) == (kind == "copy")
     assert args[2].contents.loss == other.loss.data_ptr()
+
+
+def test_sizes_past_31_bits_are_refused_not_cut():
+    """The library's structs hold 32-bit sizes: 2^32 + 16 tokens would arrive as 16."""
+    with pytest.raises(ValueError, match="2\\^31"):
+        ep.ep_route(torch.empty(2 ** 32 + 16, 1, device="meta"), ep.Router(1, 1), out=ep.alloc_routing(16, 1, 1, device="cpu"))
+    with pytest.raises(ValueError, match="2\\^31"):
+        ep.ep_route_workspace_bytes(16, 2, 2 ** 32 + 8)
+    x, off = torch.empty(4, 2 ** 32 + 8, dtype=torch.bfloat16, device="meta"), torch.zeros(2, dtype=torch.int32)
+    weight = torch.empty(1, 8, 2 ** 32 + 8, dtype=torch.bfloat16, device="meta")
+    with pytest.raises(ValueError, match="2\\^31"):
+        ep.ep_expert_matmul(x, off, weight, y=torch.empty(4, 8, dtype=torch.bfloat16, device="meta"))
+    with pytest.raises(ValueError, match="2\\^31"):
+        ep.ep_expert_matmul_backward(torch.empty(4, 8, dtype=torch.bfloat16, device="meta"), x, off, weight)
+    with pytest.raises(ValueError, match="2\\^31"):
+        ep.alloc_expert_grads(4, 2 ** 32 + 8, 8, 1, device="meta")
