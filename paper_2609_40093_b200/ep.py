@@ -547,12 +547,11 @@ class Routing:
 
     def _args(self, T, E, K, device):
         """(topk_idx, topk_weights, a pointer to ep_balance_t or None, status, workspace, its bytes) as the library takes them.
-        Types, shapes and devices are checked when a tensor is new or its memory has moved."""
-        tensors = (self.topk_idx, self.topk_weights, self.status, self.expert_counts, self.tokens, self.mean_probs, self.loss, self.workspace)
-        key = (T, E, K, device, *[None if t is None else t.data_ptr() for t in tensors])
+        Types, shapes and devices are checked when a tensor is new or its memory, extent or order has changed."""
         known = self._checked
-        if known is not None and known[0] == key:
-            return known[1]
+        if known is not None and known[0] == (T, E, K, device) and [f() for f in known[1]] == known[2]:
+            return known[3]
+        tensors = (self.topk_idx, self.topk_weights, self.status, self.expert_counts, self.tokens, self.mean_probs, self.loss, self.workspace)
         idx, w, status = (_at(self.topk_idx, (T, K), torch.int32, "topk_idx"), _at(self.topk_weights, (T, K), torch.float32, "topk_weights"),
                           _at(self.status, (1,), torch.int32, "status"))
         balance = None
@@ -563,7 +562,9 @@ class Routing:
         ws, nbytes = (None, 0) if self.workspace is None else (_ptr(self.workspace), self.workspace.numel() * self.workspace.element_size())
         _on_device(device, *tensors)
         args = (idx, w, balance, status, ws, nbytes)
-        object.__setattr__(self, "_checked", (key, args))
+        there = [t for t in tensors if t is not None]                # (one element: without it, no address)
+        probes = [t.data_ptr for t in there] + [t.numel for t in there if t.numel() > 1] + [t.is_contiguous for t in there if t.dim() > 1]
+        object.__setattr__(self, "_checked", ((T, E, K, device), probes, [f() for f in probes], args))
         return args
 
 

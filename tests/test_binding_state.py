@@ -70,3 +70,28 @@ def test_sizes_past_31_bits_are_refused_not_cut():
         ep.ep_expert_matmul_backward(torch.empty(4, 8, dtype=torch.bfloat16, device="meta"), x, off, weight)
     with pytest.raises(ValueError, match="2\\^31"):
         ep.alloc_expert_grads(4, 2 ** 32 + 8, 8, 1, device="meta")
+
+
+def test_a_routing_whose_tensors_changed_in_place_is_checked_again(monkeypatch):
+    """The memory may be the same and its extent or order another."""
+    monkeypatch.setattr(ep, "_on_device", lambda *a: None)
+
+    def checked():
+        r = ep.alloc_routing(4, 8, 4, balance=True, device="cpu")
+        r._args(4, 8, 4, -1)
+        r._args(4, 8, 4, -1)
+        return r
+
+    r = checked()
+    at = r.mean_probs.data_ptr()
+    r.mean_probs.resize_(4)
+    assert r.mean_probs.data_ptr() == at
+    with pytest.raises(ValueError, match="mean_probs"):
+        r._args(4, 8, 4, -1)
+    r = checked()
+    r.topk_idx.t_()
+    with pytest.raises(ValueError, match="contiguous"):
+        r._args(4, 8, 4, -1)
+    r = checked()
+    r.workspace.resize_(16)
+    assert r._args(4, 8, 4, -1)[5] == 16                        # the library refuses it
