@@ -1,8 +1,10 @@
-"""One mixture-of-experts layer, forward and backward, on the library's calls alone:
+"""One mixture-of-experts layer, forward and backward, on the library's calls:
 
     router -> layout + dispatch -> group -> gated experts -> combine        y = sum_k w_k W2_e( silu(Wg_e x) * (Wu_e x) )
 
-with the balance loss, and the gradients of the input, the router's logits and the experts' weights.
+with the balance loss, and the gradients of the input, the router's logits and the experts' weights. The router's projection, the
+gradient of the combine's weights and the sum of the two branches' gradients are torch, and part of the times. Nothing waits for the GPU,
+so that a step can be captured in a CUDA graph.
 
     python examples/moe_layer.py [--tokens 4096 --hidden 2048 --inner 1024 --experts 128 --top-k 8 --ranks 8 --steps 10]
 
@@ -56,10 +58,10 @@ class MoELayer:
         ep.ep_layout_dispatch(r.topk_idx, x, self.recv, E, R, lay, self.ws)
         ep.ep_group(self.recv, lay, self.x, E, R, status=lay.status)
         off = lay.expert_offsets
-        ep.ep_expert_matmul(self.x, off, self.w_up, y=self.up)
+        ep.ep_expert_matmul(self.x, off, self.w_up, y=self.up, status=lay.status)
         ep.ep_expert_matmul(self.x, off, self.w_gate, activation=ep.ACT_SILU, operand=self.up, operand_op=ep.OPERAND_MUL, y=self.hidden,
-                            pre=self.gate)
-        ep.ep_expert_matmul(self.hidden, off, self.w_down, y=self.out)
+                            pre=self.gate, status=lay.status)
+        ep.ep_expert_matmul(self.hidden, off, self.w_down, y=self.out, status=lay.status)
         return ep.ep_combine(self.out, lay.pair_slot, r.topk_weights, self.y, E, R, status=lay.status)
 
     def backward(self, dy, d_loss):
@@ -69,14 +71,14 @@ class MoELayer:
         slot = lay.pair_slot.long().clamp(min=0)
         valid = lay.pair_slot >= 0
         # combine: a pair's output row gets its token's gradient times its weight, its weight the product of the two rows
-        w_pair = torch.zeros(P, 1, device=dy.device)
-        w_pair[slot[valid]] = r.topk_weights[valid].unsqueeze(1)
-        d_out = ep.ep_combine(dy, lay.pair_token.view(P, 1), w_pair, torch.empty(P, H, dtype=torch.bfloat16, device=dy.device), 1, 1)
+        w_pair = torch.zeros(P + 1, 1, device=dy.device)                    # entries that name no pair go to the last one
+        w_pair[torch.where(valid, slot, P), 0] = r.topk_weights
+        d_out = ep.ep_combine(dy, lay.pair_token.view(P, 1), w_pair[:P], torch.empty(P, H, dtype=torch.bfloat16, device=dy.device), 1, 1)
         d_weights = torch.stack([(dy.float() * self.out[slot[:, k]].float()).sum(1) for k in range(K)], 1) * valid
-        down = ep.ep_expert_matmul_backward(d_out, self.hidden, off, self.w_down)
+        down = ep.ep_expert_matmul_backward(d_out, self.hidden, off, self.w_down, status=lay.status)
         gate = ep.ep_expert_matmul_backward(down.dx, self.x, off, self.w_gate, pre=self.gate, activation=ep.ACT_SILU, operand=self.up,
-                                            operand_op=ep.OPERAND_MUL, grads=ep.alloc_expert_grads(P, H, N, E, operand=True))
-        up = ep.ep_expert_matmul_backward(gate.doperand, self.x, off, self.w_up)
+                                            operand_op=ep.OPERAND_MUL, grads=ep.alloc_expert_grads(P, H, N, E, operand=True), status=lay.status)
+        up = ep.ep_expert_matmul_backward(gate.doperand, self.x, off, self.w_up, status=lay.status)
         # dispatch: a token's rows come back with unit weights, here from the pair space, once per branch
         dx = torch.empty_like(dy)
         ep.ep_combine(gate.dx, lay.pair_slot, self.ones, dx, E, R)
