@@ -563,11 +563,16 @@ int ep_route_backward(const ep_router_t *router, const void *logits, const int32
  * 0 and does not decrease. `rows` is the capacity of the row buffers; rows from
  * expert_offsets[num_experts] on are neither used nor written, whatever they hold;
  * an offset past `rows` is cut there and sets EP_STATUS_CAPACITY in *status
- * (device, may be NULL). Experts without rows cost nothing here.
+ * (device, may be NULL). Experts without rows cost nothing here. The launch is
+ * chosen from `rows`, which the host knows, not from the offsets: buffers far
+ * larger than the rows in use cost speed (one row in a buffer for 65536 takes the
+ * form for long segments), not correctness.
  * Limits: in_features and out_features multiples of 8, from 8 to 2^24 - 8;
  * 1 <= num_experts <= 4096; 0 <= rows < 2^31. y, pre and operand may not overlap
  * x or weight; operand may be y itself.
- * Waits inside the kernel are bounded: one that ran out sets EP_STATUS_TIMEOUT.
+ * Waits inside the kernel are bounded (some two seconds): one that ran out sets
+ * EP_STATUS_TIMEOUT and leaves the results incomplete, of which a call without a
+ * status word says nothing. The same holds for the gradients.
  */
 enum { EP_ACT_NONE = 0, EP_ACT_RELU = 1, EP_ACT_SILU = 2, EP_ACT_GELU = 3 };
 enum { EP_OPERAND_ADD = 0, EP_OPERAND_MUL = 1 };

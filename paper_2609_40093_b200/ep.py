@@ -641,7 +641,8 @@ def _matmul_args(rows, weight, expert_offsets, activation, operand_op):
 def ep_expert_matmul(x, expert_offsets, weight, bias=None, activation=ACT_NONE, operand=None, operand_op=OPERAND_ADD, y=None,
                      pre=None, status=None):
     """y[p] = act(x[p] weight[e]^T + bias[e]) (+ or *) operand[p] for the rows p of expert e's segment of the pair space.
-    x [rows, in], weight [experts, out, in], bias [experts, out], operand, y and pre [rows, out], all bf16."""
+    x [rows, in], weight [experts, out, in], bias [experts, out], operand, y and pre [rows, out], all bf16. What cuts the result short (offsets
+    past the buffers, a wait inside the kernel that ran out) is reported in `status` alone: pass one and look at it with `ep_status`."""
     bf, P = torch.bfloat16, x.shape[0]
     m, E, N, H = _matmul_args(P, weight, expert_offsets, activation, operand_op)
     if y is None:
