@@ -5,9 +5,9 @@
 //   dweight   dW[e] = sum_p dz[p]^T x[p]
 //
 // All three are one kernel. The accumulator's 128 lanes hold the axis that is contiguous in the result (features), its
-// columns hold the other one (rows p, or the weight's out features), so a warp stores 32 neighbouring elements of a result
-// row per column, and the ragged axis of a segment, the rows, is cut in steps of 16 columns: an expert that got one row
-// costs a 16-column product, not one of 128 rows.
+// columns hold the other one (rows p, or the weight's out features), so that a column is a run of neighbouring elements of a
+// result row, and the ragged axis of a segment, the rows, is cut in steps of 16 columns: an expert that got one row costs a
+// 16-column product, not one of 128 rows.
 //
 //   mode      lanes (M)       columns (N)     contracted (K)   lane operand             column operand
 //   forward   out features    rows            in features      W, K-major               x, K-major
@@ -18,7 +18,7 @@
 // tile, each with a part of the contracted axis, and add their accumulators through each other's shared memory in a fixed order.
 //
 // One persistent CTA per SM. A warp keeps a ring of shared-memory stages full by TMA (64 of the contracted axis each), one
-// thread issues the products, four warps empty the accumulators, of which there are two of 256 columns, so that a tile's
+// thread issues the products, eight warps empty the accumulators, of which there are two of 256 columns, so that a tile's
 // epilogue runs under the next tile's products. Rows behind a segment's end that a box brings along only feed columns that
 // are not stored; in the dweight mode, where the rows are contracted, the operands are read through tensor maps that end
 // with the segment (one pair per expert, made on the device from the offsets), so that the rest of the last box is zero
@@ -83,6 +83,10 @@ __device__ __forceinline__ int segment_bound(int32_t v, long long rows)
 // a / b rounded up, for a up to 2^31 - 1
 __device__ __forceinline__ int quotient_up(int a, int b) { return (int)(((unsigned)a + (unsigned)b - 1u) / (unsigned)b); }
 
+// Activations by the fast exponential and division: errors of 2 + 1.16 |z| units in the last place of fp32 where the exponential
+// decides (z < 0), some 2^-20 for |z| up to 8, far below the rounding to bf16 of y, dz and doperand; dbias, a sum in fp32, sees it. expf
+// and an exact division cost: forward of 65536 rows through four experts of 512 x 512, silu, 100 us instead of 50; dz, doperand and dbias of
+// 32768 rows of 1024 features, silu and a multiplied operand, 81 instead of 61.
 __device__ __forceinline__ float act_value(int act, float z)
 {
     switch (act) {
@@ -601,8 +605,9 @@ segment_maps_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
 }
 
 // ---- dz = dy * (operand) * act'(pre), doperand = dy * act(pre), and the partial sums of dbias -------------------------
-// A warp owns 256 columns (8 a lane) and a run of rows; three 16-byte loads and one or two 16-byte stores per row and lane,
-// bound by memory. A run is cut where a segment ends: chunk c and expert e share at most one piece, and c + e grows along
+// A warp owns 256 columns (8 a lane) and a run of rows; three 16-byte loads and one or two 16-byte stores per row and lane:
+// bound by memory, with gelu by instruction issue (erff). 32768 rows of 1024 features, silu and a multiplied operand, doperand and dbias:
+// 61 us with the sums' kernel, the bytes take 41; 32768 of 2048, gelu, dbias alone: 120 and 41. A run is cut where a segment ends: chunk c and expert e share at most one piece, and c + e grows along
 // the rows, so it numbers the pieces; their sums go to partial[c + e] and the second kernel adds an expert's pieces in
 // their order (no atomics: the same bits every time).
 
@@ -639,7 +644,6 @@ slope_kernel(const SlopeArgs a)
         e = lo;
     }
     const bool live = vec < a.vecs;
-    constexpr int kRows = 1;
     while (p < end) {
         long long stop = end;
         if (a.partial) {
@@ -648,36 +652,27 @@ slope_kernel(const SlopeArgs a)
             stop = min(end, (long long)next);
         }
         float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        for (; p < stop; p += kRows) {
-            uint4 g[kRows], z[kRows], r[kRows];
+        for (; live && p < stop; ++p) {
+            const size_t at = (size_t)p * a.vecs + vec;
+            uint4 z = make_uint4(0u, 0u, 0u, 0u), r = z;
+            const uint4 g = ld_stream(a.dy + at);
+            if (ACT != EP_ACT_NONE || a.doperand) z = ld_stream(a.pre + at);
+            if (a.operand) r = ld_stream(a.operand + at);
+            float fg[8], fz[8], fr[8], o[8];
+            unpack8(g, fg);
+            unpack8(z, fz);
+            unpack8(r, fr);
 #pragma unroll
-            for (int i = 0; i < kRows; ++i)
-                if (live && p + i < stop) {
-                    const size_t at = (size_t)(p + i) * a.vecs + vec;
-                    g[i] = ld_stream(a.dy + at);
-                    if (ACT != EP_ACT_NONE || a.doperand) z[i] = ld_stream(a.pre + at);
-                    if (a.operand) r[i] = ld_stream(a.operand + at);
-                }
-#pragma unroll
-            for (int i = 0; i < kRows; ++i)
-                if (live && p + i < stop) {
-                    const size_t at = (size_t)(p + i) * a.vecs + vec;
-                    float fg[8], fz[8], fr[8], o[8];
-                    unpack8(g[i], fg);
-                    if (ACT != EP_ACT_NONE || a.doperand) unpack8(z[i], fz);
-                    if (a.operand) unpack8(r[i], fr);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        float value = 0.f, slope = 1.f;
-                        if (ACT != EP_ACT_NONE || a.doperand) act_both(ACT, fz[j], value, slope);
-                        o[j] = fg[j] * value;
-                        if (a.operand) fg[j] *= fr[j];
-                        fg[j] *= slope;
-                        sum[j] += fg[j];
-                    }
-                    if (a.doperand) st_stream(a.doperand + at, pack8(o));
-                    if (a.dz) a.dz[at] = pack8(fg);
-                }
+            for (int j = 0; j < 8; ++j) {
+                float value = 0.f, slope = 1.f;
+                if (ACT != EP_ACT_NONE || a.doperand) act_both(ACT, fz[j], value, slope);
+                o[j] = fg[j] * value;
+                if (a.operand) fg[j] *= fr[j];
+                fg[j] *= slope;
+                sum[j] += fg[j];
+            }
+            if (a.doperand) st_stream(a.doperand + at, pack8(o));
+            if (a.dz) a.dz[at] = pack8(fg);
         }
         p = stop;
         if (a.partial && live) {
@@ -810,7 +805,6 @@ int row_columns(int64_t rows, int E)
     return c;
 }
 
-
 template <int MODE>
 int launch_rows(const ProductArgs &a, const CUtensorMap &map_a, const ColumnMaps &map_b, cudaStream_t stream)
 {
@@ -838,7 +832,6 @@ size_t partial_bytes(const ep_matmul_t &m)
     return up256((chunks + m.num_experts) * (size_t)m.out_features * 4);
 }
 size_t dz_bytes(const ep_matmul_t &m) { return up256((size_t)m.rows * m.out_features * 2); }
-
 
 }  // namespace
 
@@ -979,7 +972,7 @@ extern "C" int ep_expert_matmul_backward(const ep_matmul_t *m, const void *dy, c
         a.M = m->in_features, a.K = m->out_features, a.N = 0;
         a.out = static_cast<uint16_t *>(dx);
         a.columns = row_columns(m->rows, m->num_experts);
-            rc = launch_rows<kDx>(a, map_a, map_b, stream);
+        rc = launch_rows<kDx>(a, map_a, map_b, stream);
         if (rc != EP_OK) return rc;
     }
     if (dweight) {

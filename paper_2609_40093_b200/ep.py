@@ -631,8 +631,8 @@ def ep_route_backward(logits: torch.Tensor, router: Router, routing: Routing, d_
     return dlogits
 
 
-def _matmul_args(rows, weight, expert_offsets, activation, operand_op):
-    """(ep_matmul_t, rows, experts, out features, in features)"""
+def _matmul_args(rows, weight, activation, operand_op):
+    """(ep_matmul_t, experts, out features, in features)"""
     E, N, H = weight.shape
     _fit(E, N, H)
     return _Matmul(rows, H, N, E, activation, operand_op), E, N, H
@@ -644,7 +644,7 @@ def ep_expert_matmul(x, expert_offsets, weight, bias=None, activation=ACT_NONE, 
     x [rows, in], weight [experts, out, in], bias [experts, out], operand, y and pre [rows, out], all bf16. What cuts the result short (offsets
     past the buffers, a wait inside the kernel that ran out) is reported in `status` alone: pass one and look at it with `ep_status`."""
     bf, P = torch.bfloat16, x.shape[0]
-    m, E, N, H = _matmul_args(P, weight, expert_offsets, activation, operand_op)
+    m, E, N, H = _matmul_args(P, weight, activation, operand_op)
     if y is None:
         y = torch.empty(P, N, dtype=bf, device=x.device)
     _check(lib().ep_expert_matmul(ctypes.byref(m), _at(x, (P, H), bf, "x"), _at(expert_offsets, (E + 1,), torch.int32, "expert_offsets"),
@@ -686,7 +686,7 @@ def ep_expert_matmul_backward(dy, x, expert_offsets, weight, pre=None, activatio
     """The gradients of `ep_expert_matmul` for dy, written to the tensors that `grads` has (default: dx and dweight).
     `pre` is what the forward call wrote; the gradient of an added operand is dy itself."""
     bf, P = torch.bfloat16, dy.shape[0]
-    m, E, N, H = _matmul_args(P, weight, expert_offsets, activation, operand_op)
+    m, E, N, H = _matmul_args(P, weight, activation, operand_op)
     if grads is None:
         grads = alloc_expert_grads(P, H, N, E, device=dy.device)
     _check(lib().ep_expert_matmul_backward(
