@@ -513,8 +513,8 @@ route_kernel(const RouteArgs a)
 // ---- few experts -------------------------------------------------------------------------------------------------
 // Up to 16 experts and many tokens: a thread per token, its row in registers, the picks by plain scans over them. A warp per token
 // leaves most lanes idle there, but its chain is shorter: us with a warp -> a thread per token, forward / with the loss / gradient,
-//   8 experts, top 2:    4096 tokens 2.8 -> 2.4 / 6.6 -> 7.5 / 3.8 -> 3.6     16384 5.8 -> 2.4 / 10.9 -> 7.7 / 8.0 -> 3.7
-//   16, sigmoid + bias, top 8: 16384 7.8 -> 9.0 / 13.2 -> 20.8 / 7.8 -> 7.7   65536 24.9 -> 11.6 / 32.2 -> 23.3 / 22.4 -> 9.8
+//   8 experts, top 2:    4096 tokens 2.8 -> 2.4 / 7.1 -> 7.7 / 3.8 -> 3.8     16384 6.0 -> 2.6 / 11.7 -> 7.8 / 8.1 -> 3.8
+//   16, sigmoid + bias, top 8: 16384 8.1 -> 9.1 / 14.1 -> 20.8 / 8.1 -> 7.5   65536 25.9 -> 12.7 / 34.4 -> 23.5 / 23.4 -> 9.5
 // hence from 2048 tokens per expert on.
 
 constexpr int kFew = 16, kFewWarps = 8, kFewCtas = 4 * 148;
