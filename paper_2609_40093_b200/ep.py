@@ -498,13 +498,13 @@ class Router:
     balance_coef: float = 0.0
 
     def __post_init__(self):
-        self.__setstate__(self.__getstate__())
+        self.__dict__["_structs"] = {}                     # the library's structs by batch size and type: no field, not copied
 
     def __getstate__(self):
         return {f.name: getattr(self, f.name) for f in fields(self)}
 
     def __setstate__(self, state):
-        self.__dict__.update(state, _structs={})          # the library's structs by batch size and type: no field, not copied
+        self.__dict__.update(state, _structs={})
 
     def _struct(self, logits):
         """(a pointer to ep_router_t, T) for these logits."""
