@@ -557,7 +557,7 @@ int ep_route_backward(const ep_router_t *router, const void *logits, const int32
  * bf16(z), which the gradient of an activation needs. Sums, bias, activation and
  * operand are fp32, one rounding to bf16 at the end. A gated expert is two calls:
  * u = x Wu^T, then silu(x Wg^T) * u with operand = u, EP_OPERAND_MUL.
- * EP_ACT_GELU is z * Phi(z) (the error-function form).
+ * EP_ACT_GELU is z * Phi(z) (the error-function form, Phi to 2^-24 absolute).
  *
  * expert_offsets [num_experts+1] (device, int32) is ep_layout's array: it starts at
  * 0 and does not decrease. `rows` is the capacity of the row buffers; rows from
