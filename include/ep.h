@@ -608,6 +608,122 @@ int ep_expert_matmul_backward(const ep_matmul_t *m, const void *dy, const void *
                               float *dbias, void *doperand, int32_t *status, void *workspace,
                               size_t workspace_bytes, void *stream);
 
+/*
+ * Rows sorted by expert and back, with weights, as a training step needs them (Section 2.1:
+ * dispatch takes a token's activation to its experts, combine sums what they give back;
+ * these are the same movements with their gradients). `slot` [T][K] (device, int32) is
+ * pair_slot, or recv_slot where the row buffer is a receive buffer; entries below 0 are
+ * skipped. num_experts and num_ranks of the shape take no part (1 and 1 will do). Row
+ * buffers are bf16 and 16-byte aligned, weights fp32 [T][K]. Sums are fp32 in ascending k
+ * with one rounding at the end. Rows of a buffer that no slot names are not touched; a
+ * slot past the buffer is skipped (its d_weights are 0) and sets EP_STATUS_CAPACITY in
+ * *status (device, may be NULL).
+ *
+ *   ep_sort           sorted[slot[t][k]] = bf16( weights[t][k] * x[t] )
+ *                     without weights (NULL): x[t] bit for bit, as ep_dispatch
+ *   ep_sort_backward  dx[t] = bf16( add[t] + sum_k weights[t][k] * d_sorted[slot[t][k]] )
+ *                     d_weights[t][k] = sum_h x[t][h] * d_sorted[slot[t][k]][h]
+ *                     add [T][H] may be NULL, or dx itself. dx or d_weights may be NULL
+ *                     and is then not computed; d_weights needs weights and x.
+ *   ep_combine_residual   y[t] = bf16( residual[t] + drop( sum_k w[t][k] * out[slot[t][k]] ) )
+ *                     residual and dropout may be NULL; residual may be y itself. With
+ *                     neither, it is ep_combine.
+ *   ep_combine_backward   with g = drop(dy), the drop of the forward call (same dropout):
+ *                     d_out[slot[t][k]] = bf16( w[t][k] * g[t] )
+ *                     d_weights[t][k] = sum_h g[t][h] * out[slot[t][k]][h]
+ *                     d_out or d_weights may be NULL; d_out may be `out` itself. The
+ *                     gradient of residual is dy.
+ * Where several picks of a token name one row (recv_slot), the row's weight is the sum of
+ * theirs; without weights it counts once, as dispatch stores it once. Different tokens
+ * never share a row.
+ */
+typedef struct {
+    const uint64_t *state; /* device, 8-byte aligned: [0] seed, [1] step (its low 32 bits count) */
+    double p;              /* 0 <= p <= 1, taken to the nearest multiple of 2^-16 */
+    uint32_t site;         /* tells the uses of one state apart */
+} ep_dropout_t;
+int ep_sort(const ep_shape_t *shape, const void *x, const int32_t *slot, const float *weights, void *sorted,
+            int64_t sorted_rows, int32_t *status, void *stream);
+int ep_sort_backward(const ep_shape_t *shape, const void *d_sorted, int64_t sorted_rows, const int32_t *slot,
+                     const float *weights, const void *x, const void *add, void *dx, float *d_weights,
+                     int32_t *status, void *stream);
+int ep_combine_residual(const ep_shape_t *shape, const void *out, int64_t out_rows, const int32_t *slot,
+                        const float *topk_weights, const void *residual, const ep_dropout_t *dropout, void *y,
+                        int32_t *status, void *stream);
+int ep_combine_backward(const ep_shape_t *shape, const void *dy, const void *out, int64_t out_rows,
+                        const int32_t *slot, const float *topk_weights, const ep_dropout_t *dropout, void *d_out,
+                        float *d_weights, int32_t *status, void *stream);
+
+/*
+ * Dropout without a stored mask: y = bf16( residual + drop(x) ) over [rows][cols] bf16
+ * (cols a multiple of 8, rows < 2^31), residual may be NULL. limit (device, int32, may be
+ * NULL): rows from *limit on are neither read nor written (expert_offsets + num_experts
+ * for rows of the pair space). x, residual and y may be the same buffer. The gradient of x
+ * is the same call on dy, without residual.
+ *   drop(v)  0 where the element's 16 random bits are below round(65536 p), whatever v is;
+ *            v / (1 - round(65536 p) / 65536) elsewhere
+ * The bits are Philox4x32-10 (Salmon et al. 2011): elements 8 v .. 8 v + 7 of the row-major
+ * array share the call with counter (low word of v, high word of v, step, site) and key
+ * (low, high word of seed), and take the low and high half of its first word, of its
+ * second, and so on. seed and step are read when the kernel runs, so that the replays of a
+ * captured graph take what is there then; the backward call has to find what its forward
+ * call found.
+ */
+int ep_dropout(const void *x, const void *residual, void *y, int64_t rows, int32_t cols, const int32_t *limit,
+               const ep_dropout_t *dropout, void *stream);
+
+/*
+ * Low-rank adapters of many requests beside a shared projection:
+ *   mid[i] = bf16( x[row] down[a]^T )
+ *   y[row] = bf16( base[row] + scale[a] * mid[i] up[a]^T )       row = row_index[i]
+ * for the entries i of adapter a, adapter_offsets[a] <= i < adapter_offsets[a+1]. x
+ * [rows][in_features], down [num_adapters][rank][in_features], up
+ * [num_adapters][out_features][rank], base and y [rows][out_features], mid
+ * [entries][rank], all bf16 and 16-byte aligned; scale [num_adapters] fp32 (NULL: 1).
+ * base, what the shared projection gave, may be y itself; NULL: nothing is added. mid may
+ * be NULL (needed by the gradients); y may be NULL where mid is not. mid is rounded before the second product,
+ * whose operand it is; sums are fp32.
+ *
+ * The entries: a batch whose row t asks for adapter ids[t] (-1: none) is laid out by
+ * ep_layout with top_k = 1, E adapters and one rank, once for all projections of a step:
+ * adapter_offsets = expert_offsets, row_index = pair_token. row_index NULL: entry i is row
+ * i, as in the pair space, where adapter_offsets = expert_offsets gives every expert an
+ * adapter of its own. adapter_offsets [num_adapters+1] starts at 0 and does not decrease;
+ * an offset past `entries` is cut there and sets EP_STATUS_CAPACITY. Entries from
+ * adapter_offsets[num_adapters] on are not used, and rows that no entry names not
+ * touched. A row outside [0, rows) is skipped (its mid is 0) with EP_STATUS_BAD_INDEX. An
+ * entry list that names a row twice loses one of the two sums.
+ * Limits: in_features and out_features multiples of 8, from 8 to 2^24 - 8; rank a multiple
+ * of 8, from 8 to 128; 1 <= num_adapters <= 4096; rows, entries < 2^31; entries <= rows
+ * without row_index. y, mid may not overlap x or weights. Waits inside the kernels are
+ * bounded, as those of ep_expert_matmul (EP_STATUS_TIMEOUT).
+ *
+ * Gradients, for dy [rows][out_features]:
+ *   dmid = scale[a] * dy[row] up[a]                 dx[row] = bf16( base[row] + dmid down[a] )
+ *   ddown[a] = sum dmid[i]^T x[row]                 dup[a] = scale[a] * sum dy[row]^T mid[i]
+ * bf16, the shapes of x, down and up; each may be NULL and is then not computed. base
+ * [rows][in_features], what else dx is made of, may be dx itself or NULL. dmid is rounded
+ * to bf16 once. Adapters without entries get zero ddown and dup. No atomics: the same bits
+ * every time. workspace (for ddown alone): ep_adapter_matmul_backward_workspace_bytes()
+ * bytes (device, 256-byte aligned), uninitialised.
+ */
+typedef struct {
+    int64_t rows;    /* of x, base and y */
+    int64_t entries; /* of row_index and mid */
+    int32_t in_features;
+    int32_t out_features;
+    int32_t rank;
+    int32_t num_adapters;
+} ep_adapter_t;
+int ep_adapter_matmul(const ep_adapter_t *m, const void *x, const int32_t *adapter_offsets, const int32_t *row_index,
+                      const void *down, const void *up, const float *scale, const void *base, void *y, void *mid,
+                      int32_t *status, void *stream);
+size_t ep_adapter_matmul_backward_workspace_bytes(const ep_adapter_t *m);
+int ep_adapter_matmul_backward(const ep_adapter_t *m, const void *dy, const void *x, const int32_t *adapter_offsets,
+                               const int32_t *row_index, const void *down, const void *up, const float *scale,
+                               const void *mid, const void *base, void *dx, void *ddown, void *dup, int32_t *status,
+                               void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,431 @@
+// Rows sorted by expert and back with weights, as a training step needs them: ep_sort, ep_sort_backward, ep_combine_residual,
+// ep_combine_backward; and ep_dropout. Two row kernels, each the other's gradient:
+//
+//   spread   dst[slot[t][k]] = w[t][k] * v[t]                       d[t][k] = <v[t], table[slot[t][k]]>
+//            (ep_sort: v = x, no d; ep_combine_backward: v = drop(dy), table = out)
+//   gather   y[t] = add[t] + drop(sum_k w[t][k] * table[slot[t][k]])       d[t][k] = <v[t], table[slot[t][k]]>
+//            (ep_combine_residual: no d; ep_sort_backward: v = x, no drop)
+//
+// A group of G threads (32, 64 or 128) owns a token, a thread 16-byte columns of it. Every row named is read once and the
+// products for d are taken on the way. Sums are fp32 in ascending k; a d is the sum of a thread's columns, then of the group's
+// threads in a fixed tree: the same bits every time. Slots and weights sit one per lane and travel by warp shuffle.
+#include <cmath>
+
+#include "ep_random.cuh"
+
+namespace ep {
+namespace {
+
+constexpr int kBlock = 128;
+constexpr int kChunk = 8;   // rows in flight per column
+
+struct RowArgs {
+    const uint4 *v;             // [T] rows
+    const uint4 *add;           // gather: [T] rows, may be NULL
+    const uint4 *table;         // rows by slot
+    uint4 *out;                 // spread: rows by slot; gather: [T] rows
+    long long rows;             // of the table, or the destination
+    const int32_t *slot;
+    const float *weights;       // NULL: unit weights, a row that several picks name counts once
+    float *dots;
+    int T, K, vec_per_row;
+    int32_t *status;
+    DropoutArgs drop;
+};
+
+// 16 bytes that nothing else will read; the destination may be the same memory, so not through the read-only path.
+__device__ __forceinline__ uint4 ld_once(const uint4 *p)
+{
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ void unpack8(const uint4 &v, float (&f)[8])
+{
+    f[0] = bf16_lo(v.x), f[1] = bf16_hi(v.x), f[2] = bf16_lo(v.y), f[3] = bf16_hi(v.y);
+    f[4] = bf16_lo(v.z), f[5] = bf16_hi(v.z), f[6] = bf16_lo(v.w), f[7] = bf16_hi(v.w);
+}
+__device__ __forceinline__ uint4 pack8(const float (&f)[8])
+{
+    return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
+}
+
+// Sums of eight values over a warp, nine shuffles: lane l returns the sum of value (l >> 2).
+__device__ __forceinline__ float warp_sums8(float (&d)[8])
+{
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float give = lane & 16 ? d[i] : d[i + 4], keep = lane & 16 ? d[i + 4] : d[i];
+        d[i] = keep + __shfl_xor_sync(kFullMask, give, 16);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const float give = lane & 8 ? d[i] : d[i + 2], keep = lane & 8 ? d[i + 2] : d[i];
+        d[i] = keep + __shfl_xor_sync(kFullMask, give, 8);
+    }
+    const float give = lane & 4 ? d[0] : d[1], keep = lane & 4 ? d[1] : d[0];
+    float s = keep + __shfl_xor_sync(kFullMask, give, 4);
+    s += __shfl_xor_sync(kFullMask, s, 2);
+    return s + __shfl_xor_sync(kFullMask, s, 1);
+}
+
+// A token's picks, one per lane.
+struct Picks {
+    int32_t slot;               // -1: nothing to read or write
+    float w;
+    int first;                  // the lowest pick that names the same row
+    unsigned mask;              // the picks whose row is visited: those that are their row's first
+};
+
+// SHARED_ONCE: a row that several picks name is visited once, with the sum of their weights (in ascending k).
+template <bool SHARED_ONCE>
+__device__ __forceinline__ Picks load_picks(const RowArgs &a, int t)
+{
+    const int lane = threadIdx.x & 31;
+    Picks p;
+    p.slot = -1, p.w = 0.f;
+    if (t < a.T && lane < a.K) {
+        p.slot = __ldg(a.slot + (size_t)t * a.K + lane);
+        p.w = a.weights ? __ldg(a.weights + (size_t)t * a.K + lane) : 1.f;
+        if (p.slot >= a.rows) {
+            if (a.status) atomicOr(a.status, EP_STATUS_CAPACITY);
+            p.slot = -1;
+        }
+        if (p.slot < 0) p.slot = -1, p.w = 0.f;
+    }
+    const unsigned same = __match_any_sync(kFullMask, p.slot);
+    p.first = __ffs(same) - 1;
+    if (SHARED_ONCE && a.weights && __any_sync(kFullMask, p.slot >= 0 && p.first != lane)) {
+        float sum = 0.f;
+        for (int k = 0; k < a.K; ++k) {
+            const float w = __shfl_sync(kFullMask, p.w, k);
+            if ((same >> k) & 1u) sum += w;
+        }
+        p.w = sum;
+    }
+    const bool visit = p.slot >= 0 && (p.first == lane || !(SHARED_ONCE || !a.weights));
+    p.mask = __ballot_sync(kFullMask, visit);
+    return p;
+}
+
+// d[t][k] from the threads' partial sums: over the warp, then over the group's warps.
+template <int G, int CHUNKS, bool SHARED_ONCE>
+__device__ __forceinline__ void store_dots(const RowArgs &a, const Picks &p, float (&dot)[CHUNKS][kChunk], int t)
+{
+    __shared__ float part[kBlock / 32][CHUNKS * kChunk];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) {
+        const float s = warp_sums8(dot[c]);
+        if ((lane & 3) == 0) part[warp][c * kChunk + (lane >> 2)] = s;
+    }
+    if (G > 32) __syncthreads(); else __syncwarp();
+    const int g = threadIdx.x % G, w0 = warp - g / 32;
+    if (t < a.T && g < a.K) {                                            // the group's first warp: its lanes hold the picks
+        const int from = SHARED_ONCE ? p.first : g;
+        float s = 0.f;
+#pragma unroll
+        for (int w = 0; w < G / 32; ++w) s += part[w0 + w][from];
+        a.dots[(size_t)t * a.K + g] = p.slot < 0 ? 0.f : s;
+    }
+}
+
+template <int G, int CHUNKS, bool DOTS>
+__global__ void __launch_bounds__(kBlock)
+spread_rows_kernel(const RowArgs a)
+{
+    const int g = threadIdx.x % G, t = blockIdx.x * (kBlock / G) + threadIdx.x / G;
+    pdl_wait();                                                          // nothing is read or written before this
+    const Picks p = load_picks<true>(a, t);
+    const Dropout drop(a.drop);
+    const bool copy = !a.weights && !a.drop.state;
+    float dot[CHUNKS][kChunk];
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+        for (int j = 0; j < kChunk; ++j) dot[c][j] = 0.f;
+
+    if (p.mask)
+        for (int base = 0; base < a.vec_per_row; base += G) {            // trip count uniform over the warp
+            const int col = base + g;
+            const bool live = col < a.vec_per_row;
+            uint4 mine = make_uint4(0u, 0u, 0u, 0u);
+            if (live) mine = ld_once(a.v + (size_t)t * a.vec_per_row + col);
+            uint4 row[kChunk];
+            const auto request = [&](int c) {
+#pragma unroll
+                for (int j = 0; j < kChunk; ++j) {
+                    const int32_t s = __shfl_sync(kFullMask, p.slot, c * kChunk + j);
+                    if (live && ((p.mask >> (c * kChunk + j)) & 1u)) row[j] = ld_once(a.table + (size_t)s * a.vec_per_row + col);
+                }
+            };
+            if (DOTS) request(0);
+            float f[8];
+            unpack8(mine, f);
+            if (a.drop.state) drop.apply(f, (size_t)t * a.vec_per_row + col);
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c) {
+                if (DOTS && c > 0) request(c);
+#pragma unroll
+                for (int j = 0; j < kChunk; ++j) {
+                    const int k = c * kChunk + j;
+                    const int32_t s = __shfl_sync(kFullMask, p.slot, k);
+                    const float w = __shfl_sync(kFullMask, p.w, k);
+                    if (live && ((p.mask >> k) & 1u)) {
+                        if (DOTS) {
+                            float r[8];
+                            unpack8(row[j], r);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) dot[c][j] = fmaf(f[i], r[i], dot[c][j]);
+                        }
+                        float o[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) o[i] = w * f[i];
+                        if (a.out) st_stream(a.out + (size_t)s * a.vec_per_row + col, copy ? mine : pack8(o));
+                    }
+                }
+            }
+        }
+    if (DOTS) store_dots<G, CHUNKS, true>(a, p, dot, t);
+}
+
+template <int G, int CHUNKS, bool DOTS>
+__global__ void __launch_bounds__(kBlock)
+gather_rows_kernel(const RowArgs a)
+{
+    const int g = threadIdx.x % G, t = blockIdx.x * (kBlock / G) + threadIdx.x / G;
+    pdl_wait();
+    const Picks p = load_picks<false>(a, t);
+    const Dropout drop(a.drop);
+    float dot[CHUNKS][kChunk];
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+        for (int j = 0; j < kChunk; ++j) dot[c][j] = 0.f;
+
+    if (t < a.T)
+        for (int base = 0; base < a.vec_per_row; base += G) {
+            const int col = base + g;
+            const bool live = col < a.vec_per_row;
+            const size_t at = (size_t)t * a.vec_per_row + col;
+            uint4 mine = make_uint4(0u, 0u, 0u, 0u), add = mine;
+            float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c) {
+                uint4 row[kChunk];
+#pragma unroll
+                for (int j = 0; j < kChunk; ++j) {
+                    const int32_t s = __shfl_sync(kFullMask, p.slot, c * kChunk + j);
+                    if (live && ((p.mask >> (c * kChunk + j)) & 1u)) row[j] = ld_once(a.table + (size_t)s * a.vec_per_row + col);
+                }
+                if (c == 0 && live) {
+                    if (DOTS) mine = ld_once(a.v + at);
+                    if (a.add) add = ld_once(a.add + at);
+                }
+                float f[8];
+                if (DOTS) unpack8(mine, f);
+#pragma unroll
+                for (int j = 0; j < kChunk; ++j) {
+                    const int k = c * kChunk + j;
+                    const float w = __shfl_sync(kFullMask, p.w, k);
+                    if (live && ((p.mask >> k) & 1u)) {
+                        float r[8];
+                        unpack8(row[j], r);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            acc[i] = fmaf(w, r[i], acc[i]);
+                            if (DOTS) dot[c][j] = fmaf(f[i], r[i], dot[c][j]);
+                        }
+                    }
+                }
+            }
+            if (live && a.out) {
+                if (a.drop.state) drop.apply(acc, at);
+                if (a.add) {
+                    float r[8];
+                    unpack8(add, r);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) acc[i] += r[i];
+                }
+                st_stream(a.out + at, pack8(acc));
+            }
+        }
+    if (DOTS) store_dots<G, CHUNKS, false>(a, p, dot, t);
+}
+
+template <template <int, int, bool> class Kernel, int CHUNKS, bool DOTS>
+int launch_group(const RowArgs &a, cudaStream_t stream)
+{
+    const int vpr = a.vec_per_row;
+    cudaError_t e;
+    if (vpr <= 64)
+        e = launch_pdl(Kernel<32, CHUNKS, DOTS>::get(), dim3(ceil_div(a.T, kBlock / 32)), dim3(kBlock), 0, stream, a);
+    else if (vpr <= 256)
+        e = launch_pdl(Kernel<64, CHUNKS, DOTS>::get(), dim3(ceil_div(a.T, kBlock / 64)), dim3(kBlock), 0, stream, a);
+    else
+        e = launch_pdl(Kernel<128, CHUNKS, DOTS>::get(), dim3(a.T), dim3(kBlock), 0, stream, a);
+    EP_CUDA_TRY(e);
+    EP_LAUNCH_CHECK(1);
+    return EP_OK;
+}
+template <template <int, int, bool> class Kernel, bool DOTS>
+int launch_chunks(const RowArgs &a, cudaStream_t stream)
+{
+    return a.K <= 8 ? launch_group<Kernel, 1, DOTS>(a, stream) : a.K <= 16 ? launch_group<Kernel, 2, DOTS>(a, stream) : launch_group<Kernel, 4, DOTS>(a, stream);
+}
+template <template <int, int, bool> class Kernel>
+int launch_rows(const RowArgs &a, cudaStream_t stream)
+{
+    return a.dots ? launch_chunks<Kernel, true>(a, stream) : launch_chunks<Kernel, false>(a, stream);
+}
+template <int G, int CHUNKS, bool DOTS>
+struct Spread {
+    static auto get() { return spread_rows_kernel<G, CHUNKS, DOTS>; }
+};
+template <int G, int CHUNKS, bool DOTS>
+struct Gather {
+    static auto get() { return gather_rows_kernel<G, CHUNKS, DOTS>; }
+};
+
+// ---- dropout of whole rows ----------------------------------------------------------------------------------------
+
+constexpr int kDropThreads = 256, kDropVecs = 4;
+
+__global__ void __launch_bounds__(kDropThreads)
+dropout_kernel(const uint4 *x, const uint4 *residual, uint4 *y, const int32_t *limit, long long rows, int vec_per_row, const DropoutArgs args)
+{
+    pdl_wait();
+    if (limit) rows = max(0ll, min(rows, (long long)__ldg(limit)));
+    const long long total = rows * vec_per_row, first = (long long)blockIdx.x * (kDropThreads * kDropVecs) + threadIdx.x;
+    if (first >= total) return;
+    const Dropout drop(args);
+    uint4 v[kDropVecs], r[kDropVecs];
+#pragma unroll
+    for (int i = 0; i < kDropVecs; ++i) {
+        const long long at = first + i * kDropThreads;
+        if (at < total) {
+            v[i] = ld_once(x + at);
+            if (residual) r[i] = ld_once(residual + at);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kDropVecs; ++i) {
+        const long long at = first + i * kDropThreads;
+        if (at < total) {
+            float f[8];
+            unpack8(v[i], f);
+            if (args.state) drop.apply(f, at);
+            if (residual) {
+                float g[8];
+                unpack8(r[i], g);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f[j] += g[j];
+            }
+            st_stream(y + at, pack8(f));
+        }
+    }
+}
+
+// The checks and arguments that the four row calls share.
+int row_args(const ep_shape_t *shape, const int32_t *slot, const float *weights, int64_t rows, int32_t *status, RowArgs *a)
+{
+    const int rc = check_shape(shape, true);
+    if (rc != EP_OK) return rc;
+    if (rows < 0) return EP_ERR_INVALID_ARG;
+    if (shape->num_tokens > 0 && !slot) return EP_ERR_NULL;
+    *a = RowArgs{};
+    a->slot = slot, a->weights = weights, a->rows = rows, a->status = status;
+    a->T = shape->num_tokens, a->K = shape->top_k, a->vec_per_row = shape->hidden / 8;
+    return EP_OK;
+}
+
+}  // namespace
+}  // namespace ep
+
+extern "C" int ep_sort(const ep_shape_t *shape, const void *x, const int32_t *slot, const float *weights, void *sorted, int64_t sorted_rows,
+                       int32_t *status, void *stream)
+{
+    using namespace ep;
+    RowArgs a;
+    const int rc = row_args(shape, slot, weights, sorted_rows, status, &a);
+    if (rc != EP_OK || a.T == 0) return rc;
+    if (!x || !sorted) return EP_ERR_NULL;
+    if (!aligned16(x) || !aligned16(sorted)) return EP_ERR_INVALID_ARG;
+    a.v = static_cast<const uint4 *>(x);
+    a.out = static_cast<uint4 *>(sorted);
+    return launch_chunks<Spread, false>(a, static_cast<cudaStream_t>(stream));
+}
+
+extern "C" int ep_sort_backward(const ep_shape_t *shape, const void *d_sorted, int64_t sorted_rows, const int32_t *slot, const float *weights,
+                                const void *x, const void *add, void *dx, float *d_weights, int32_t *status, void *stream)
+{
+    using namespace ep;
+    RowArgs a;
+    const int rc = row_args(shape, slot, weights, sorted_rows, status, &a);
+    if (rc != EP_OK) return rc;
+    if (d_weights && !weights) return EP_ERR_INVALID_ARG;                // unit weights have no gradient
+    if (a.T == 0) return EP_OK;
+    if (!d_sorted || (d_weights && !x) || (!dx && !d_weights)) return EP_ERR_NULL;
+    if (!aligned16(d_sorted) || !aligned16(x) || !aligned16(add) || !aligned16(dx)) return EP_ERR_INVALID_ARG;
+    a.table = static_cast<const uint4 *>(d_sorted);
+    a.v = static_cast<const uint4 *>(x);
+    a.add = static_cast<const uint4 *>(dx ? add : nullptr);
+    a.out = static_cast<uint4 *>(dx);
+    a.dots = d_weights;
+    return launch_rows<Gather>(a, static_cast<cudaStream_t>(stream));
+}
+
+extern "C" int ep_combine_residual(const ep_shape_t *shape, const void *out, int64_t out_rows, const int32_t *slot, const float *topk_weights,
+                                   const void *residual, const ep_dropout_t *dropout, void *y, int32_t *status, void *stream)
+{
+    using namespace ep;
+    RowArgs a;
+    int rc = row_args(shape, slot, topk_weights, out_rows, status, &a);
+    if (rc == EP_OK) rc = dropout_args(dropout, &a.drop);
+    if (rc != EP_OK || a.T == 0) return rc;
+    if (!out || !topk_weights || !y) return EP_ERR_NULL;
+    if (!aligned16(out) || !aligned16(residual) || !aligned16(y)) return EP_ERR_INVALID_ARG;
+    a.table = static_cast<const uint4 *>(out);
+    a.add = static_cast<const uint4 *>(residual);
+    a.out = static_cast<uint4 *>(y);
+    return launch_chunks<Gather, false>(a, static_cast<cudaStream_t>(stream));
+}
+
+extern "C" int ep_combine_backward(const ep_shape_t *shape, const void *dy, const void *out, int64_t out_rows, const int32_t *slot,
+                                   const float *topk_weights, const ep_dropout_t *dropout, void *d_out, float *d_weights, int32_t *status,
+                                   void *stream)
+{
+    using namespace ep;
+    RowArgs a;
+    int rc = row_args(shape, slot, topk_weights, out_rows, status, &a);
+    if (rc == EP_OK) rc = dropout_args(dropout, &a.drop);
+    if (rc != EP_OK || a.T == 0) return rc;
+    if (!dy || !topk_weights || (d_weights && !out) || (!d_out && !d_weights)) return EP_ERR_NULL;
+    if (!aligned16(dy) || !aligned16(out) || !aligned16(d_out)) return EP_ERR_INVALID_ARG;
+    a.v = static_cast<const uint4 *>(dy);
+    a.table = static_cast<const uint4 *>(out);
+    a.out = static_cast<uint4 *>(d_out);
+    a.dots = d_weights;
+    return launch_rows<Spread>(a, static_cast<cudaStream_t>(stream));
+}
+
+extern "C" int ep_dropout(const void *x, const void *residual, void *y, int64_t rows, int32_t cols, const int32_t *limit,
+                          const ep_dropout_t *dropout, void *stream)
+{
+    using namespace ep;
+    DropoutArgs d;
+    const int rc = dropout_args(dropout, &d);
+    if (rc != EP_OK) return rc;
+    if (rows < 0 || rows >= (int64_t(1) << 31) || cols < 8 || cols % 8) return EP_ERR_INVALID_ARG;
+    if (rows == 0) return EP_OK;
+    if (!x || !y) return EP_ERR_NULL;
+    if (!aligned16(x) || !aligned16(residual) || !aligned16(y)) return EP_ERR_INVALID_ARG;
+    const int64_t vecs = rows * (cols / 8), blocks = (vecs + kDropThreads * kDropVecs - 1) / (kDropThreads * kDropVecs);
+    if (blocks >= (int64_t(1) << 31)) return EP_ERR_INVALID_ARG;
+    EP_CUDA_TRY(launch_pdl(dropout_kernel, dim3((unsigned)blocks), dim3(kDropThreads), 0, static_cast<cudaStream_t>(stream),
+                           static_cast<const uint4 *>(x), static_cast<const uint4 *>(residual), static_cast<uint4 *>(y), limit, rows,
+                           (int)(cols / 8), d));
+    EP_LAUNCH_CHECK(1);
+    return EP_OK;
+}

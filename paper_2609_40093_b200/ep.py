@@ -34,6 +34,8 @@ EXPORTS = [
     "ep_dispatch_copy_engine", "ep_host_step_arena_bytes", "ep_host_step", "ep_status",
     "ep_route", "ep_route_backward", "ep_route_workspace_bytes", "ep_balance_loss",
     "ep_expert_matmul", "ep_expert_matmul_backward", "ep_expert_matmul_backward_workspace_bytes",
+    "ep_sort", "ep_sort_backward", "ep_combine_residual", "ep_combine_backward", "ep_dropout",
+    "ep_adapter_matmul", "ep_adapter_matmul_backward", "ep_adapter_matmul_backward_workspace_bytes",
     "ep_probe_bandwidth", "ep_launch_count", "ep_strerror", "ep_last_cuda_error",
 ]
 
@@ -75,6 +77,15 @@ class _Balance(ctypes.Structure):
 class _Matmul(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("in_features", ctypes.c_int32), ("out_features", ctypes.c_int32),
                 ("num_experts", ctypes.c_int32), ("activation", ctypes.c_int32), ("operand_op", ctypes.c_int32)]
+
+
+class _Dropout(ctypes.Structure):
+    _fields_ = [("state", ctypes.c_void_p), ("p", ctypes.c_double), ("site", ctypes.c_uint32)]
+
+
+class _Adapter(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("entries", ctypes.c_int64), ("in_features", ctypes.c_int32), ("out_features", ctypes.c_int32),
+                ("rank", ctypes.c_int32), ("num_adapters", ctypes.c_int32)]
 
 
 def lib() -> ctypes.CDLL:
@@ -126,6 +137,16 @@ def lib() -> ctypes.CDLL:
         L.ep_expert_matmul_backward.argtypes = [mp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.ep_expert_matmul_backward_workspace_bytes.restype = sz
         L.ep_expert_matmul_backward_workspace_bytes.argtypes = [mp]
+        dp, ap = ctypes.POINTER(_Dropout), ctypes.POINTER(_Adapter)
+        L.ep_sort.argtypes = [sp, vp, vp, vp, vp, i64, vp, vp]
+        L.ep_sort_backward.argtypes = [sp, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.ep_combine_residual.argtypes = [sp, vp, i64, vp, vp, vp, dp, vp, vp, vp]
+        L.ep_combine_backward.argtypes = [sp, vp, vp, i64, vp, vp, dp, vp, vp, vp, vp]
+        L.ep_dropout.argtypes = [vp, vp, vp, i64, i32, vp, dp, vp]
+        L.ep_adapter_matmul.argtypes = [ap, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.ep_adapter_matmul_backward.argtypes = [ap, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.ep_adapter_matmul_backward_workspace_bytes.restype = sz
+        L.ep_adapter_matmul_backward_workspace_bytes.argtypes = [ap]
         L.ep_status.argtypes = [vp, vp, vp]
         L.ep_probe_bandwidth.argtypes = [i32, vp, vp, sz, i32, vp, ctypes.POINTER(ctypes.c_double)]
         L.ep_launch_count.restype = i64
@@ -134,7 +155,9 @@ def lib() -> ctypes.CDLL:
         for name in ["ep_layout", "ep_dispatch", "ep_combine", "ep_group", "ep_dispatch_copy_engine",
                      "ep_combine_partial", "ep_dense_allgather", "ep_dense_reduce_scatter",
                      "ep_host_roundtrip", "ep_host_dispatch_per_sender", "ep_host_combine", "ep_wait_senders", "ep_post_flags",
-                     "ep_host_step", "ep_route", "ep_balance_loss", "ep_route_backward", "ep_expert_matmul", "ep_expert_matmul_backward", "ep_status", "ep_probe_bandwidth", "ep_last_cuda_error"]:
+                     "ep_host_step", "ep_route", "ep_balance_loss", "ep_route_backward", "ep_expert_matmul", "ep_expert_matmul_backward",
+                     "ep_sort", "ep_sort_backward", "ep_combine_residual", "ep_combine_backward", "ep_dropout", "ep_adapter_matmul",
+                     "ep_adapter_matmul_backward", "ep_status", "ep_probe_bandwidth", "ep_last_cuda_error"]:
             getattr(L, name).restype = i32
         _lib = L
     return _lib
@@ -697,6 +720,189 @@ def ep_expert_matmul_backward(dy, x, expert_offsets, weight, pre=None, activatio
         _at(status, (1,), torch.int32, "status"), _ptr(grads.workspace), grads.workspace.numel(),
         _stream_of(dy, x, expert_offsets, weight, pre, operand, grads.dx, grads.dweight, grads.dbias, grads.doperand, status,
                    grads.workspace)), "ep_expert_matmul_backward")
+    return grads
+
+
+@dataclass(frozen=True)
+class Dropout:
+    """Dropout by a counter-based generator (`ep_dropout_t`). state [2] (int64, device) holds the seed and the step, which the
+    kernels read when they run: a forward call and its gradient have to find the same. site tells the uses of one state apart."""
+    p: float
+    state: torch.Tensor
+    site: int = 0
+
+    def __post_init__(self):
+        if not 0 <= self.site < 1 << 32:
+            raise ValueError(f"site must be a 32-bit unsigned number, got {self.site}")
+        self.__dict__["_made"] = (None, None)
+
+    def __getstate__(self):
+        return {f.name: getattr(self, f.name) for f in fields(self)}
+
+    def __setstate__(self, state):
+        self.__dict__.update(state, _made=(None, None))
+
+    def _struct(self):
+        at = _at(self.state, (2,), torch.int64, "the dropout's state")
+        if self._made[0] != at:
+            self.__dict__["_made"] = (at, ctypes.pointer(_Dropout(at, float(self.p), int(self.site))))
+        return self._made[1]
+
+
+def _drop(dropout):
+    """(a pointer to ep_dropout_t or None, its state)"""
+    return (None, None) if dropout is None else (dropout._struct(), dropout.state)
+
+
+def _row_shape(slot, H):
+    T, K = slot.shape
+    _fit(T, K, H)
+    return ctypes.byref(_Shape(T, K, H, 1, 1)), T, K
+
+
+def ep_sort(x, slot, sorted, weights=None, status=None):
+    """sorted[slot[t][k]] = weights[t][k] * x[t] (without weights: a copy) for slots >= 0. x [T, H], sorted [rows, H] bf16, slot [T, K] int32
+    (`pair_slot`), weights [T, K] fp32. Rows that no slot names are not touched."""
+    bf, H = torch.bfloat16, x.shape[1]
+    shape, T, K = _row_shape(slot, H)
+    rows = sorted.shape[0]
+    _check(lib().ep_sort(shape, _at(x, (T, H), bf, "x"), _at(slot, (T, K), torch.int32, "slot"), _at(weights, (T, K), torch.float32, "weights"),
+                         _at(sorted, (rows, H), bf, "sorted"), rows, _at(status, (1,), torch.int32, "status"),
+                         _stream_of(x, slot, sorted, weights, status)), "ep_sort")
+    return sorted
+
+
+def ep_sort_backward(d_sorted, slot, dx=None, weights=None, x=None, d_weights=None, add=None, status=None):
+    """The gradients of `ep_sort`: dx[t] = add[t] + sum_k weights[t][k] * d_sorted[slot[t][k]], and d_weights[t][k] = <x[t], d_sorted[slot[t][k]]>.
+    Each is computed where its tensor is given; add (may be dx) is what else dx is made of. Returns dx."""
+    bf, (rows, H) = torch.bfloat16, d_sorted.shape
+    shape, T, K = _row_shape(slot, H)
+    _check(lib().ep_sort_backward(shape, _at(d_sorted, (rows, H), bf, "d_sorted"), rows, _at(slot, (T, K), torch.int32, "slot"),
+                                  _at(weights, (T, K), torch.float32, "weights"), _at(x, (T, H), bf, "x"), _at(add, (T, H), bf, "add"),
+                                  _at(dx, (T, H), bf, "dx"), _at(d_weights, (T, K), torch.float32, "d_weights"),
+                                  _at(status, (1,), torch.int32, "status"),
+                                  _stream_of(d_sorted, slot, weights, x, add, dx, d_weights, status)), "ep_sort_backward")
+    return dx
+
+
+def ep_combine_residual(out, slot, topk_weights, y, residual=None, dropout: Dropout = None, status=None):
+    """y[t] = residual[t] + drop(sum_k topk_weights[t][k] * out[slot[t][k]]); residual may be y itself."""
+    bf, (rows, H) = torch.bfloat16, out.shape
+    shape, T, K = _row_shape(slot, H)
+    drop, state = _drop(dropout)
+    _check(lib().ep_combine_residual(shape, _at(out, (rows, H), bf, "out"), rows, _at(slot, (T, K), torch.int32, "slot"),
+                                     _at(topk_weights, (T, K), torch.float32, "topk_weights"), _at(residual, (T, H), bf, "residual"), drop,
+                                     _at(y, (T, H), bf, "y"), _at(status, (1,), torch.int32, "status"),
+                                     _stream_of(out, slot, topk_weights, residual, y, status, state)), "ep_combine_residual")
+    return y
+
+
+def ep_combine_backward(dy, slot, topk_weights, d_out=None, out=None, d_weights=None, dropout: Dropout = None, status=None):
+    """The gradients of `ep_combine` and `ep_combine_residual`: d_out[slot[t][k]] = topk_weights[t][k] * drop(dy[t]), and d_weights[t][k] =
+    <drop(dy[t]), out[slot[t][k]]>. Each is computed where its tensor is given (d_out may be `out` itself); rows of d_out that no slot names
+    are not touched. Returns d_out."""
+    bf, H = torch.bfloat16, dy.shape[1]
+    shape, T, K = _row_shape(slot, H)
+    drop, state = _drop(dropout)
+    some = d_out if d_out is not None else out
+    if some is None:
+        raise ValueError("ep_combine_backward needs d_out, or out and d_weights")
+    rows = some.shape[0]
+    _check(lib().ep_combine_backward(shape, _at(dy, (T, H), bf, "dy"), _at(out, (rows, H), bf, "out"), rows, _at(slot, (T, K), torch.int32, "slot"),
+                                     _at(topk_weights, (T, K), torch.float32, "topk_weights"), drop, _at(d_out, (rows, H), bf, "d_out"),
+                                     _at(d_weights, (T, K), torch.float32, "d_weights"), _at(status, (1,), torch.int32, "status"),
+                                     _stream_of(dy, out, slot, topk_weights, d_out, d_weights, status, state)), "ep_combine_backward")
+    return d_out
+
+
+def ep_dropout(x, dropout: Dropout, residual=None, y=None, limit=None):
+    """y = residual + drop(x), x [rows, cols] bf16. limit (int32, one element on the device): rows from there on are left alone. x, residual and
+    y may be one buffer. The gradient of x is the same call on dy, without residual, with the same dropout."""
+    bf, (rows, cols) = torch.bfloat16, x.shape
+    _fit(rows, cols)
+    if y is None:
+        y = torch.empty_like(x)
+    drop, state = _drop(dropout)
+    if limit is not None and limit.numel() != 1:
+        raise ValueError(f"limit must be one number, got {list(limit.shape)}")
+    _check(lib().ep_dropout(_at(x, (rows, cols), bf, "x"), _at(residual, (rows, cols), bf, "residual"), _at(y, (rows, cols), bf, "y"), rows, cols,
+                            _at(limit, None, torch.int32, "limit"), drop, _stream_of(x, residual, y, limit, state)), "ep_dropout")
+    return y
+
+
+@dataclass
+class Adapters:
+    """The weights of low-rank adapters: down [A, rank, in], up [A, out, rank] bf16, scale [A] fp32 (None: 1)."""
+    down: torch.Tensor
+    up: torch.Tensor
+    scale: torch.Tensor = None
+
+    def _args(self, rows, entries):
+        """(ep_adapter_t, addresses of down, up and scale)"""
+        (A, r, H), N, bf = self.down.shape, self.up.shape[1], torch.bfloat16
+        _fit(A, r, H, N)
+        return (_Adapter(rows, entries, H, N, r, A), _at(self.down, (A, r, H), bf, "down"), _at(self.up, (A, N, r), bf, "up"),
+                _at(self.scale, (A,), torch.float32, "scale"))
+
+
+@dataclass
+class AdapterGrads:
+    """Gradients of `ep_adapter_matmul` and the workspace of the call that computes them; None: not computed."""
+    dx: torch.Tensor
+    ddown: torch.Tensor
+    dup: torch.Tensor
+    workspace: torch.Tensor
+
+
+def ep_adapter_matmul_backward_workspace_bytes(rows, entries, in_features, out_features, rank, num_adapters) -> int:
+    _fit(in_features, out_features, rank, num_adapters)
+    m = _Adapter(int(rows), int(entries), int(in_features), int(out_features), int(rank), int(num_adapters))
+    return int(lib().ep_adapter_matmul_backward_workspace_bytes(ctypes.byref(m)))
+
+
+def alloc_adapter_grads(x, adapters: Adapters, entries=None, dx=True, down=True, up=True) -> AdapterGrads:
+    """Allocates the outputs and the workspace of `ep_adapter_matmul_backward` (torch owns the memory)."""
+    (A, r, H), N, rows = adapters.down.shape, adapters.up.shape[1], x.shape[0]
+    nbytes = max(256, ep_adapter_matmul_backward_workspace_bytes(rows, rows if entries is None else entries, H, N, r, A))
+    return AdapterGrads(torch.empty_like(x) if dx else None, torch.empty_like(adapters.down) if down else None,
+                        torch.empty_like(adapters.up) if up else None, torch.empty(nbytes, dtype=torch.uint8, device=x.device))
+
+
+def _entries(row_index, rows):
+    return rows if row_index is None else row_index.shape[0]
+
+
+def ep_adapter_matmul(x, adapter_offsets, adapters: Adapters, y=None, base=None, row_index=None, mid=None, status=None):
+    """y[row] = base[row] + scale[a] * (x[row] down[a]^T) up[a]^T for the rows of adapter a: row_index[i] (None: i) for adapter_offsets[a] <= i <
+    adapter_offsets[a+1]. `ep_layout` of the adapters' ids [T, 1] gives both (expert_offsets, pair_token). base (what the shared projection gave)
+    may be y itself; rows that no entry names are not touched. mid [entries, rank] receives the first product, which the gradients need."""
+    bf, (rows, H) = torch.bfloat16, x.shape
+    n = _entries(row_index, rows)
+    m, down, up, scale = adapters._args(rows, n)
+    N, A, r = m.out_features, m.num_adapters, m.rank
+    _check(lib().ep_adapter_matmul(
+        ctypes.byref(m), _at(x, (rows, m.in_features), bf, "x"), _at(adapter_offsets, (A + 1,), torch.int32, "adapter_offsets"),
+        _at(row_index, (n,), torch.int32, "row_index"), down, up, scale, _at(base, (rows, N), bf, "base"), _at(y, (rows, N), bf, "y"),
+        _at(mid, (n, r), bf, "mid"), _at(status, (1,), torch.int32, "status"),
+        _stream_of(x, adapter_offsets, row_index, adapters.down, adapters.up, adapters.scale, base, y, mid, status)), "ep_adapter_matmul")
+    return y
+
+
+def ep_adapter_matmul_backward(dy, x, adapter_offsets, adapters: Adapters, mid, grads: AdapterGrads, base=None, row_index=None, status=None) -> AdapterGrads:
+    """The gradients of `ep_adapter_matmul` for dy, written to the tensors that `grads` has. mid is what the forward call wrote; dx is added to
+    base (may be dx itself, None: nothing is added)."""
+    bf, rows = torch.bfloat16, dy.shape[0]
+    n = _entries(row_index, rows)
+    m, down, up, scale = adapters._args(rows, n)
+    H, N, A, r = m.in_features, m.out_features, m.num_adapters, m.rank
+    ws = grads.workspace
+    _check(lib().ep_adapter_matmul_backward(
+        ctypes.byref(m), _at(dy, (rows, N), bf, "dy"), _at(x, (rows, H), bf, "x"), _at(adapter_offsets, (A + 1,), torch.int32, "adapter_offsets"),
+        _at(row_index, (n,), torch.int32, "row_index"), down, up, scale, _at(mid, (n, r), bf, "mid"), _at(base, (rows, H), bf, "base"),
+        _at(grads.dx, (rows, H), bf, "dx"), _at(grads.ddown, (A, r, H), bf, "ddown"), _at(grads.dup, (A, N, r), bf, "dup"),
+        _at(status, (1,), torch.int32, "status"), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(),
+        _stream_of(dy, x, adapter_offsets, row_index, adapters.down, adapters.up, adapters.scale, mid, base, grads.dx, grads.ddown, grads.dup, status,
+                   ws)), "ep_adapter_matmul_backward")
     return grads
 
 
