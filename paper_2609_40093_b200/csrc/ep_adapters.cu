@@ -34,17 +34,30 @@ __device__ __forceinline__ int quotient_up(int a, int b) { return (int)(((unsign
 
 __device__ __forceinline__ int segment_bound(int32_t v, long long entries) { return v < 0 ? 0 : (v > entries ? (int)entries : v); }
 
-// Four rows' 64 elements from column x on, as four 128-byte lines. A row that does not exist gives zeros.
-__device__ __forceinline__ void tma_gather4(uint32_t dst, const CUtensorMap *map, int x, const int (&row)[4], uint32_t bar)
+// 16 bytes from global to shared memory, in the background; zeros where `there` is false.
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there)
 {
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst),
-        "l"(map), "r"(x), "r"(row[0]), "r"(row[1]), "r"(row[2]), "r"(row[3]), "r"(bar)
-        : "memory");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16u : 0u) : "memory");
 }
+__device__ __forceinline__ void copy_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// All groups of this thread but the last N have landed.
+template <int N>
+__device__ __forceinline__ void copy_wait()
+{
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+// Where 16-byte piece `piece` of line `line` lies in a tile with the 128-byte swizzle.
+__device__ __forceinline__ uint32_t swizzled(int line, int piece) { return line * 128 + ((piece ^ (line & 7)) << 4); }
 
 // What this thread wrote to shared memory is there for the tensor cores.
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// A box on its way into L2.
+__device__ __forceinline__ void tma_prefetch(const CUtensorMap *map, int x, int y, int z)
+{
+    asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];" ::"l"(map), "r"(x), "r"(y), "r"(z) : "memory");
+}
 
 // ---- the rank kernel ----------------------------------------------------------------------------------------------
 
@@ -59,6 +72,7 @@ constexpr int kRingBytes = 96 * 1024, kTailBytes = 15 * 1024 - 512;
 constexpr int kStageWords = 32 * 32, kStageBytes = kEpilogueWarps * kStageWords * 4;      // an epilogue warp's 32 rows x 32 columns
 constexpr int kRankSmem = 1024 + kRingBytes + kTailBytes;
 constexpr int kMaxStages = 4, kMaxUnits = 3;
+constexpr int kLag = 2;                   // stages a loader has in flight behind the one it asks for
 
 struct RankArgs {
     const int32_t *offsets;               // [A+1]
@@ -69,6 +83,7 @@ struct RankArgs {
     uint16_t *out;                        // [rows][out], may be NULL: the first product alone
     uint16_t *mid;                        // [entries][rank], may be NULL
     long long rows, entries;
+    const uint16_t *in_rows;              // [rows][in]
     int in, out_features, rank, A, split;
 };
 
@@ -85,8 +100,7 @@ __device__ __forceinline__ uint4 pack8(const float (&f)[8])
 // BACK: the weights are read along the other axis (up for the first product, down for the second), and the scale goes to `mid`.
 template <bool BACK>
 __global__ void __launch_bounds__(kThreads, 2)
-rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_in, const __grid_constant__ CUtensorMap map_first,
-            const __grid_constant__ CUtensorMap map_second)
+rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_first, const __grid_constant__ CUtensorMap map_second)
 {
     extern __shared__ char raw[];
     __shared__ uint64_t full_[kMaxStages], empty_[kMaxStages], unit_full_[kMaxUnits], unit_empty_[kMaxUnits], mid_full_, mid_ready_, acc_full_[2],
@@ -148,6 +162,7 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_in, const 
     const int blocks = a.out ? (a.out_features + kBlockColumns - 1) / kBlockColumns : 0;
     const int stage_bytes = kLines + chunks * 8192, stages = kRingBytes / stage_bytes;
     const int units = (kRingBytes - kStageBytes) / kLines - chunks;
+    const int loaders = min(kEpilogueWarps, (m + 3) / 4), quarters = (m + 31) / 32;        // warps that bring rows; quarters of the lanes with rows
     const int ex_ld = r16 + 4;
     const bool ex_small = m * ex_ld * 4 <= kTailBytes;
     const uint32_t ring = (smem_addr(raw) + 1023) & ~1023u;
@@ -157,9 +172,9 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_in, const 
     float *const exchange = reinterpret_cast<float *>(ex_small ? ring_ptr + kRingBytes : stage_ptr);
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kMaxStages; ++s) bar_init(smem_addr(&full_[s]), 1), bar_init(smem_addr(&empty_[s]), 1);
+        for (int s = 0; s < kMaxStages; ++s) bar_init(smem_addr(&full_[s]), 1 + loaders), bar_init(smem_addr(&empty_[s]), 1);
         for (int s = 0; s < kMaxUnits; ++s) bar_init(smem_addr(&unit_full_[s]), 1), bar_init(smem_addr(&unit_empty_[s]), 1);
-        for (int s = 0; s < 2; ++s) bar_init(smem_addr(&acc_full_[s]), 1), bar_init(smem_addr(&acc_empty_[s]), kEpilogueWarps);
+        for (int s = 0; s < 2; ++s) bar_init(smem_addr(&acc_full_[s]), 1), bar_init(smem_addr(&acc_empty_[s]), 2 * quarters);
         bar_init(smem_addr(&mid_full_), 1);
         bar_init(smem_addr(&mid_ready_), kEpilogueWarps);
         bar_init(smem_addr(&ex_full_), split * kEpilogueWarps);
@@ -187,32 +202,30 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_in, const 
     const uint32_t tmem = tmem_slot;
     const uint32_t full0 = smem_addr(full_), empty0 = smem_addr(empty_), unit_full0 = smem_addr(unit_full_), unit_empty0 = smem_addr(unit_empty_);
 
-    if (warp == 0) {
-        // ---- rows and the first weights into the ring: lane l brings rows 4 l .. 4 l + 3
-        int row[4];
-        const bool mine = 4 * lane < m;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            row[i] = mine ? row_of[4 * lane + i] : -1;
-            if (row[i] < 0) row[i] = (int)a.rows;                            // does not exist: zeros
-        }
-        const uint32_t bytes = (uint32_t)((m + 3) / 4 * 512 + (BACK ? chunks * 8192 : r16 * 128));
+    if (warp == 0 && elect_one()) {
+        // ---- weights
+        if (blocks && (blocks - 1) / split < 16)                             // few blocks: nobody else has brought them into L2
+            for (int b = part; b < blocks; b += split)
+                for (int c = 0; c < chunks; ++c) {
+                    if (BACK) {
+                        tma_prefetch(&map_second, b * kBlockColumns, 64 * c, adapter);
+                        tma_prefetch(&map_second, b * kBlockColumns + 64, 64 * c, adapter);
+                    } else {
+                        tma_prefetch(&map_second, 64 * c, b * kBlockColumns, adapter);
+                    }
+                }
+        const uint32_t bytes = (uint32_t)(BACK ? chunks * 8192 : r16 * 128);
         int s = 0, phase = 1, sent = 0;
         bool ok = true;
         for (int k = k_from; k < k_to; ++k) {
-            ok = __all_sync(kFullMask, bar_wait(empty0 + 8 * s, phase, gave_up));
-            if (!ok) break;
-            const uint32_t full = full0 + 8 * s, dst = ring + s * stage_bytes;
-            if (lane == 0) {
-                bar_expect(full, bytes);
-                if (BACK) {
-                    for (int u = 0; u < chunks; ++u) tma_load<1>(dst + kLines + u * 8192, &map_first, 64 * u, k * kTileK, adapter, full);
-                } else {
-                    tma_load<1>(dst + kLines, &map_first, k * kTileK, 0, adapter, full);
-                }
+            if (!(ok = bar_wait(empty0 + 8 * s, phase, gave_up))) break;
+            const uint32_t full = full0 + 8 * s, dst = ring + s * stage_bytes + kLines;
+            bar_expect(full, bytes);
+            if (BACK) {
+                for (int u = 0; u < chunks; ++u) tma_load<1>(dst + u * 8192, &map_first, 64 * u, k * kTileK, adapter, full);
+            } else {
+                tma_load<1>(dst, &map_first, k * kTileK, 0, adapter, full);
             }
-            __syncwarp();
-            if (mine) tma_gather4(dst + lane * 512, &map_in, k * kTileK, row, full);
             ++sent;
             if (++s == stages) s = 0, phase ^= 1;
         }
@@ -223,7 +236,7 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_in, const 
                 --s;
                 bar_wait(full0 + 8 * s, phase ^ 1, &none);
             }
-        } else if (lane == 0 && blocks) {
+        } else if (blocks) {
             // ---- the second weights, once the ring's memory is free
             ok = bar_wait(smem_addr(&mid_full_), 0, gave_up);
             if (ok && split > 1 && !ex_small) ok = bar_wait<true>(smem_addr(&ex_read_), 0, gave_up);
@@ -293,7 +306,56 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_in, const 
         const int q = warp & 3, half = (warp - 2) >> 2, thread = threadIdx.x - 64;
         const int my_row = q * 32 + lane;                                    // a warp reaches the lanes 32 (warp mod 4) .. + 31
         const float scale = a.scale ? __ldg(a.scale + adapter) : 1.f, mid_scale = BACK ? scale : 1.f, out_scale = BACK ? 1.f : scale;
-        bool ok = bar_wait(smem_addr(&mid_full_), 0, gave_up);
+        bool ok = true;
+        if (warp - 2 < loaders) {
+            // ---- rows into the ring: eight lanes a row's line, four rows a warp, every 32 rows
+            const int line = 4 * (warp - 2) + (lane >> 3), piece = lane & 7, n_k = k_to - k_from;
+            const uint16_t *src[4];
+            bool there[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int row = row_of[line + 32 * i];
+                there[i] = row >= 0;
+                src[i] = a.in_rows + (size_t)max(row, 0) * a.in;
+            }
+            int s = 0, phase = 1, done = 0;
+            for (int i = 0; i < n_k + kLag; ++i) {
+                if (i < n_k) {
+                    if (!(ok = __all_sync(kFullMask, bar_wait(empty0 + 8 * s, phase, gave_up)))) break;
+                    const int col = (k_from + i) * kTileK + piece * 8, at = col < a.in ? col : 0;
+                    const uint32_t dst = ring + s * stage_bytes + swizzled(line, piece);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (line + 32 * j < m) copy16(dst + j * 32 * 128, src[j] + at, there[j] && col < a.in);
+                    if (++s == stages) s = 0, phase ^= 1;
+                }
+                copy_group();
+                if (i >= kLag) {
+                    copy_wait<kLag>();
+                    fence_async();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(full0 + 8 * done);
+                    if (++done == stages) done = 0;
+                }
+            }
+            copy_wait<0>();
+        }
+        // the first block's base, under what follows: lane l of a pass holds 8 columns of row 8 i + l / 4
+        int rows[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) rows[i] = row_of[q * 32 + 8 * i + (lane >> 2)];
+        uint4 r[2][4];
+        const auto request = [&](int b, int h, int i) {
+            const int col = b * kBlockColumns + half * 64 + h * 32 + (lane & 3) * 8;
+            r[h][i] = make_uint4(0u, 0u, 0u, 0u);
+            if (a.base && rows[i] >= 0 && b < blocks && col < a.out_features)     // `base` may be the output: an ordinary load
+                r[h][i] = *reinterpret_cast<const uint4 *>(a.base + (size_t)rows[i] * a.out_features + col);
+        };
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) request(part, h, i);
+        ok = ok && bar_wait(smem_addr(&mid_full_), 0, gave_up);
         tmem_fence_after();
         // 8 columns of a row, rounded: the second product's operand, and `mid`
         const auto put = [&](int row, int col, float (&f)[8], bool store) {
@@ -350,25 +412,11 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_in, const 
         tmem_fence_before();
         __syncwarp();
         if (lane == 0) bar_arrive_cluster_release(smem_addr(&mid_ready_));
-        // ---- blocks of the output: lane l of a pass holds 8 columns of row 8 i + l / 4
+        // ---- blocks of the output; a block's base is replaced by the next one's as it is used
         float *stage = reinterpret_cast<float *>(stage_ptr) + (warp - 2) * kStageWords;
-        int rows[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) rows[i] = row_of[q * 32 + 8 * i + (lane >> 2)];
         int used = 0;
-        for (int b = part; ok && b < blocks; b += split, ++used) {
+        for (int b = part; ok && q < quarters && b < blocks; b += split, ++used) {
             const int acc = used & 1;
-            uint4 r[2][4];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int col = b * kBlockColumns + half * 64 + h * 32 + (lane & 3) * 8;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    r[h][i] = make_uint4(0u, 0u, 0u, 0u);
-                    if (a.base && rows[i] >= 0 && col < a.out_features)       // `base` may be the output: an ordinary load
-                        r[h][i] = *reinterpret_cast<const uint4 *>(a.base + (size_t)rows[i] * a.out_features + col);
-                }
-            }
             if (!(ok = bar_wait(smem_addr(&acc_full_[acc]), (used >> 1) & 1, gave_up))) break;
             tmem_fence_after();
 #pragma unroll
@@ -394,6 +442,7 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_in, const 
                     const float z[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
                     float f[8];
                     unpack8(r[h][i], f);
+                    request(b + split, h, i);
 #pragma unroll
                     for (int k = 0; k < 8; ++k) f[k] = fmaf(out_scale, z[k], f[k]);
                     if (rows[i] >= 0 && col < a.out_features)
@@ -413,178 +462,251 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_in, const 
 
 // ---- the gradient kernel ------------------------------------------------------------------------------------------
 
-constexpr int kGradThreads = 64 + 128;
+// One warp issues the products, four bring entries, four empty the accumulators, of which there are two, so that an item's results
+// leave under the next one's products. SPLIT: a cluster shares an item, one item per cluster.
+constexpr int kGradThreads = 32 * 9;
 constexpr int kGradLd = kRows + 4;        // accumulators on their way out: [rank][128 features]
 constexpr int kGradStages = 4;
+constexpr int kGradOutBytes = 32 * kGradLd * 4;
 
 struct GradArgs {
     const int32_t *offsets, *index;
     const float *scale;
-    int32_t *status;
+    const uint16_t *x, *dmid, *dy, *mid;
     uint16_t *ddown, *dup;
+    int32_t *status;
     long long rows, entries;
     int H, N, rank, A, split;
     int tiles_down, tiles_up;             // feature tiles of an adapter's ddown (0: not wanted) and dup
-    int stages, columns;                  // columns of tensor memory
+    int items;                            // A * (tiles_down + tiles_up)
+    int stages, columns;                  // columns of tensor memory of one accumulator
 };
 
+template <bool SPLIT>
 __global__ void __launch_bounds__(kGradThreads)
-adapter_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_dmid,
-                    const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUtensorMap map_mid)
+adapter_grad_kernel(const GradArgs a)
 {
     extern __shared__ char raw[];
-    __shared__ uint64_t full_[kGradStages], empty_[kGradStages], acc_full_, ex_full_;
+    __shared__ uint64_t full_[kGradStages], empty_[kGradStages], acc_full_[2], acc_empty_[2], ex_full_;
     __shared__ uint32_t tmem_slot;
     __shared__ int gave_up_;
     volatile int *gave_up = &gave_up_;
 
     const int warp = __shfl_sync(kFullMask, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-    const int split = a.split, part = split > 1 ? (int)cluster_rank() : 0;
-    const int item = blockIdx.x / split, tiles = a.tiles_down + a.tiles_up, adapter = item / tiles, f = item - adapter * tiles;
-    const bool up = f >= a.tiles_down;
-    const int m0 = (up ? f - a.tiles_down : f) * kRows, features = up ? a.N : a.H;
-    const int chunks = (a.rank + 63) / 64, r16 = (a.rank + 15) & ~15;
-
-    pdl_wait();
-    const int begin = segment_bound(__ldg(a.offsets + adapter), a.entries), end = segment_bound(__ldg(a.offsets + adapter + 1), a.entries);
-    const int n = max(0, end - begin), all_k = quotient_up(n, kTileK);
-    const int k_from = (int)((long long)all_k * part / split), k_to = (int)((long long)all_k * (part + 1) / split);
+    const int split = SPLIT ? a.split : 1, part = SPLIT ? (int)cluster_rank() : 0;
+    const int tiles = a.tiles_down + a.tiles_up;
+    const int chunks = (a.rank + 63) / 64, r16 = (a.rank + 15) & ~15, stages = a.stages;
+    const int stage_bytes = kLines + chunks * 8192;
     const uint32_t ring = (smem_addr(raw) + 1023) & ~1023u;
-    float *const out = reinterpret_cast<float *>(raw + (ring - smem_addr(raw)));
-    const int stage_bytes = kLines + chunks * 8192, stages = a.stages;
+    char *const ring_ptr = raw + (ring - smem_addr(raw));
+    float *const out = reinterpret_cast<float *>(SPLIT ? ring_ptr : ring_ptr + stages * stage_bytes);    // SPLIT: all columns, where the stages were
+    int *const bound = reinterpret_cast<int *>(ring_ptr + stages * stage_bytes + (SPLIT ? 0 : kGradOutBytes));
+
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kGradStages; ++s) bar_init(smem_addr(&full_[s]), 1), bar_init(smem_addr(&empty_[s]), 1);
-        bar_init(smem_addr(&acc_full_), 1);
+        for (int s = 0; s < kGradStages; ++s) bar_init(smem_addr(&full_[s]), 4), bar_init(smem_addr(&empty_[s]), 1);
+        for (int s = 0; s < 2; ++s) bar_init(smem_addr(&acc_full_[s]), 1), bar_init(smem_addr(&acc_empty_[s]), 4);
         bar_init(smem_addr(&ex_full_), split * 4);
         gave_up_ = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 1) tmem_alloc<1>(smem_addr(&tmem_slot), a.columns);
+    pdl_wait();
+    if (warp == 0) tmem_alloc<1>(smem_addr(&tmem_slot), 2 * a.columns);
+    for (int i = threadIdx.x; i <= a.A; i += kGradThreads) bound[i] = segment_bound(__ldg(a.offsets + i), a.entries);
     tmem_fence_before();
-    if (split > 1) cluster_sync();
+    if (SPLIT) cluster_sync();
     __syncthreads();
     tmem_fence_after();
     pdl_trigger();
     const uint32_t tmem = tmem_slot, full0 = smem_addr(full_), empty0 = smem_addr(empty_);
+    const int first = blockIdx.x / split, step = gridDim.x / split;
 
-    if (warp == 0) {
-        // ---- entries into the ring: lane l brings entries 4 (l mod 16) .. + 3 of a stage, one half of the features each
-        const CUtensorMap *rows_map = up ? &map_dy : &map_x, *rank_map = up ? &map_mid : &map_dmid;
-        const int quad = lane & 15, side = lane >> 4;
-        const uint32_t bytes = (uint32_t)stage_bytes;
-        int s = 0, phase = 1, sent = 0;
+    struct Item {
+        int adapter, m0, begin, n, k_from, k_to;
+        bool up;
+    };
+    const auto item_at = [&](int i) {
+        Item t;
+        t.adapter = i / tiles;
+        const int f = i - t.adapter * tiles;
+        t.up = f >= a.tiles_down;
+        t.m0 = (t.up ? f - a.tiles_down : f) * kRows;
+        t.begin = bound[t.adapter];
+        t.n = max(0, bound[t.adapter + 1] - t.begin);
+        const int all = quotient_up(t.n, kTileK);
+        t.k_from = (int)((long long)all * part / split), t.k_to = (int)((long long)all * (part + 1) / split);
+        return t;
+    };
+
+    if (warp >= 1 && warp < 5) {
+        // ---- entries into the ring: 16 lanes bring 128 features of one and its piece of the rank, every eighth entry
+        const int thread = threadIdx.x - 32, piece = thread & 15, line = thread >> 4, half = piece >> 3;
+        const uint32_t at = half * 8192 + swizzled(line, piece & 7);
+        int s = 0, phase = 1, done = 0, waiting = 0;
         bool ok = true;
-        for (int k = k_from; k < k_to; ++k) {
-            int row[4], entry[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int e = k * kTileK + 4 * quad + i;
-                entry[i] = (int)a.entries, row[i] = (int)a.rows;             // does not exist: zeros
-                if (e < n) {
-                    const int r = a.index ? __ldg(a.index + begin + e) : begin + e;
-                    if (r >= 0 && r < a.rows) row[i] = r, entry[i] = begin + e;
-                    else if (a.status) atomicOr(a.status, EP_STATUS_BAD_INDEX);
-                }
-            }
-            ok = __all_sync(kFullMask, bar_wait(empty0 + 8 * s, phase, gave_up));
-            if (!ok) break;
-            const uint32_t full = full0 + 8 * s, dst = ring + s * stage_bytes;
-            if (lane == 0) bar_expect(full, bytes);
+        const auto arrive = [&] {
+            fence_async();
             __syncwarp();
-            tma_gather4(dst + side * 8192 + quad * 512, rows_map, m0 + side * 64, row, full);
-            if (side < chunks) tma_gather4(dst + kLines + side * 8192 + quad * 512, rank_map, side * 64, entry, full);
-            ++sent;
-            if (++s == stages) s = 0, phase ^= 1;
-        }
-        if (!ok)
-            for (int i = min(sent, stages); i > 0; --i) {
-                int none = 0;
-                if (s == 0) s = stages, phase ^= 1;
-                --s;
-                bar_wait(full0 + 8 * s, phase ^ 1, &none);
+            if (lane == 0) bar_arrive(full0 + 8 * done);
+            if (++done == stages) done = 0;
+        };
+        for (int i = first; ok && i < a.items; i += step) {
+            const Item t = item_at(i);
+            const uint16_t *rows = t.up ? a.dy : a.x, *ranks = t.up ? a.mid : a.dmid;
+            const int features = t.up ? a.N : a.H, col = t.m0 + piece * 8;
+            const bool live = col < features, ranked = piece * 8 < r16, real = piece * 8 < a.rank;
+            rows += live ? col : 0;
+            ranks += real ? piece * 8 : 0;
+            int next[8];
+            const auto look = [&](int k) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int e = k * kTileK + line + 8 * j;
+                    next[j] = e < t.n ? (a.index ? __ldg(a.index + t.begin + e) : t.begin + e) : -1;
+                }
+            };
+            if (t.k_from < t.k_to) look(t.k_from);
+            for (int k = t.k_from; k < t.k_to; ++k) {
+                if (!(ok = __all_sync(kFullMask, bar_wait(empty0 + 8 * s, phase, gave_up)))) break;
+                const uint32_t dst = ring + s * stage_bytes + at;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int e = k * kTileK + line + 8 * j, row = next[j];
+                    const bool there = row >= 0 && row < a.rows;             // others are zeros, in both operands
+                    if (a.status && !there && e < t.n && piece == 0) atomicOr(a.status, EP_STATUS_BAD_INDEX);
+                    copy16(dst + j * 1024, rows + (there ? (size_t)row * features : 0), there && live);
+                    if (ranked) copy16(dst + kLines + j * 1024, ranks + (there ? (size_t)(t.begin + e) * a.rank : 0), there && real);
+                }
+                copy_group();
+                if (k + 1 < t.k_to) look(k + 1);
+                if (++s == stages) s = 0, phase ^= 1;
+                if (waiting == kLag) copy_wait<kLag>(), arrive(); else ++waiting;
             }
-    } else if (warp == 1 && elect_one()) {
-        int s = 0, phase = 0;
+        }
+        copy_wait<0>();
+        for (; ok && waiting > 0; --waiting) arrive();
+    } else if (warp == 0 && elect_one()) {
+        // ---- products
+        int s = 0, phase = 0, used = 0;
         bool ok = true;
         const uint32_t idesc = instr_desc(kRows, r16, true, true);
-        for (int k = k_from; k < k_to; ++k) {
-            if (!(ok = bar_wait(full0 + 8 * s, phase, gave_up))) break;
+        for (int i = first; ok && i < a.items; i += step) {
+            const Item t = item_at(i);
+            if (t.k_from == t.k_to) continue;
+            const int acc = used & 1;
+            if (!(ok = bar_wait(smem_addr(&acc_empty_[acc]), ((used >> 1) & 1) ^ 1, gave_up))) break;
             tmem_fence_after();
-            const uint32_t at = ring + s * stage_bytes;
-            const uint64_t da = desc_mn_major(at), db = desc_mn_major(at + kLines);
+            for (int k = t.k_from; k < t.k_to; ++k) {
+                if (!(ok = bar_wait(full0 + 8 * s, phase, gave_up))) break;
+                tmem_fence_after();
+                const uint32_t at = ring + s * stage_bytes;
+                const uint64_t da = desc_mn_major(at), db = desc_mn_major(at + kLines);
 #pragma unroll
-            for (int j = 0; j < kTileK / 16; ++j) mma_bf16<1>(tmem, da + j * 128, db + j * 128, idesc, k > k_from || j > 0);
-            mma_commit<1>(empty0 + 8 * s);
-            if (++s == stages) s = 0, phase ^= 1;
-        }
-        if (ok && k_to > k_from) mma_commit<1>(smem_addr(&acc_full_));
-    } else if (warp >= 2) {
-        // ---- accumulators out: through shared memory, added up over the CTAs that share them
-        const int q = warp & 3, thread = threadIdx.x - 64;
-        bool ok = true;
-        if (k_to > k_from) ok = bar_wait(smem_addr(&acc_full_), 0, gave_up);
-        tmem_fence_after();
-        for (int c0 = 0; ok && c0 < r16; c0 += 32) {
-            uint32_t v[32];
-            if (k_to > k_from) {
-                tmem_load32(tmem + (uint32_t(q * 32) << 16) + c0, v);
-            } else {
-#pragma unroll
-                for (int c = 0; c < 32; ++c) v[c] = 0u;
+                for (int j = 0; j < kTileK / 16; ++j) mma_bf16<1>(tmem + acc * a.columns, da + j * 128, db + j * 128, idesc, k > t.k_from || j > 0);
+                mma_commit<1>(empty0 + 8 * s);
+                if (++s == stages) s = 0, phase ^= 1;
             }
-#pragma unroll
-            for (int c = 0; c < 32; ++c)
-                if (c0 + c < r16) out[(c0 + c) * kGradLd + q * 32 + lane] = __uint_as_float(v[c]);
+            if (ok) mma_commit<1>(smem_addr(&acc_full_[acc]));
+            ++used;
         }
-        if (split > 1) {
-            __syncwarp();
-            if (ok && lane < split) bar_arrive_cluster_release(in_cta(smem_addr(&ex_full_), lane));
-            ok = ok && bar_wait<true>(smem_addr(&ex_full_), 0, gave_up);
-        } else {
-            asm volatile("bar.sync 1, 128;" ::: "memory");                   // the four warps
-        }
-        const float scale = up && a.scale ? __ldg(a.scale + adapter) : 1.f;
-        // ddown: 8 features of a rank; dup: 8 ranks of a feature
-        const int total = up ? kRows * (a.rank / 8) : a.rank * (kRows / 8);
-        const int from = total * part / split, to = total * (part + 1) / split;
-        for (int i = from + thread; ok && i < to; i += 128) {
-            const int feature = up ? i % kRows : i % (kRows / 8) * 8, rank = up ? i / kRows * 8 : i / (kRows / 8);
-            if (m0 + feature >= features) continue;
-            float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            const float *src = out + rank * kGradLd + feature;
-            for (int s = 0; s < split; ++s) {
-                if (split == 1 && up) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) z[j] = src[j * kGradLd];
-                } else if (split == 1) {
-                    const float4 lo = *reinterpret_cast<const float4 *>(src), hi = *reinterpret_cast<const float4 *>(src + 4);
-                    z[0] = lo.x, z[1] = lo.y, z[2] = lo.z, z[3] = lo.w, z[4] = hi.x, z[5] = hi.y, z[6] = hi.z, z[7] = hi.w;
-                } else if (up) {
-                    const uint32_t at = in_cta(smem_addr(src), s);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        float w;
-                        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(w) : "r"(at + j * kGradLd * 4) : "memory");
-                        z[j] += w;
-                    }
+    } else if (warp >= 5) {
+        // ---- accumulators out, through shared memory; SPLIT: added up over the CTAs that share them
+        const int q = warp & 3, thread = threadIdx.x - 32 * 5;
+        int used = 0;
+        bool ok = true;
+        for (int i = first; ok && i < a.items; i += step) {
+            const Item t = item_at(i);
+            const bool some = t.k_from < t.k_to;
+            const int acc = used & 1, features = t.up ? a.N : a.H;
+            const float scale = t.up && a.scale ? __ldg(a.scale + t.adapter) : 1.f;
+            if (some) {
+                ok = bar_wait(smem_addr(&acc_full_[acc]), (used >> 1) & 1, gave_up);
+                tmem_fence_after();
+                ++used;
+            }
+            // columns [c0, c0 + 32) of the accumulator, or zeros, into `out`, from its column `to` on
+            const auto down = [&](int c0, int to) {
+                uint32_t v[32];
+                if (some) {
+                    tmem_load32(tmem + (uint32_t(q * 32) << 16) + acc * a.columns + c0, v);
                 } else {
-                    const uint32_t at = in_cta(smem_addr(src), s);
-                    const float4 lo = load_cluster(at), hi = load_cluster(at + 16);
-                    z[0] += lo.x, z[1] += lo.y, z[2] += lo.z, z[3] += lo.w, z[4] += hi.x, z[5] += hi.y, z[6] += hi.z, z[7] += hi.w;
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) v[c] = 0u;
+                }
+#pragma unroll
+                for (int c = 0; c < 32; ++c)
+                    if (c0 + c < r16) out[(to + c) * kGradLd + q * 32 + lane] = __uint_as_float(v[c]);
+            };
+            // 8 results: ddown, 8 features of a rank; dup, 8 ranks of a feature
+            const auto store = [&](float (&z)[8], int feature, int rank) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) z[j] *= scale;
+                uint16_t *dst = t.up ? a.dup + ((size_t)t.adapter * a.N + t.m0 + feature) * a.rank + rank
+                                     : a.ddown + ((size_t)t.adapter * a.rank + rank) * a.H + t.m0 + feature;
+                *reinterpret_cast<uint4 *>(dst) = pack8(z);
+            };
+            if (SPLIT) {
+                for (int c0 = 0; ok && c0 < r16; c0 += 32) down(c0, c0);
+                __syncwarp();
+                if (ok && lane < split) bar_arrive_cluster_release(in_cta(smem_addr(&ex_full_), lane));
+                ok = ok && bar_wait<true>(smem_addr(&ex_full_), 0, gave_up);
+                const int total = t.up ? kRows * (a.rank / 8) : a.rank * (kRows / 8);
+                const int from = total * part / split, to = total * (part + 1) / split;
+                for (int j = from + thread; ok && j < to; j += 128) {
+                    const int feature = t.up ? j % kRows : j % (kRows / 8) * 8, rank = t.up ? j / kRows * 8 : j / (kRows / 8);
+                    if (t.m0 + feature >= features) continue;
+                    float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                    const uint32_t src = smem_addr(out + rank * kGradLd + feature);
+                    for (int s = 0; s < split; ++s) {
+                        const uint32_t at = in_cta(src, s);
+                        if (t.up) {
+#pragma unroll
+                            for (int l = 0; l < 8; ++l) {
+                                float w;
+                                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(w) : "r"(at + l * kGradLd * 4) : "memory");
+                                z[l] += w;
+                            }
+                        } else {
+                            const float4 lo = load_cluster(at), hi = load_cluster(at + 16);
+                            z[0] += lo.x, z[1] += lo.y, z[2] += lo.z, z[3] += lo.w, z[4] += hi.x, z[5] += hi.y, z[6] += hi.z, z[7] += hi.w;
+                        }
+                    }
+                    store(z, feature, rank);
+                }
+            } else {
+                for (int c0 = 0; ok && c0 < r16; c0 += 32) {
+                    down(c0, 0);
+                    if (some && c0 + 32 >= r16) {                            // this warp has read its last column
+                        tmem_fence_before();
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(smem_addr(&acc_empty_[acc]));
+                    }
+                    asm volatile("bar.sync 1, 128;" ::: "memory");           // the four warps
+                    const int ranks = min(32, a.rank - c0), total = t.up ? kRows * (ranks / 8) : ranks * (kRows / 8);
+                    for (int j = thread; j < total; j += 128) {
+                        const int feature = t.up ? j % kRows : j % (kRows / 8) * 8, rank = t.up ? j / kRows * 8 : j / (kRows / 8);
+                        if (t.m0 + feature >= features) continue;
+                        const float *src = out + rank * kGradLd + feature;
+                        float z[8];
+                        if (t.up) {
+#pragma unroll
+                            for (int l = 0; l < 8; ++l) z[l] = src[l * kGradLd];
+                        } else {
+                            const float4 lo = *reinterpret_cast<const float4 *>(src), hi = *reinterpret_cast<const float4 *>(src + 4);
+                            z[0] = lo.x, z[1] = lo.y, z[2] = lo.z, z[3] = lo.w, z[4] = hi.x, z[5] = hi.y, z[6] = hi.z, z[7] = hi.w;
+                        }
+                        store(z, feature, c0 + rank);
+                    }
+                    asm volatile("bar.sync 1, 128;" ::: "memory");           // `out` may be written again
                 }
             }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) z[j] *= scale;
-            uint16_t *dst = up ? a.dup + ((size_t)adapter * a.N + m0 + feature) * a.rank + rank : a.ddown + ((size_t)adapter * a.rank + rank) * a.H + m0 + feature;
-            *reinterpret_cast<uint4 *>(dst) = pack8(z);
         }
     }
     __syncwarp();
     tmem_fence_before();
     __syncthreads();
-    if (split > 1) cluster_sync();
+    if (SPLIT) cluster_sync();                                               // the others' reads come from this CTA's memory
     tmem_fence_after();
-    if (warp == 1) tmem_free<1>(tmem, a.columns);
+    if (warp == 0) tmem_free<1>(tmem, 2 * a.columns);
     if (threadIdx.x == 0 && gave_up_ && a.status) atomicOr(a.status, EP_STATUS_TIMEOUT);
 }
 
@@ -599,21 +721,6 @@ int check_adapter(const ep_adapter_t *m)
         m->out_features >= (1 << 24))
         return EP_ERR_INVALID_ARG;
     if (m->rank < 8 || m->rank % 8 || m->rank > kMaxRank || m->num_adapters < 1 || m->num_adapters > kMaxExperts) return EP_ERR_INVALID_ARG;
-    return EP_OK;
-}
-
-// A bf16 array [rows][inner], read four single rows at a time.
-int make_gather_map(TensorMapEncode encode, CUtensorMap *map, const void *base, uint64_t inner, uint64_t rows)
-{
-    const cuuint64_t dim[2] = {inner, rows}, stride[1] = {inner * 2};
-    const cuuint32_t box[2] = {64, 1}, step[2] = {1, 1};
-    const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(base), dim, stride, box, step,
-                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    if (r != CUDA_SUCCESS) {
-        note_cuda_error(cudaErrorInvalidValue);
-        return EP_ERR_CUDA;
-    }
     return EP_OK;
 }
 
@@ -655,10 +762,9 @@ int launch_rank(const ep_adapter_t &m, TensorMapEncode encode, RankArgs a, const
     const uint64_t H = m.in_features, N = m.out_features, r = m.rank, A = m.num_adapters;
     a.rows = m.rows, a.entries = m.entries, a.rank = m.rank, a.A = m.num_adapters;
     a.in = BACK ? m.out_features : m.in_features, a.out_features = BACK ? m.in_features : m.out_features;
-    CUtensorMap map_in, map_first, map_second;
-    int rc = make_gather_map(encode, &map_in, in, a.in, m.rows);
-    if (rc == EP_OK)
-        rc = BACK ? make_map(encode, &map_first, up, r, N, A, 64) : make_map(encode, &map_first, down, H, r, A, (uint32_t)((r + 15) & ~15));
+    a.in_rows = static_cast<const uint16_t *>(in);
+    CUtensorMap map_first, map_second;
+    int rc = BACK ? make_map(encode, &map_first, up, r, N, A, 64) : make_map(encode, &map_first, down, H, r, A, (uint32_t)((r + 15) & ~15));
     if (rc == EP_OK) {
         if (!a.out) map_second = map_first;
         else rc = BACK ? make_map(encode, &map_second, down, H, r, A, 64) : make_map(encode, &map_second, up, r, N, A, 128);
@@ -668,7 +774,7 @@ int launch_rank(const ep_adapter_t &m, TensorMapEncode encode, RankArgs a, const
     const int stages = (a.in + kTileK - 1) / kTileK;
     a.split = 1;
     while (a.split < kMaxCluster && tiles * a.split * 2 <= 2 * 148 && stages >= 4 * a.split) a.split *= 2;
-    return launch_cluster(rank_kernel<BACK>, ready, tiles, a.split, kThreads, kRankSmem, kRankSmem, stream, a, map_in, map_first, map_second);
+    return launch_cluster(rank_kernel<BACK>, ready, tiles, a.split, kThreads, kRankSmem, kRankSmem, stream, a, map_first, map_second);
 }
 
 size_t up256(size_t n) { return (n + 255) & ~size_t(255); }
@@ -739,34 +845,29 @@ extern "C" int ep_adapter_matmul_backward(const ep_adapter_t *m, const void *dy,
         if (rc != EP_OK) return rc;
     }
     if (!ddown && !dup) return EP_OK;
-    CUtensorMap map_x, map_dmid, map_dy, map_mid;
-    if (ddown) {
-        rc = make_gather_map(encode, &map_x, x, H, m->rows);
-        if (rc == EP_OK) rc = make_gather_map(encode, &map_dmid, dmid, r, m->entries);
-        if (rc != EP_OK) return rc;
-    }
-    if (dup) {
-        rc = make_gather_map(encode, &map_dy, dy, N, m->rows);
-        if (rc == EP_OK) rc = make_gather_map(encode, &map_mid, mid, r, m->entries);
-        if (rc != EP_OK) return rc;
-    }
-    if (!ddown) map_x = map_dy, map_dmid = map_mid;
-    if (!dup) map_dy = map_x, map_mid = map_dmid;
     GradArgs g = {};
     g.offsets = adapter_offsets, g.index = row_index, g.scale = scale, g.status = status;
+    g.x = static_cast<const uint16_t *>(x), g.dmid = static_cast<const uint16_t *>(dmid);
+    g.dy = static_cast<const uint16_t *>(dy), g.mid = static_cast<const uint16_t *>(mid);
     g.ddown = static_cast<uint16_t *>(ddown), g.dup = static_cast<uint16_t *>(dup);
     g.rows = m->rows, g.entries = m->entries, g.H = m->in_features, g.N = m->out_features, g.rank = m->rank, g.A = m->num_adapters;
     g.tiles_down = ddown ? (m->in_features + kRows - 1) / kRows : 0;
     g.tiles_up = dup ? (m->out_features + kRows - 1) / kRows : 0;
     const int64_t items = (int64_t)g.A * (g.tiles_down + g.tiles_up), average = m->entries / m->num_adapters / kTileK;
+    if (items * kMaxCluster >= (int64_t(1) << 31)) return EP_ERR_INVALID_ARG;
+    g.items = (int)items;
     g.split = 1;
     while (g.split < kMaxCluster && items * g.split * 2 <= 2 * 148 && average >= 4 * g.split) g.split *= 2;
-    const int r16 = (m->rank + 15) & ~15, chunks = (m->rank + 63) / 64, stage = kLines + chunks * 8192;
+    const int r16 = (m->rank + 15) & ~15, chunks = (m->rank + 63) / 64, stage = kLines + chunks * 8192, table = (g.A + 1) * 4;
     g.columns = r16 <= 32 ? 32 : r16 <= 64 ? 64 : 128;
-    // three or four CTAs on an SM; those of a cluster take over half of it (see the rank kernel)
-    g.stages = chunks == 1 ? 3 : 3;
-    int smem = 1024 + g.stages * stage;
-    if (g.split > 1) smem = kRankSmem, g.stages = (smem - 1024) / stage < kGradStages ? (smem - 1024) / stage : kGradStages;
-    static std::atomic<uint64_t> ready{0};
-    return launch_cluster(adapter_grad_kernel, ready, items, g.split, kGradThreads, smem, kRankSmem, stream, g, map_x, map_dmid, map_dy, map_mid);
+    static std::atomic<uint64_t> ready[2];
+    if (g.split > 1) {                                                       // over half of an SM's memory each: see the rank kernel
+        g.stages = (kRankSmem - 1024 - table) / stage;
+        if (g.stages > kGradStages) g.stages = kGradStages;
+        return launch_cluster(adapter_grad_kernel<true>, ready[1], items, g.split, kGradThreads, kRankSmem, kRankSmem, stream, g);
+    }
+    const int most = kRankSmem + kGradOutBytes + (kMaxExperts + 1) * 4;
+    g.stages = 3;
+    const int smem = 1024 + g.stages * stage + kGradOutBytes + table, per_sm = smem <= kRankSmem ? 2 : 1;
+    return launch_cluster(adapter_grad_kernel<false>, ready[0], items < per_sm * 148 ? items : per_sm * 148, 1, kGradThreads, smem, most, stream, g);
 }
