@@ -53,6 +53,11 @@ __device__ __forceinline__ uint32_t swizzled(int line, int piece) { return line 
 // What this thread wrote to shared memory is there for the tensor cores.
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
+__device__ __forceinline__ void store_cluster(uint32_t addr, const uint4 &v)
+{
+    asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+
 // A box on its way into L2.
 __device__ __forceinline__ void tma_prefetch(const CUtensorMap *map, int x, int y, int z)
 {
@@ -63,16 +68,25 @@ __device__ __forceinline__ void tma_prefetch(const CUtensorMap *map, int x, int 
 
 constexpr int kEpilogueWarps = 8;
 constexpr int kThreads = 64 + 32 * kEpilogueWarps;
-// Shared memory, from a 1024-byte boundary. The stages of the first product take 96 KB (a stage: 128 lines of rows and 64 or 128 lines
-// of weights); afterwards the same memory holds the row operand of the second (16 or 32 KB), the epilogue's buffers (32 KB) and the
-// weights' blocks (16 KB each). 15 KB behind them are for what the CTAs of a cluster exchange, if it fits there. Two CTAs
+// Shared memory. The stages of the first product take 96 KB (a stage: 128 lines of rows and 64 or 128 lines of weights); afterwards
+// the same memory holds the row operand of the second (16 or 32 KB), the epilogue's buffers (16 KB for every 32 rows) and one to five
+// blocks of the weights (16 KB each); barriers and tables follow. What the CTAs of a cluster exchange lies in the epilogue's buffers. Two CTAs
 // fit on an SM, so that one reads while the other writes; 113 KB each also keep a CTA of the experts' products, which holds all of the
 // tensor memory, from sharing an SM with one of a cluster: two clusters that each wait for the other's would wait for good.
-constexpr int kRingBytes = 96 * 1024, kTailBytes = 15 * 1024 - 512;
-constexpr int kStageWords = 32 * 32, kStageBytes = kEpilogueWarps * kStageWords * 4;      // an epilogue warp's 32 rows x 32 columns
-constexpr int kRankSmem = 1024 + kRingBytes + kTailBytes;
-constexpr int kMaxStages = 4, kMaxUnits = 3;
+constexpr int kRingBytes = 96 * 1024, kAreaBytes = 112 * 1024;
+constexpr int kBufferBytes = 32 * 128;    // an epilogue warp's 32 rows x 64 columns of bf16; two of them
+constexpr int kMaxStages = 4, kMaxUnits = 5;
 constexpr int kLag = 2;                   // stages a loader has in flight behind the one it asks for
+
+struct RankTables {
+    uint64_t full[kMaxStages], empty[kMaxStages], unit_full[kMaxUnits], unit_empty[kMaxUnits], mid_full, mid_ready, acc_full[2], acc_empty[2],
+        ex_full;
+    uint32_t tmem_slot;
+    int gave_up, warp_sum[kThreads / 32], where[3];
+    int row_of[kRows];
+};
+constexpr int kRankSmem = kAreaBytes + 1024;
+static_assert(sizeof(RankTables) <= 1024, "two CTAs per SM");
 
 struct RankArgs {
     const int32_t *offsets;               // [A+1]
@@ -84,7 +98,7 @@ struct RankArgs {
     uint16_t *mid;                        // [entries][rank], may be NULL
     long long rows, entries;
     const uint16_t *in_rows;              // [rows][in]
-    int in, out_features, rank, A, split;
+    int in, out_features, rank, A, split, width;      // width: rows of a tile at most
 };
 
 __device__ __forceinline__ void unpack8(const uint4 &v, float (&f)[8])
@@ -102,13 +116,10 @@ template <bool BACK>
 __global__ void __launch_bounds__(kThreads, 2)
 rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_first, const __grid_constant__ CUtensorMap map_second)
 {
-    extern __shared__ char raw[];
-    __shared__ uint64_t full_[kMaxStages], empty_[kMaxStages], unit_full_[kMaxUnits], unit_empty_[kMaxUnits], mid_full_, mid_ready_, acc_full_[2],
-        acc_empty_[2], ex_full_, ex_read_;
-    __shared__ uint32_t tmem_slot;
-    __shared__ int gave_up_, warp_sum[kThreads / 32], where[3];
-    __shared__ int row_of[kRows];
-    volatile int *gave_up = &gave_up_;
+    extern __shared__ __align__(1024) char area[];                           // no static shared memory: it would push the area off its boundary
+    RankTables &tab = *reinterpret_cast<RankTables *>(area + kAreaBytes);
+    int *const warp_sum = tab.warp_sum, *const where = tab.where, *const row_of = tab.row_of;
+    volatile int *gave_up = &tab.gave_up;
 
     const int warp = __shfl_sync(kFullMask, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const int split = a.split, part = split > 1 ? (int)cluster_rank() : 0;
@@ -123,7 +134,7 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_first, con
         const int first = begin;
         for (int i = from; i < to; ++i) {
             const int end = segment_bound(__ldg(a.offsets + i + 1), a.entries);
-            sum += quotient_up(max(0, end - begin), kRows);
+            sum += quotient_up(max(0, end - begin), a.width);
             begin = end;
         }
         int scan = sum;
@@ -139,7 +150,7 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_first, con
             begin = first;
             for (int i = from; i < to; ++i) {
                 const int end = segment_bound(__ldg(a.offsets + i + 1), a.entries), count = max(0, end - begin);
-                const int pieces = quotient_up(count, kRows);
+                const int pieces = quotient_up(count, a.width);
                 if (tile < run + pieces) {
                     const int width = (quotient_up(count, pieces) + 3) & ~3, piece = tile - run;
                     where[0] = i;
@@ -161,28 +172,25 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_first, con
     const int all_k = (a.in + kTileK - 1) / kTileK, k_from = all_k * part / split, k_to = all_k * (part + 1) / split;
     const int blocks = a.out ? (a.out_features + kBlockColumns - 1) / kBlockColumns : 0;
     const int stage_bytes = kLines + chunks * 8192, stages = kRingBytes / stage_bytes;
-    const int units = (kRingBytes - kStageBytes) / kLines - chunks;
     const int loaders = min(kEpilogueWarps, (m + 3) / 4), quarters = (m + 31) / 32;        // warps that bring rows; quarters of the lanes with rows
-    const int ex_ld = r16 + 4;
-    const bool ex_small = m * ex_ld * 4 <= kTailBytes;
-    const uint32_t ring = (smem_addr(raw) + 1023) & ~1023u;
-    char *const ring_ptr = raw + (ring - smem_addr(raw));
-    const uint32_t s_base = ring, unit_base = ring + chunks * kLines + kStageBytes;
-    char *const stage_ptr = ring_ptr + chunks * kLines;
-    float *const exchange = reinterpret_cast<float *>(ex_small ? ring_ptr + kRingBytes : stage_ptr);
+    const int units = kAreaBytes / kLines - chunks - quarters;
+    const uint32_t ring = smem_addr(area), unit_base = ring + (chunks + quarters) * kLines;
+    char *const buffers = area + chunks * kLines;
+    float *const exchange = reinterpret_cast<float *>(buffers);              // [m][r16], 16-byte pieces turned so that neither axis meets a bank twice
+    const int ex_turn = r16 % 32 == 0 ? 7 : 6;
+    const auto ex_at = [&](int row, int piece) { return row * r16 + ((piece ^ (ex_turn == 7 ? row & 7 : (row & 6) >> 1)) << 2); };
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kMaxStages; ++s) bar_init(smem_addr(&full_[s]), 1 + loaders), bar_init(smem_addr(&empty_[s]), 1);
-        for (int s = 0; s < kMaxUnits; ++s) bar_init(smem_addr(&unit_full_[s]), 1), bar_init(smem_addr(&unit_empty_[s]), 1);
-        for (int s = 0; s < 2; ++s) bar_init(smem_addr(&acc_full_[s]), 1), bar_init(smem_addr(&acc_empty_[s]), 2 * quarters);
-        bar_init(smem_addr(&mid_full_), 1);
-        bar_init(smem_addr(&mid_ready_), kEpilogueWarps);
-        bar_init(smem_addr(&ex_full_), split * kEpilogueWarps);
-        bar_init(smem_addr(&ex_read_), split * kEpilogueWarps);
-        gave_up_ = 0;
+        for (int s = 0; s < kMaxStages; ++s) bar_init(smem_addr(&tab.full[s]), 1 + loaders), bar_init(smem_addr(&tab.empty[s]), 1);
+        for (int s = 0; s < kMaxUnits; ++s) bar_init(smem_addr(&tab.unit_full[s]), 1), bar_init(smem_addr(&tab.unit_empty[s]), 1);
+        for (int s = 0; s < 2; ++s) bar_init(smem_addr(&tab.acc_full[s]), 1), bar_init(smem_addr(&tab.acc_empty[s]), 2 * quarters);
+        bar_init(smem_addr(&tab.mid_full), 1);
+        bar_init(smem_addr(&tab.mid_ready), split * kEpilogueWarps);
+        bar_init(smem_addr(&tab.ex_full), split * kEpilogueWarps);
+        tab.gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 1) tmem_alloc<1>(smem_addr(&tmem_slot), 2 * kBlockColumns);
+    if (warp == 1) tmem_alloc<1>(smem_addr(&tab.tmem_slot), 2 * kBlockColumns);
     for (int i = threadIdx.x; i < kRows; i += kThreads) {
         int row = -1;
         if (i < m) {
@@ -199,8 +207,8 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_first, con
     __syncthreads();
     tmem_fence_after();
     pdl_trigger();
-    const uint32_t tmem = tmem_slot;
-    const uint32_t full0 = smem_addr(full_), empty0 = smem_addr(empty_), unit_full0 = smem_addr(unit_full_), unit_empty0 = smem_addr(unit_empty_);
+    const uint32_t tmem = tab.tmem_slot;
+    const uint32_t full0 = smem_addr(tab.full), empty0 = smem_addr(tab.empty), unit_full0 = smem_addr(tab.unit_full), unit_empty0 = smem_addr(tab.unit_empty);
 
     if (warp == 0 && elect_one()) {
         // ---- weights
@@ -238,8 +246,7 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_first, con
             }
         } else if (blocks) {
             // ---- the second weights, once the ring's memory is free
-            ok = bar_wait(smem_addr(&mid_full_), 0, gave_up);
-            if (ok && split > 1 && !ex_small) ok = bar_wait<true>(smem_addr(&ex_read_), 0, gave_up);
+            ok = bar_wait(smem_addr(&tab.mid_full), 0, gave_up);
             int u = 0, uphase = 1, usent = 0;
             for (int b = part; ok && b < blocks; b += split)
                 for (int c = 0; c < chunks; ++c) {
@@ -278,28 +285,29 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_first, con
             mma_commit<1>(empty0 + 8 * s);
             if (++s == stages) s = 0, phase ^= 1;
         }
-        if (ok) mma_commit<1>(smem_addr(&mid_full_));
+        if (ok) mma_commit<1>(smem_addr(&tab.mid_full));
         if (ok && blocks) {
-            ok = bar_wait(smem_addr(&mid_ready_), 0, gave_up);
+            ok = bar_wait<true>(smem_addr(&tab.mid_ready), 0, gave_up);
+            fence_async();                                                   // what the cluster's other CTAs wrote, too
             tmem_fence_after();
             const uint32_t idesc2 = instr_desc(kRows, kBlockColumns, false, BACK);
             int u = 0, uphase = 0, used = 0;
             for (int b = part; ok && b < blocks; b += split, ++used) {
                 const int acc = used & 1;
-                if (!(ok = bar_wait(smem_addr(&acc_empty_[acc]), ((used >> 1) & 1) ^ 1, gave_up))) break;
+                if (!(ok = bar_wait(smem_addr(&tab.acc_empty[acc]), ((used >> 1) & 1) ^ 1, gave_up))) break;
                 tmem_fence_after();
                 for (int c = 0; c < chunks; ++c) {
                     if (!(ok = bar_wait(unit_full0 + 8 * u, uphase, gave_up))) break;
                     tmem_fence_after();
                     const uint32_t at = unit_base + u * kLines;
-                    const uint64_t da = desc_k_major(s_base + c * kLines), db = BACK ? desc_mn_major(at) : desc_k_major(at);
+                    const uint64_t da = desc_k_major(ring + c * kLines), db = BACK ? desc_mn_major(at) : desc_k_major(at);
                     const int steps = min(4, (r16 - 64 * c) / 16);
                     for (int j = 0; j < steps; ++j)
                         mma_bf16<1>(tmem + acc * kBlockColumns, da + j * 2, db + j * (BACK ? 128 : 2), idesc2, c > 0 || j > 0);
                     mma_commit<1>(unit_empty0 + 8 * u);
                     if (++u == units) u = 0, uphase ^= 1;
                 }
-                if (ok) mma_commit<1>(smem_addr(&acc_full_[acc]));
+                if (ok) mma_commit<1>(smem_addr(&tab.acc_full[acc]));
             }
         }
     } else if (warp >= 2) {
@@ -307,6 +315,12 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_first, con
         const int my_row = q * 32 + lane;                                    // a warp reaches the lanes 32 (warp mod 4) .. + 31
         const float scale = a.scale ? __ldg(a.scale + adapter) : 1.f, mid_scale = BACK ? scale : 1.f, out_scale = BACK ? 1.f : scale;
         bool ok = true;
+        if (a.base && quarters == 1 && (blocks - 1) / split < 16)            // few rows: their base into L2, under the first product
+            for (int i = thread; i < m * ((blocks - part + split - 1) / split) * 2; i += 32 * kEpilogueWarps) {
+                const int line = i % m, col = (part + i / m / 2 * split) * kBlockColumns + (i / m & 1) * 64;
+                if (row_of[line] >= 0 && col < a.out_features)
+                    asm volatile("prefetch.global.L2 [%0];" ::"l"(a.base + (size_t)row_of[line] * a.out_features + col));
+            }
         if (warp - 2 < loaders) {
             // ---- rows into the ring: eight lanes a row's line, four rows a warp, every 32 rows
             const int line = 4 * (warp - 2) + (lane >> 3), piece = lane & 7, n_k = k_to - k_from;
@@ -340,32 +354,17 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_first, con
             }
             copy_wait<0>();
         }
-        // the first block's base, under what follows: lane l of a pass holds 8 columns of row 8 i + l / 4
-        int rows[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) rows[i] = row_of[q * 32 + 8 * i + (lane >> 2)];
-        uint4 r[2][4];
-        const auto request = [&](int b, int h, int i) {
-            const int col = b * kBlockColumns + half * 64 + h * 32 + (lane & 3) * 8;
-            r[h][i] = make_uint4(0u, 0u, 0u, 0u);
-            if (a.base && rows[i] >= 0 && b < blocks && col < a.out_features)     // `base` may be the output: an ordinary load
-                r[h][i] = *reinterpret_cast<const uint4 *>(a.base + (size_t)rows[i] * a.out_features + col);
-        };
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) request(part, h, i);
-        ok = ok && bar_wait(smem_addr(&mid_full_), 0, gave_up);
+        ok = ok && bar_wait(smem_addr(&tab.mid_full), 0, gave_up);
         tmem_fence_after();
         // 8 columns of a row, rounded: the second product's operand, and `mid`
-        const auto put = [&](int row, int col, float (&f)[8], bool store) {
+        const auto rounded = [&](int row, int col, float (&f)[8]) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[i] *= mid_scale;
             const uint4 v = pack8(f);
-            *reinterpret_cast<uint4 *>(ring_ptr + (col >> 6) * kLines + row * 128 + ((((col & 63) >> 3) ^ (row & 7)) << 4)) = v;
-            if (store && a.mid && row < m && col < a.rank)
-                *reinterpret_cast<uint4 *>(a.mid + (size_t)(entry0 + row) * a.rank + col) = v;
+            if (a.mid && row < m && col < a.rank) *reinterpret_cast<uint4 *>(a.mid + (size_t)(entry0 + row) * a.rank + col) = v;
+            return v;
         };
+        const auto operand_at = [&](int row, int col) { return (col >> 6) * kLines + swizzled(row, (col & 63) >> 3); };
         if (ok) {
             for (int c0 = half * 32; c0 < r16; c0 += 64) {
                 uint32_t v[32];
@@ -377,48 +376,70 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_first, con
                             float f[8];
 #pragma unroll
                             for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(v[8 * j + i]);
-                            put(my_row, c0 + 8 * j, f, true);
+                            *reinterpret_cast<uint4 *>(area + operand_at(my_row, c0 + 8 * j)) = rounded(my_row, c0 + 8 * j, f);
                         } else if (my_row < m) {
-                            uint4 *dst = reinterpret_cast<uint4 *>(exchange + my_row * ex_ld + c0 + 8 * j);
-                            dst[0] = make_uint4(v[8 * j], v[8 * j + 1], v[8 * j + 2], v[8 * j + 3]);
-                            dst[1] = make_uint4(v[8 * j + 4], v[8 * j + 5], v[8 * j + 6], v[8 * j + 7]);
+                            const int piece = c0 / 4 + 2 * j;
+                            *reinterpret_cast<uint4 *>(exchange + ex_at(my_row, piece)) = make_uint4(v[8 * j], v[8 * j + 1], v[8 * j + 2], v[8 * j + 3]);
+                            *reinterpret_cast<uint4 *>(exchange + ex_at(my_row, piece + 1)) =
+                                make_uint4(v[8 * j + 4], v[8 * j + 5], v[8 * j + 6], v[8 * j + 7]);
                         }
                     }
             }
         }
         if (split > 1 && ok) {
-            // ---- the parts of all CTAs, added in their order by each of them
+            // ---- the parts of all CTAs: each CTA adds a share of the elements, in the order of the CTAs, and tells all of them
             __syncwarp();
-            if (lane < split) bar_arrive_cluster_release(in_cta(smem_addr(&ex_full_), lane));
-            ok = bar_wait<true>(smem_addr(&ex_full_), 0, gave_up);
+            if (lane < split) bar_arrive_cluster_release(in_cta(smem_addr(&tab.ex_full), lane));
+            ok = bar_wait<true>(smem_addr(&tab.ex_full), 0, gave_up);
             const int groups = r16 / 8;
-            for (int i = thread; ok && i < m * groups; i += 32 * kEpilogueWarps) {
+            for (int i = thread * split + part; ok && i < m * groups; i += 32 * kEpilogueWarps * split) {
                 const int row = i / groups, col = i % groups * 8;
-                const uint32_t from = smem_addr(exchange + row * ex_ld + col);
+                const uint32_t lo = smem_addr(exchange + ex_at(row, col / 4)), hi = smem_addr(exchange + ex_at(row, col / 4 + 1));
                 float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                for (int s = 0; s < split; ++s) {
-                    const float4 lo = load_cluster(in_cta(from, s)), hi = load_cluster(in_cta(from, s) + 16);
-                    f[0] += lo.x, f[1] += lo.y, f[2] += lo.z, f[3] += lo.w, f[4] += hi.x, f[5] += hi.y, f[6] += hi.z, f[7] += hi.w;
+                for (int s = 0; s < split; s += 2) {                         // split is a power of two; four reads under way
+                    const float4 l0 = load_cluster(in_cta(lo, s)), h0 = load_cluster(in_cta(hi, s));
+                    const float4 l1 = load_cluster(in_cta(lo, s + 1)), h1 = load_cluster(in_cta(hi, s + 1));
+                    f[0] += l0.x, f[1] += l0.y, f[2] += l0.z, f[3] += l0.w, f[4] += h0.x, f[5] += h0.y, f[6] += h0.z, f[7] += h0.w;
+                    f[0] += l1.x, f[1] += l1.y, f[2] += l1.z, f[3] += l1.w, f[4] += h1.x, f[5] += h1.y, f[6] += h1.z, f[7] += h1.w;
                 }
-                put(row, col, f, part == 0);
-            }
-            __syncwarp();
-            if (!ex_small) {
-                if (lane < split) bar_arrive_cluster_release(in_cta(smem_addr(&ex_read_), lane));
-                ok = ok && bar_wait<true>(smem_addr(&ex_read_), 0, gave_up);
+                const uint4 v = rounded(row, col, f);
+                const uint32_t to = ring + operand_at(row, col);
+                for (int s = 0; s < split; ++s) store_cluster(in_cta(to, s), v);
             }
         }
         fence_async();
         tmem_fence_before();
         __syncwarp();
-        if (lane == 0) bar_arrive_cluster_release(smem_addr(&mid_ready_));
-        // ---- blocks of the output; a block's base is replaced by the next one's as it is used
-        float *stage = reinterpret_cast<float *>(stage_ptr) + (warp - 2) * kStageWords;
+        if (lane < split) bar_arrive_cluster_release(in_cta(smem_addr(&tab.mid_ready), lane));
+        if (split > 1) ok = ok && bar_wait<true>(smem_addr(&tab.mid_ready), 0, gave_up);     // all have read: the buffers are free
+        // ---- blocks of the output. A warp has 32 rows and 64 columns of one: whole lines of `base` come into its buffer in the
+        // background, a block ahead; there each lane adds its row's accumulators and rounds, and whole lines go out.
+        char *const buffer = buffers + (2 * q + half) * 2 * kBufferBytes;
+        const uint32_t buffer_at = smem_addr(buffer);
+        const int piece = lane & 7;
+        int line_row[8];                                                     // eight lanes a row's line, four rows a pass
+#pragma unroll
+        for (int i = 0; i < 8; ++i) line_row[i] = row_of[q * 32 + 4 * i + (lane >> 3)];
+        const auto request = [&](int b, int which) {
+            const int col = b * kBlockColumns + half * 64 + piece * 8;
+            if (a.base && b < blocks && col < a.out_features)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (line_row[i] >= 0)                                    // `base` may be the output: not through the read-only path
+                        copy16(buffer_at + which * kBufferBytes + swizzled(4 * i + (lane >> 3), piece),
+                               a.base + (size_t)line_row[i] * a.out_features + col, true);
+            copy_group();
+        };
         int used = 0;
+        if (q < quarters) request(part, 0);
         for (int b = part; ok && q < quarters && b < blocks; b += split, ++used) {
             const int acc = used & 1;
-            if (!(ok = bar_wait(smem_addr(&acc_full_[acc]), (used >> 1) & 1, gave_up))) break;
+            request(b + split, acc ^ 1);
+            copy_wait<1>();
+            __syncwarp();
+            if (!(ok = bar_wait(smem_addr(&tab.acc_full[acc]), (used >> 1) & 1, gave_up))) break;
             tmem_fence_after();
+            char *const mine = buffer + acc * kBufferBytes;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 uint32_t v[32];
@@ -426,30 +447,29 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_first, con
                 if (h == 1) {
                     tmem_fence_before();
                     __syncwarp();
-                    if (lane == 0) bar_arrive_cluster(smem_addr(&acc_empty_[acc]));
+                    if (lane == 0) bar_arrive(smem_addr(&tab.acc_empty[acc]));
                 }
-                __syncwarp();
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    *reinterpret_cast<uint4 *>(stage + lane * 32 + ((j ^ (lane & 7)) << 2)) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-                __syncwarp();
-                const int col = b * kBlockColumns + half * 64 + h * 32 + (lane & 3) * 8;
+                for (int j = 0; j < 4; ++j) {
+                    uint4 *at = reinterpret_cast<uint4 *>(mine + swizzled(lane, 4 * h + j));
+                    float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                    if (a.base) unpack8(*at, f);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int row = 8 * i + (lane >> 2), j = (lane & 3) * 2;
-                    const float4 lo = *reinterpret_cast<const float4 *>(stage + row * 32 + ((j ^ (row & 7)) << 2));
-                    const float4 hi = *reinterpret_cast<const float4 *>(stage + row * 32 + (((j + 1) ^ (row & 7)) << 2));
-                    const float z[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-                    float f[8];
-                    unpack8(r[h][i], f);
-                    request(b + split, h, i);
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) f[k] = fmaf(out_scale, z[k], f[k]);
-                    if (rows[i] >= 0 && col < a.out_features)
-                        *reinterpret_cast<uint4 *>(a.out + (size_t)rows[i] * a.out_features + col) = pack8(f);
+                    for (int k = 0; k < 8; ++k) f[k] = fmaf(out_scale, __uint_as_float(v[8 * j + k]), f[k]);
+                    *at = pack8(f);
                 }
             }
+            __syncwarp();
+            const int col = b * kBlockColumns + half * 64 + piece * 8;
+            if (col < a.out_features)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (line_row[i] >= 0)
+                        *reinterpret_cast<uint4 *>(a.out + (size_t)line_row[i] * a.out_features + col) =
+                            *reinterpret_cast<const uint4 *>(mine + swizzled(4 * i + (lane >> 3), piece));
+            __syncwarp();                                                    // the buffer may be written again
         }
+        copy_wait<0>();
     }
     __syncwarp();
     tmem_fence_before();
@@ -457,7 +477,7 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_first, con
     if (split > 1) cluster_sync();                                           // the others' reads come from this CTA's memory
     tmem_fence_after();
     if (warp == 1) tmem_free<1>(tmem, 2 * kBlockColumns);
-    if (threadIdx.x == 0 && gave_up_ && a.status) atomicOr(a.status, EP_STATUS_TIMEOUT);
+    if (threadIdx.x == 0 && tab.gave_up && a.status) atomicOr(a.status, EP_STATUS_TIMEOUT);
 }
 
 // ---- the gradient kernel ------------------------------------------------------------------------------------------
@@ -770,10 +790,18 @@ int launch_rank(const ep_adapter_t &m, TensorMapEncode encode, RankArgs a, const
         else rc = BACK ? make_map(encode, &map_second, down, H, r, A, 64) : make_map(encode, &map_second, up, r, N, A, 128);
     }
     if (rc != EP_OK) return rc;
-    const int64_t tiles = m.entries / kRows + (m.entries < m.num_adapters ? m.entries : m.num_adapters);      // at most
+    // At most this many tiles of `width` rows; two CTAs per SM. Clusters while they fit at once, then narrower tiles up to that number.
+    const int64_t adapters = m.entries < m.num_adapters ? m.entries : m.num_adapters, slots = 2 * 148;
+    int64_t tiles = m.entries / kRows + adapters;
     const int stages = (a.in + kTileK - 1) / kTileK;
     a.split = 1;
-    while (a.split < kMaxCluster && tiles * a.split * 2 <= 2 * 148 && stages >= 4 * a.split) a.split *= 2;
+    while (a.split < kMaxCluster && tiles * a.split * 2 <= slots && stages >= 4 * a.split) a.split *= 2;
+    a.width = kRows;
+    if (slots / a.split > adapters) {
+        const int64_t even = (m.entries + slots / a.split - adapters - 1) / (slots / a.split - adapters);
+        if (even > 64 && even < kRows) a.width = (int)(even + 3) / 4 * 4;
+    }
+    tiles = m.entries / a.width + adapters;
     return launch_cluster(rank_kernel<BACK>, ready, tiles, a.split, kThreads, kRankSmem, kRankSmem, stream, a, map_first, map_second);
 }
 
@@ -868,6 +896,6 @@ extern "C" int ep_adapter_matmul_backward(const ep_adapter_t *m, const void *dy,
     }
     const int most = kRankSmem + kGradOutBytes + (kMaxExperts + 1) * 4;
     g.stages = 3;
-    const int smem = 1024 + g.stages * stage + kGradOutBytes + table, per_sm = smem <= kRankSmem ? 2 : 1;
+    const int smem = 1024 + g.stages * stage + kGradOutBytes + table, per_sm = smem <= kRankSmem - 1024 ? 2 : 1;
     return launch_cluster(adapter_grad_kernel<false>, ready[0], items < per_sm * 148 ? items : per_sm * 148, 1, kGradThreads, smem, most, stream, g);
 }
