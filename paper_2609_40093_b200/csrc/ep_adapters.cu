@@ -37,7 +37,7 @@ __device__ __forceinline__ int segment_bound(int32_t v, long long entries) { ret
 // 16 bytes from global to shared memory, in the background; zeros where `there` is false.
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there)
 {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16u : 0u) : "memory");
+    asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16u : 0u) : "memory");
 }
 __device__ __forceinline__ void copy_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 // All groups of this thread but the last N have landed.
@@ -56,6 +56,22 @@ __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.
 __device__ __forceinline__ void store_cluster(uint32_t addr, const uint4 &v)
 {
     asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+
+// 16 accumulator columns of this warp's 32 lanes, and the wait for them: nothing reads v in between.
+__device__ __forceinline__ void tmem_request16(uint32_t addr, uint32_t (&v)[16])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
+                   "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+                 : "r"(addr)
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_wait16(uint32_t (&v)[16])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]),
+                   "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])::"memory");
 }
 
 // A box on its way into L2.
@@ -417,17 +433,20 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_first, con
         char *const buffer = buffers + (2 * q + half) * 2 * kBufferBytes;
         const uint32_t buffer_at = smem_addr(buffer);
         const int piece = lane & 7;
-        int line_row[8];                                                     // eight lanes a row's line, four rows a pass
+        long long line_at[8];                                                // eight lanes a row's line, four rows a pass; < 0: no row
 #pragma unroll
-        for (int i = 0; i < 8; ++i) line_row[i] = row_of[q * 32 + 4 * i + (lane >> 3)];
+        for (int i = 0; i < 8; ++i) {
+            const int row = row_of[q * 32 + 4 * i + (lane >> 3)];
+            line_at[i] = row < 0 ? -1 : (long long)row * a.out_features + half * 64 + piece * 8;
+        }
         const auto request = [&](int b, int which) {
-            const int col = b * kBlockColumns + half * 64 + piece * 8;
-            if (a.base && b < blocks && col < a.out_features)
+            const int col = b * kBlockColumns;
+            if (a.base && b < blocks && col + half * 64 + piece * 8 < a.out_features) {
+                const uint32_t to = buffer_at + which * kBufferBytes;
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (line_row[i] >= 0)                                    // `base` may be the output: not through the read-only path
-                        copy16(buffer_at + which * kBufferBytes + swizzled(4 * i + (lane >> 3), piece),
-                               a.base + (size_t)line_row[i] * a.out_features + col, true);
+                for (int i = 0; i < 8; ++i)                                  // `base` may be the output: not through the read-only path
+                    if (line_at[i] >= 0) copy16(to + swizzled(4 * i + (lane >> 3), piece), a.base + line_at[i] + col, true);
+            }
             copy_group();
         };
         int used = 0;
@@ -440,33 +459,44 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_first, con
             if (!(ok = bar_wait(smem_addr(&tab.acc_full[acc]), (used >> 1) & 1, gave_up))) break;
             tmem_fence_after();
             char *const mine = buffer + acc * kBufferBytes;
+            // 16 columns at a time, the next ones on their way
+            const uint32_t from = tmem + (uint32_t(q * 32) << 16) + acc * kBlockColumns + half * 64;
+            uint32_t v[2][16];
+            tmem_request16(from, v[0]);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                uint32_t v[32];
-                tmem_load32(tmem + (uint32_t(q * 32) << 16) + acc * kBlockColumns + half * 64 + h * 32, v);
-                if (h == 1) {
+            for (int c = 0; c < 4; ++c) {
+                tmem_wait16(v[c & 1]);
+                if (c < 3) {
+                    tmem_request16(from + 16 * (c + 1), v[(c + 1) & 1]);
+                } else {
                     tmem_fence_before();
                     __syncwarp();
                     if (lane == 0) bar_arrive(smem_addr(&tab.acc_empty[acc]));
                 }
+                uint4 *at[2];
+                float f[2][8];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    uint4 *at = reinterpret_cast<uint4 *>(mine + swizzled(lane, 4 * h + j));
-                    float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                    if (a.base) unpack8(*at, f);
+                for (int j = 0; j < 2; ++j) {
+                    at[j] = reinterpret_cast<uint4 *>(mine + swizzled(lane, 2 * c + j));
+                    unpack8(a.base ? *at[j] : make_uint4(0u, 0u, 0u, 0u), f[j]);
+                }
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) f[k] = fmaf(out_scale, __uint_as_float(v[8 * j + k]), f[k]);
-                    *at = pack8(f);
+                for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) f[j][k] = fmaf(out_scale, __uint_as_float(v[c & 1][8 * j + k]), f[j][k]);
+                    *at[j] = pack8(f[j]);
                 }
             }
             __syncwarp();
-            const int col = b * kBlockColumns + half * 64 + piece * 8;
-            if (col < a.out_features)
+            const int col = b * kBlockColumns;
+            if (col + half * 64 + piece * 8 < a.out_features) {
+                uint4 line[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) line[i] = *reinterpret_cast<const uint4 *>(mine + swizzled(4 * i + (lane >> 3), piece));
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    if (line_row[i] >= 0)
-                        *reinterpret_cast<uint4 *>(a.out + (size_t)line_row[i] * a.out_features + col) =
-                            *reinterpret_cast<const uint4 *>(mine + swizzled(4 * i + (lane >> 3), piece));
+                    if (line_at[i] >= 0) *reinterpret_cast<uint4 *>(a.out + line_at[i] + col) = line[i];
+            }
             __syncwarp();                                                    // the buffer may be written again
         }
         copy_wait<0>();
@@ -484,10 +514,11 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_first, con
 
 // One warp issues the products, four bring entries, four empty the accumulators, of which there are two, so that an item's results
 // leave under the next one's products. SPLIT: a cluster shares an item, one item per cluster.
-constexpr int kGradThreads = 32 * 9;
+constexpr int kGradLoaders = 8;
+constexpr int kGradThreads = 32 * (5 + kGradLoaders);
 constexpr int kGradLd = kRows + 4;        // accumulators on their way out: [rank][128 features]
-constexpr int kGradStages = 4;
-constexpr int kGradOutBytes = 32 * kGradLd * 4;
+constexpr int kGradColumns = 16;          // of them at a time
+constexpr int kGradOutBytes = kGradColumns * kGradLd * 4;
 
 struct GradArgs {
     const int32_t *offsets, *index;
@@ -499,15 +530,15 @@ struct GradArgs {
     int H, N, rank, A, split;
     int tiles_down, tiles_up;             // feature tiles of an adapter's ddown (0: not wanted) and dup
     int items;                            // A * (tiles_down + tiles_up)
-    int stages, columns;                  // columns of tensor memory of one accumulator
+    int columns;                          // of tensor memory, one accumulator
 };
 
-template <bool SPLIT>
-__global__ void __launch_bounds__(kGradThreads)
+template <bool SPLIT, int STAGES>
+__global__ void __launch_bounds__(kGradThreads, 2)
 adapter_grad_kernel(const GradArgs a)
 {
     extern __shared__ char raw[];
-    __shared__ uint64_t full_[kGradStages], empty_[kGradStages], acc_full_[2], acc_empty_[2], ex_full_;
+    __shared__ uint64_t full_[STAGES], empty_[STAGES], acc_full_[2], acc_empty_[2], ex_full_;
     __shared__ uint32_t tmem_slot;
     __shared__ int gave_up_;
     volatile int *gave_up = &gave_up_;
@@ -515,7 +546,8 @@ adapter_grad_kernel(const GradArgs a)
     const int warp = __shfl_sync(kFullMask, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const int split = SPLIT ? a.split : 1, part = SPLIT ? (int)cluster_rank() : 0;
     const int tiles = a.tiles_down + a.tiles_up;
-    const int chunks = (a.rank + 63) / 64, r16 = (a.rank + 15) & ~15, stages = a.stages;
+    const int chunks = (a.rank + 63) / 64, r16 = (a.rank + 15) & ~15;
+    constexpr int stages = STAGES, kLag = STAGES - 1;
     const int stage_bytes = kLines + chunks * 8192;
     const uint32_t ring = (smem_addr(raw) + 1023) & ~1023u;
     char *const ring_ptr = raw + (ring - smem_addr(raw));
@@ -523,7 +555,7 @@ adapter_grad_kernel(const GradArgs a)
     int *const bound = reinterpret_cast<int *>(ring_ptr + stages * stage_bytes + (SPLIT ? 0 : kGradOutBytes));
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kGradStages; ++s) bar_init(smem_addr(&full_[s]), 4), bar_init(smem_addr(&empty_[s]), 1);
+        for (int s = 0; s < stages; ++s) bar_init(smem_addr(&full_[s]), kGradLoaders), bar_init(smem_addr(&empty_[s]), 1);
         for (int s = 0; s < 2; ++s) bar_init(smem_addr(&acc_full_[s]), 1), bar_init(smem_addr(&acc_empty_[s]), 4);
         bar_init(smem_addr(&ex_full_), split * 4);
         gave_up_ = 0;
@@ -557,10 +589,11 @@ adapter_grad_kernel(const GradArgs a)
         return t;
     };
 
-    if (warp >= 1 && warp < 5) {
-        // ---- entries into the ring: 16 lanes bring 128 features of one and its piece of the rank, every eighth entry
-        const int thread = threadIdx.x - 32, piece = thread & 15, line = thread >> 4, half = piece >> 3;
-        const uint32_t at = half * 8192 + swizzled(line, piece & 7);
+    if (warp >= 5) {
+        // ---- entries into the ring: 16 lanes bring 128 features of one and its piece of the rank, every 16th entry. Pieces that no
+        // result depends on (features and ranks behind the last) are not brought; entries behind the segment's end are zeros.
+        const int thread = threadIdx.x - 32 * 5, piece = thread & 15, line = thread >> 4;
+        const uint32_t at = (piece >> 3) * 8192 + swizzled(line, piece & 7);
         int s = 0, phase = 1, done = 0, waiting = 0;
         bool ok = true;
         const auto arrive = [&] {
@@ -571,33 +604,46 @@ adapter_grad_kernel(const GradArgs a)
         };
         for (int i = first; ok && i < a.items; i += step) {
             const Item t = item_at(i);
-            const uint16_t *rows = t.up ? a.dy : a.x, *ranks = t.up ? a.mid : a.dmid;
-            const int features = t.up ? a.N : a.H, col = t.m0 + piece * 8;
-            const bool live = col < features, ranked = piece * 8 < r16, real = piece * 8 < a.rank;
-            rows += live ? col : 0;
-            ranks += real ? piece * 8 : 0;
-            int next[8];
+            const int features = t.up ? a.N : a.H;
+            const bool live = t.m0 + piece * 8 < features, real = piece * 8 < a.rank;
+            const uint16_t *const rows = (t.up ? a.dy : a.x) + (live ? t.m0 + piece * 8 : 0);
+            const uint16_t *const ranks = (t.up ? a.mid : a.dmid) + (real ? piece * 8 : 0) + (size_t)t.begin * a.rank;
+            const bool plain = a.index == nullptr;
+            const size_t row_step = (size_t)16 * features, rank_step = (size_t)16 * a.rank;
+            int next[4];
             const auto look = [&](int k) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int e = k * kTileK + line + 8 * j;
-                    next[j] = e < t.n ? (a.index ? __ldg(a.index + t.begin + e) : t.begin + e) : -1;
+                for (int j = 0; j < 4; ++j) {
+                    const int e = k * kTileK + line + 16 * j;
+                    next[j] = e < t.n ? (plain ? t.begin + e : __ldg(a.index + t.begin + e)) : -1;
                 }
             };
-            if (t.k_from < t.k_to) look(t.k_from);
+            if (!plain && t.k_from < t.k_to) look(t.k_from);
             for (int k = t.k_from; k < t.k_to; ++k) {
                 if (!(ok = __all_sync(kFullMask, bar_wait(empty0 + 8 * s, phase, gave_up)))) break;
                 const uint32_t dst = ring + s * stage_bytes + at;
+                const int e = k * kTileK + line;
+                const uint16_t *rank = ranks + (size_t)e * a.rank;
+                if (plain && (k + 1) * (long long)kTileK <= t.n) {           // a whole stage of rows one behind the other
+                    const uint16_t *row = rows + (size_t)(t.begin + e) * features;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int e = k * kTileK + line + 8 * j, row = next[j];
-                    const bool there = row >= 0 && row < a.rows;             // others are zeros, in both operands
-                    if (a.status && !there && e < t.n && piece == 0) atomicOr(a.status, EP_STATUS_BAD_INDEX);
-                    copy16(dst + j * 1024, rows + (there ? (size_t)row * features : 0), there && live);
-                    if (ranked) copy16(dst + kLines + j * 1024, ranks + (there ? (size_t)(t.begin + e) * a.rank : 0), there && real);
+                    for (int j = 0; j < 4; ++j, row += row_step, rank += rank_step) {
+                        if (live) copy16(dst + j * 2048, row, true);
+                        if (real) copy16(dst + kLines + j * 2048, rank, true);
+                    }
+                } else {
+                    if (plain) look(k);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j, rank += rank_step) {
+                        const int row = next[j];
+                        const bool there = row >= 0 && row < a.rows;         // others are zeros, in both operands
+                        if (a.status && !there && e + 16 * j < t.n && piece == 0) atomicOr(a.status, EP_STATUS_BAD_INDEX);
+                        if (live) copy16(dst + j * 2048, rows + (there ? (size_t)row * features : 0), there);
+                        if (real) copy16(dst + kLines + j * 2048, there ? rank : ranks, there);
+                    }
+                    if (!plain && k + 1 < t.k_to) look(k + 1);
                 }
                 copy_group();
-                if (k + 1 < t.k_to) look(k + 1);
                 if (++s == stages) s = 0, phase ^= 1;
                 if (waiting == kLag) copy_wait<kLag>(), arrive(); else ++waiting;
             }
@@ -628,9 +674,9 @@ adapter_grad_kernel(const GradArgs a)
             if (ok) mma_commit<1>(smem_addr(&acc_full_[acc]));
             ++used;
         }
-    } else if (warp >= 5) {
+    } else if (warp >= 1) {
         // ---- accumulators out, through shared memory; SPLIT: added up over the CTAs that share them
-        const int q = warp & 3, thread = threadIdx.x - 32 * 5;
+        const int q = warp & 3, thread = threadIdx.x - 32;
         int used = 0;
         bool ok = true;
         for (int i = first; ok && i < a.items; i += step) {
@@ -643,18 +689,15 @@ adapter_grad_kernel(const GradArgs a)
                 tmem_fence_after();
                 ++used;
             }
-            // columns [c0, c0 + 32) of the accumulator, or zeros, into `out`, from its column `to` on
-            const auto down = [&](int c0, int to) {
-                uint32_t v[32];
+            uint32_t v[32];
+            // columns [c0, c0 + 32) of the accumulator, or zeros
+            const auto load = [&](int c0) {
                 if (some) {
                     tmem_load32(tmem + (uint32_t(q * 32) << 16) + acc * a.columns + c0, v);
                 } else {
 #pragma unroll
                     for (int c = 0; c < 32; ++c) v[c] = 0u;
                 }
-#pragma unroll
-                for (int c = 0; c < 32; ++c)
-                    if (c0 + c < r16) out[(to + c) * kGradLd + q * 32 + lane] = __uint_as_float(v[c]);
             };
             // 8 results: ddown, 8 features of a rank; dup, 8 ranks of a feature
             const auto store = [&](float (&z)[8], int feature, int rank) {
@@ -665,7 +708,12 @@ adapter_grad_kernel(const GradArgs a)
                 *reinterpret_cast<uint4 *>(dst) = pack8(z);
             };
             if (SPLIT) {
-                for (int c0 = 0; ok && c0 < r16; c0 += 32) down(c0, c0);
+                for (int c0 = 0; ok && c0 < r16; c0 += 32) {
+                    load(c0);
+#pragma unroll
+                    for (int c = 0; c < 32; ++c)
+                        if (c0 + c < r16) out[(c0 + c) * kGradLd + q * 32 + lane] = __uint_as_float(v[c]);
+                }
                 __syncwarp();
                 if (ok && lane < split) bar_arrive_cluster_release(in_cta(smem_addr(&ex_full_), lane));
                 ok = ok && bar_wait<true>(smem_addr(&ex_full_), 0, gave_up);
@@ -694,29 +742,35 @@ adapter_grad_kernel(const GradArgs a)
                 }
             } else {
                 for (int c0 = 0; ok && c0 < r16; c0 += 32) {
-                    down(c0, 0);
+                    load(c0);
                     if (some && c0 + 32 >= r16) {                            // this warp has read its last column
                         tmem_fence_before();
                         __syncwarp();
                         if (lane == 0) bar_arrive(smem_addr(&acc_empty_[acc]));
                     }
-                    asm volatile("bar.sync 1, 128;" ::: "memory");           // the four warps
-                    const int ranks = min(32, a.rank - c0), total = t.up ? kRows * (ranks / 8) : ranks * (kRows / 8);
-                    for (int j = thread; j < total; j += 128) {
-                        const int feature = t.up ? j % kRows : j % (kRows / 8) * 8, rank = t.up ? j / kRows * 8 : j / (kRows / 8);
-                        if (t.m0 + feature >= features) continue;
-                        const float *src = out + rank * kGradLd + feature;
-                        float z[8];
-                        if (t.up) {
 #pragma unroll
-                            for (int l = 0; l < 8; ++l) z[l] = src[l * kGradLd];
-                        } else {
-                            const float4 lo = *reinterpret_cast<const float4 *>(src), hi = *reinterpret_cast<const float4 *>(src + 4);
-                            z[0] = lo.x, z[1] = lo.y, z[2] = lo.z, z[3] = lo.w, z[4] = hi.x, z[5] = hi.y, z[6] = hi.z, z[7] = hi.w;
+                    for (int h = 0; h < 2; ++h) {
+                        if (c0 + kGradColumns * h >= a.rank) break;
+#pragma unroll
+                        for (int c = 0; c < kGradColumns; ++c) out[c * kGradLd + q * 32 + lane] = __uint_as_float(v[kGradColumns * h + c]);
+                        asm volatile("bar.sync 1, 128;" ::: "memory");       // the four warps
+                        const int ranks = min(kGradColumns, a.rank - c0 - kGradColumns * h), total = t.up ? kRows * (ranks / 8) : ranks * (kRows / 8);
+                        for (int j = thread; j < total; j += 128) {
+                            const int feature = t.up ? j % kRows : j % (kRows / 8) * 8, rank = t.up ? j / kRows * 8 : j / (kRows / 8);
+                            if (t.m0 + feature >= features) continue;
+                            const float *src = out + rank * kGradLd + feature;
+                            float z[8];
+                            if (t.up) {
+#pragma unroll
+                                for (int l = 0; l < 8; ++l) z[l] = src[l * kGradLd];
+                            } else {
+                                const float4 lo = *reinterpret_cast<const float4 *>(src), hi = *reinterpret_cast<const float4 *>(src + 4);
+                                z[0] = lo.x, z[1] = lo.y, z[2] = lo.z, z[3] = lo.w, z[4] = hi.x, z[5] = hi.y, z[6] = hi.z, z[7] = hi.w;
+                            }
+                            store(z, feature, c0 + kGradColumns * h + rank);
                         }
-                        store(z, feature, c0 + rank);
+                        asm volatile("bar.sync 1, 128;" ::: "memory");       // `out` may be written again
                     }
-                    asm volatile("bar.sync 1, 128;" ::: "memory");           // `out` may be written again
                 }
             }
         }
@@ -888,14 +942,13 @@ extern "C" int ep_adapter_matmul_backward(const ep_adapter_t *m, const void *dy,
     while (g.split < kMaxCluster && items * g.split * 2 <= 2 * 148 && average >= 4 * g.split) g.split *= 2;
     const int r16 = (m->rank + 15) & ~15, chunks = (m->rank + 63) / 64, stage = kLines + chunks * 8192, table = (g.A + 1) * 4;
     g.columns = r16 <= 32 ? 32 : r16 <= 64 ? 64 : 128;
-    static std::atomic<uint64_t> ready[2];
+    static std::atomic<uint64_t> ready[4];
+    const int fixed = 1024 + kGradOutBytes + table;                          // beside the stages
     if (g.split > 1) {                                                       // over half of an SM's memory each: see the rank kernel
-        g.stages = (kRankSmem - 1024 - table) / stage;
-        if (g.stages > kGradStages) g.stages = kGradStages;
-        return launch_cluster(adapter_grad_kernel<true>, ready[1], items, g.split, kGradThreads, kRankSmem, kRankSmem, stream, g);
+        if (chunks == 1) return launch_cluster(adapter_grad_kernel<true, 4>, ready[0], items, g.split, kGradThreads, kRankSmem, kRankSmem, stream, g);
+        return launch_cluster(adapter_grad_kernel<true, 6>, ready[1], items, g.split, kGradThreads, fixed + 6 * stage, 222 * 1024, stream, g);
     }
-    const int most = kRankSmem + kGradOutBytes + (kMaxExperts + 1) * 4;
-    g.stages = 3;
-    const int smem = 1024 + g.stages * stage + kGradOutBytes + table, per_sm = smem <= kRankSmem - 1024 ? 2 : 1;
-    return launch_cluster(adapter_grad_kernel<false>, ready[0], items < per_sm * 148 ? items : per_sm * 148, 1, kGradThreads, smem, most, stream, g);
+    if (chunks == 1 && fixed + 4 * stage <= kRankSmem - 1024)                // two on an SM
+        return launch_cluster(adapter_grad_kernel<false, 4>, ready[2], items < 296 ? items : 296, 1, kGradThreads, fixed + 4 * stage, kRankSmem, stream, g);
+    return launch_cluster(adapter_grad_kernel<false, 6>, ready[3], items < 148 ? items : 148, 1, kGradThreads, fixed + 6 * stage, 222 * 1024, stream, g);
 }
