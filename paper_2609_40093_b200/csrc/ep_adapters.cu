@@ -74,10 +74,10 @@ __device__ __forceinline__ void tmem_wait16(uint32_t (&v)[16])
                    "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])::"memory");
 }
 
-// A box on its way into L2.
-__device__ __forceinline__ void tma_prefetch(const CUtensorMap *map, int x, int y, int z)
+// Bytes (a multiple of 16, from a 16-byte boundary) on their way into L2.
+__device__ __forceinline__ void l2_prefetch(const void *p, uint32_t bytes)
 {
-    asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];" ::"l"(map), "r"(x), "r"(y), "r"(z) : "memory");
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
 }
 
 // ---- the rank kernel ----------------------------------------------------------------------------------------------
@@ -113,7 +113,7 @@ struct RankArgs {
     uint16_t *out;                        // [rows][out], may be NULL: the first product alone
     uint16_t *mid;                        // [entries][rank], may be NULL
     long long rows, entries;
-    const uint16_t *in_rows;              // [rows][in]
+    const uint16_t *in_rows, *second;     // [rows][in]; the second product's weights
     int in, out_features, rank, A, split, width;      // width: rows of a tile at most
 };
 
@@ -187,8 +187,10 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_first, con
     const int chunks = (a.rank + 63) / 64, r16 = (a.rank + 15) & ~15;
     const int all_k = (a.in + kTileK - 1) / kTileK, k_from = all_k * part / split, k_to = all_k * (part + 1) / split;
     const int blocks = a.out ? (a.out_features + kBlockColumns - 1) / kBlockColumns : 0;
+    const int b_from = (int)((long long)blocks * part / split), b_to = (int)((long long)blocks * (part + 1) / split);
     const int stage_bytes = kLines + chunks * 8192, stages = kRingBytes / stage_bytes;
     const int loaders = min(kEpilogueWarps, (m + 3) / 4), quarters = (m + 31) / 32;        // warps that bring rows; quarters of the lanes with rows
+    const bool narrow = quarters == 1;                                       // each quarter of the lanes holds the same rows, see below
     const int units = kAreaBytes / kLines - chunks - quarters;
     const uint32_t ring = smem_addr(area), unit_base = ring + (chunks + quarters) * kLines;
     char *const buffers = area + chunks * kLines;
@@ -199,7 +201,7 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_first, con
     if (threadIdx.x == 0) {
         for (int s = 0; s < kMaxStages; ++s) bar_init(smem_addr(&tab.full[s]), 1 + loaders), bar_init(smem_addr(&tab.empty[s]), 1);
         for (int s = 0; s < kMaxUnits; ++s) bar_init(smem_addr(&tab.unit_full[s]), 1), bar_init(smem_addr(&tab.unit_empty[s]), 1);
-        for (int s = 0; s < 2; ++s) bar_init(smem_addr(&tab.acc_full[s]), 1), bar_init(smem_addr(&tab.acc_empty[s]), 2 * quarters);
+        for (int s = 0; s < 2; ++s) bar_init(smem_addr(&tab.acc_full[s]), 1), bar_init(smem_addr(&tab.acc_empty[s]), narrow ? kEpilogueWarps : 2 * quarters);
         bar_init(smem_addr(&tab.mid_full), 1);
         bar_init(smem_addr(&tab.mid_ready), split * kEpilogueWarps);
         bar_init(smem_addr(&tab.ex_full), split * kEpilogueWarps);
@@ -228,16 +230,6 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_first, con
 
     if (warp == 0 && elect_one()) {
         // ---- weights
-        if (blocks && (blocks - 1) / split < 16)                             // few blocks: nobody else has brought them into L2
-            for (int b = part; b < blocks; b += split)
-                for (int c = 0; c < chunks; ++c) {
-                    if (BACK) {
-                        tma_prefetch(&map_second, b * kBlockColumns, 64 * c, adapter);
-                        tma_prefetch(&map_second, b * kBlockColumns + 64, 64 * c, adapter);
-                    } else {
-                        tma_prefetch(&map_second, 64 * c, b * kBlockColumns, adapter);
-                    }
-                }
         const uint32_t bytes = (uint32_t)(BACK ? chunks * 8192 : r16 * 128);
         int s = 0, phase = 1, sent = 0;
         bool ok = true;
@@ -251,6 +243,14 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_first, con
                 tma_load<1>(dst, &map_first, k * kTileK, 0, adapter, full);
             }
             ++sent;
+            if (b_to > b_from && b_to - b_from <= 16 && sent == min(stages, k_to - k_from)) {
+                // few blocks a CTA: nobody else has brought the second weights into L2
+                const int col = b_from * kBlockColumns, cols = min(b_to * kBlockColumns, a.out_features) - col;
+                if (BACK)
+                    for (int j = 0; j < a.rank; ++j) l2_prefetch(a.second + ((size_t)adapter * a.rank + j) * a.out_features + col, cols * 2);
+                else
+                    l2_prefetch(a.second + ((size_t)adapter * a.out_features + col) * a.rank, cols * a.rank * 2);
+            }
             if (++s == stages) s = 0, phase ^= 1;
         }
         if (!ok) {                                                           // gave up: let the copies in flight land
@@ -264,7 +264,7 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_first, con
             // ---- the second weights, once the ring's memory is free
             ok = bar_wait(smem_addr(&tab.mid_full), 0, gave_up);
             int u = 0, uphase = 1, usent = 0;
-            for (int b = part; ok && b < blocks; b += split)
+            for (int b = b_from; ok && b < b_to; ++b)
                 for (int c = 0; c < chunks; ++c) {
                     if (!(ok = bar_wait(unit_empty0 + 8 * u, uphase, gave_up))) break;
                     const uint32_t full = unit_full0 + 8 * u, dst = unit_base + u * kLines;
@@ -308,7 +308,7 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_first, con
             tmem_fence_after();
             const uint32_t idesc2 = instr_desc(kRows, kBlockColumns, false, BACK);
             int u = 0, uphase = 0, used = 0;
-            for (int b = part; ok && b < blocks; b += split, ++used) {
+            for (int b = b_from; ok && b < b_to; ++b, ++used) {
                 const int acc = used & 1;
                 if (!(ok = bar_wait(smem_addr(&tab.acc_empty[acc]), ((used >> 1) & 1) ^ 1, gave_up))) break;
                 tmem_fence_after();
@@ -331,12 +331,9 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_first, con
         const int my_row = q * 32 + lane;                                    // a warp reaches the lanes 32 (warp mod 4) .. + 31
         const float scale = a.scale ? __ldg(a.scale + adapter) : 1.f, mid_scale = BACK ? scale : 1.f, out_scale = BACK ? 1.f : scale;
         bool ok = true;
-        if (a.base && quarters == 1 && (blocks - 1) / split < 16)            // few rows: their base into L2, under the first product
-            for (int i = thread; i < m * ((blocks - part + split - 1) / split) * 2; i += 32 * kEpilogueWarps) {
-                const int line = i % m, col = (part + i / m / 2 * split) * kBlockColumns + (i / m & 1) * 64;
-                if (row_of[line] >= 0 && col < a.out_features)
-                    asm volatile("prefetch.global.L2 [%0];" ::"l"(a.base + (size_t)row_of[line] * a.out_features + col));
-            }
+        if (a.base && narrow && thread < m && b_to > b_from && row_of[thread] >= 0)       // few rows: their base into L2, under the first product
+            l2_prefetch(a.base + (size_t)row_of[thread] * a.out_features + b_from * kBlockColumns,
+                        (min(b_to * kBlockColumns, a.out_features) - b_from * kBlockColumns) * 2);
         if (warp - 2 < loaders) {
             // ---- rows into the ring: eight lanes a row's line, four rows a warp, every 32 rows
             const int line = 4 * (warp - 2) + (lane >> 3), piece = lane & 7, n_k = k_to - k_from;
@@ -392,7 +389,13 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_first, con
                             float f[8];
 #pragma unroll
                             for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(v[8 * j + i]);
-                            *reinterpret_cast<uint4 *>(area + operand_at(my_row, c0 + 8 * j)) = rounded(my_row, c0 + 8 * j, f);
+                            const uint4 w = rounded(my_row, c0 + 8 * j, f);
+                            if (!narrow) {
+                                *reinterpret_cast<uint4 *>(area + operand_at(my_row, c0 + 8 * j)) = w;
+                            } else if (q == 0) {
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4 *>(area + operand_at(32 * i + lane, c0 + 8 * j)) = w;
+                            }
                         } else if (my_row < m) {
                             const int piece = c0 / 4 + 2 * j;
                             *reinterpret_cast<uint4 *>(exchange + ex_at(my_row, piece)) = make_uint4(v[8 * j], v[8 * j + 1], v[8 * j + 2], v[8 * j + 3]);
@@ -420,7 +423,12 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_first, con
                 }
                 const uint4 v = rounded(row, col, f);
                 const uint32_t to = ring + operand_at(row, col);
-                for (int s = 0; s < split; ++s) store_cluster(in_cta(to, s), v);
+                for (int s = 0; s < split; ++s) {
+                    store_cluster(in_cta(to, s), v);
+                    if (narrow)
+#pragma unroll
+                        for (int i = 1; i < 4; ++i) store_cluster(in_cta(to + i * 32 * 128, s), v);
+                }
             }
         }
         fence_async();
@@ -441,7 +449,7 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_first, con
         }
         const auto request = [&](int b, int which) {
             const int col = b * kBlockColumns;
-            if (a.base && b < blocks && col + half * 64 + piece * 8 < a.out_features) {
+            if (a.base && b < b_to && col + half * 64 + piece * 8 < a.out_features) {
                 const uint32_t to = buffer_at + which * kBufferBytes;
 #pragma unroll
                 for (int i = 0; i < 8; ++i)                                  // `base` may be the output: not through the read-only path
@@ -450,10 +458,10 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_first, con
             copy_group();
         };
         int used = 0;
-        if (q < quarters) request(part, 0);
-        for (int b = part; ok && q < quarters && b < blocks; b += split, ++used) {
+        if (q < quarters && !narrow) request(b_from, 0);
+        for (int b = b_from; ok && q < quarters && !narrow && b < b_to; ++b, ++used) {
             const int acc = used & 1;
-            request(b + split, acc ^ 1);
+            request(b + 1, acc ^ 1);
             copy_wait<1>();
             __syncwarp();
             if (!(ok = bar_wait(smem_addr(&tab.acc_full[acc]), (used >> 1) & 1, gave_up))) break;
@@ -500,6 +508,44 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_first, con
             __syncwarp();                                                    // the buffer may be written again
         }
         copy_wait<0>();
+        // ... of up to 32 rows: every quarter of the lanes has them, and each of the eight warps 16 of a block's columns, straight from
+        // the accumulators: 256 rows on 64 adapters of 2048 x 8192 take 0.3 us a block so, with one quarter's two warps at work 0.9
+        if (narrow) {
+            const int row = row_of[lane], first = (q * 2 + half) * 16;
+            const long long at = row < 0 ? -1 : (long long)row * a.out_features + first;
+            uint4 r[2];
+            const auto ask = [&](int b) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int col = b * kBlockColumns + 8 * j;
+                    r[j] = make_uint4(0u, 0u, 0u, 0u);
+                    if (a.base && at >= 0 && b < b_to && col + first < a.out_features) r[j] = *reinterpret_cast<const uint4 *>(a.base + at + col);
+                }
+            };
+            ask(b_from);
+            for (int b = b_from; ok && b < b_to; ++b, ++used) {
+                const int acc = used & 1;
+                if (!(ok = bar_wait(smem_addr(&tab.acc_full[acc]), (used >> 1) & 1, gave_up))) break;
+                tmem_fence_after();
+                uint32_t v[16];
+                tmem_request16(tmem + (uint32_t(q * 32) << 16) + acc * kBlockColumns + first, v);
+                tmem_wait16(v);
+                tmem_fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(smem_addr(&tab.acc_empty[acc]));
+                float f[2][8];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) unpack8(r[j], f[j]);
+                ask(b + 1);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int col = b * kBlockColumns + 8 * j;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) f[j][k] = fmaf(out_scale, __uint_as_float(v[8 * j + k]), f[j][k]);
+                    if (at >= 0 && col + first < a.out_features) *reinterpret_cast<uint4 *>(a.out + at + col) = pack8(f[j]);
+                }
+            }
+        }
     }
     __syncwarp();
     tmem_fence_before();
@@ -610,15 +656,16 @@ adapter_grad_kernel(const GradArgs a)
             const uint16_t *const ranks = (t.up ? a.mid : a.dmid) + (real ? piece * 8 : 0) + (size_t)t.begin * a.rank;
             const bool plain = a.index == nullptr;
             const size_t row_step = (size_t)16 * features, rank_step = (size_t)16 * a.rank;
-            int next[4];
-            const auto look = [&](int k) {
+            // indexed rows are looked up two stages ahead; -1 behind the end
+            int next[2][4];
+            const auto look = [&](int k, int (&row)[4]) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int e = k * kTileK + line + 16 * j;
-                    next[j] = e < t.n ? (plain ? t.begin + e : __ldg(a.index + t.begin + e)) : -1;
+                    row[j] = k < t.k_to && e < t.n ? (plain ? t.begin + e : __ldg(a.index + t.begin + e)) : -1;
                 }
             };
-            if (!plain && t.k_from < t.k_to) look(t.k_from);
+            if (!plain) look(t.k_from, next[0]), look(t.k_from + 1, next[1]);
             for (int k = t.k_from; k < t.k_to; ++k) {
                 if (!(ok = __all_sync(kFullMask, bar_wait(empty0 + 8 * s, phase, gave_up)))) break;
                 const uint32_t dst = ring + s * stage_bytes + at;
@@ -632,16 +679,19 @@ adapter_grad_kernel(const GradArgs a)
                         if (real) copy16(dst + kLines + j * 2048, rank, true);
                     }
                 } else {
-                    if (plain) look(k);
+                    if (plain) look(k, next[0]);
+                    bool bad = false;
 #pragma unroll
                     for (int j = 0; j < 4; ++j, rank += rank_step) {
-                        const int row = next[j];
-                        const bool there = row >= 0 && row < a.rows;         // others are zeros, in both operands
-                        if (a.status && !there && e + 16 * j < t.n && piece == 0) atomicOr(a.status, EP_STATUS_BAD_INDEX);
-                        if (live) copy16(dst + j * 2048, rows + (there ? (size_t)row * features : 0), there);
+                        const unsigned row = (unsigned)next[0][j];
+                        const bool there = row < (unsigned)a.rows;           // others are zeros, in both operands
+                        bad |= !there && e + 16 * j < t.n;
+                        if (live) copy16(dst + j * 2048, rows + (there ? (size_t)row * (unsigned)features : 0), there);
                         if (real) copy16(dst + kLines + j * 2048, there ? rank : ranks, there);
+                        next[0][j] = next[1][j];
                     }
-                    if (!plain && k + 1 < t.k_to) look(k + 1);
+                    if (bad && a.status && piece == 0) atomicOr(a.status, EP_STATUS_BAD_INDEX);
+                    if (!plain) look(k + 2, next[1]);
                 }
                 copy_group();
                 if (++s == stages) s = 0, phase ^= 1;
@@ -836,7 +886,7 @@ int launch_rank(const ep_adapter_t &m, TensorMapEncode encode, RankArgs a, const
     const uint64_t H = m.in_features, N = m.out_features, r = m.rank, A = m.num_adapters;
     a.rows = m.rows, a.entries = m.entries, a.rank = m.rank, a.A = m.num_adapters;
     a.in = BACK ? m.out_features : m.in_features, a.out_features = BACK ? m.in_features : m.out_features;
-    a.in_rows = static_cast<const uint16_t *>(in);
+    a.in_rows = static_cast<const uint16_t *>(in), a.second = static_cast<const uint16_t *>(BACK ? down : up);
     CUtensorMap map_first, map_second;
     int rc = BACK ? make_map(encode, &map_first, up, r, N, A, 64) : make_map(encode, &map_first, down, H, r, A, (uint32_t)((r + 15) & ~15));
     if (rc == EP_OK) {
