@@ -53,27 +53,40 @@ struct Dropout {
         }
     }
 
-    __device__ __forceinline__ uint4 words(unsigned long long v) const
+    // The words of N vectors, round by round, so that they share a round's keys (and the first product of the step).
+    template <int N>
+    __device__ __forceinline__ void words(const unsigned long long (&v)[N], uint32_t (&w)[N][4]) const
     {
-        uint32_t c0 = (uint32_t)v, c1 = (uint32_t)(v >> 32), c2 = step, c3 = site;
+#pragma unroll
+        for (int n = 0; n < N; ++n) w[n][0] = (uint32_t)v[n], w[n][1] = (uint32_t)(v[n] >> 32), w[n][2] = step, w[n][3] = site;
 #pragma unroll
         for (uint32_t i = 0; i < 10; ++i) {
-            const unsigned long long p = (unsigned long long)c0 * 0xD2511F53u, q = (unsigned long long)c2 * 0xCD9E8D57u;
-            const uint32_t n0 = (uint32_t)(q >> 32) ^ c1 ^ (k0 + i * 0x9E3779B9u), n2 = (uint32_t)(p >> 32) ^ c3 ^ (k1 + i * 0xBB67AE85u);
-            c0 = n0, c1 = (uint32_t)q, c2 = n2, c3 = (uint32_t)p;
+            const uint32_t a = k0 + i * 0x9E3779B9u, b = k1 + i * 0xBB67AE85u;
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const unsigned long long p = (unsigned long long)w[n][0] * 0xD2511F53u, q = (unsigned long long)w[n][2] * 0xCD9E8D57u;
+                w[n][0] = (uint32_t)(q >> 32) ^ w[n][1] ^ a, w[n][1] = (uint32_t)q;
+                w[n][2] = (uint32_t)(p >> 32) ^ w[n][3] ^ b, w[n][3] = (uint32_t)p;
+            }
         }
-        return make_uint4(c0, c1, c2, c3);
+    }
+
+    // Two packed elements, 0 where the word's halves say so.
+    __device__ __forceinline__ uint32_t masked(uint32_t pair, uint32_t word) const
+    {
+        return pair & (((word << 16) >= edge ? 0x0000ffffu : 0u) | (word >= edge ? 0xffff0000u : 0u));
     }
 
     // The eight elements of vector v of the row-major array: 0 where dropped (whatever they hold), scaled elsewhere.
     __device__ __forceinline__ void apply(float (&f)[8], unsigned long long v) const
     {
-        const uint4 w = words(v);
-        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+        const unsigned long long one[1] = {v};
+        uint32_t w[1][4];
+        words(one, w);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            f[2 * i] = (u[i] << 16) >= edge && !all ? f[2 * i] * scale : 0.f;
-            f[2 * i + 1] = u[i] >= edge && !all ? f[2 * i + 1] * scale : 0.f;
+            f[2 * i] = (w[0][i] << 16) >= edge && !all ? f[2 * i] * scale : 0.f;
+            f[2 * i + 1] = w[0][i] >= edge && !all ? f[2 * i + 1] * scale : 0.f;
         }
     }
 };

@@ -19,6 +19,11 @@ namespace {
 constexpr int kBlock = 128;
 constexpr int kChunk = 8;   // rows in flight per column
 
+// CTAs per SM that the compiler leaves registers for. Left to itself it takes 125 and more where there are products, to have several
+// columns' loads under way in one thread; seven CTAs with 72 each and one column are faster (gather with products, 8192 tokens of
+// 1024 elements, 4 picks: 22.3 us with 72, 23.7 with 80, 25.5 with 64, 34.5 with 125).
+constexpr int resident(bool spread, int chunks, bool dots) { return !dots ? (spread ? 12 : 7) : chunks == 1 ? 7 : chunks == 2 ? 4 : 3; }
+
 struct RowArgs {
     const uint4 *v;             // [T] rows
     const uint4 *add;           // gather: [T] rows, may be NULL
@@ -132,10 +137,11 @@ __device__ __forceinline__ void store_dots(const RowArgs &a, const Picks &p, flo
 }
 
 template <int G, int CHUNKS, bool DOTS>
-__global__ void __launch_bounds__(kBlock)
+__global__ void __launch_bounds__(kBlock, resident(true, CHUNKS, DOTS))
 spread_rows_kernel(const RowArgs a)
 {
     const int g = threadIdx.x % G, t = blockIdx.x * (kBlock / G) + threadIdx.x / G;
+    pdl_trigger();                                                       // the next kernel's CTAs may take the places that get free
     pdl_wait();                                                          // nothing is read or written before this
     const Picks p = load_picks<true>(a, t);
     const Dropout drop(a.drop);
@@ -146,12 +152,17 @@ spread_rows_kernel(const RowArgs a)
 #pragma unroll
         for (int j = 0; j < kChunk; ++j) dot[c][j] = 0.f;
 
-    if (p.mask)
+    if (p.mask) {
+        const uint4 *const own = a.v + (size_t)t * a.vec_per_row;
+        uint4 next = make_uint4(0u, 0u, 0u, 0u);                         // without d, a column ahead
+        if (!DOTS && g < a.vec_per_row) next = ld_once(own + g);
+#pragma unroll 1
         for (int base = 0; base < a.vec_per_row; base += G) {            // trip count uniform over the warp
             const int col = base + g;
             const bool live = col < a.vec_per_row;
-            uint4 mine = make_uint4(0u, 0u, 0u, 0u);
-            if (live) mine = ld_once(a.v + (size_t)t * a.vec_per_row + col);
+            uint4 mine = next;
+            if (DOTS && live) mine = ld_once(own + col);
+            if (!DOTS && col + G < a.vec_per_row) next = ld_once(own + col + G);
             uint4 row[kChunk];
             const auto request = [&](int c) {
 #pragma unroll
@@ -187,14 +198,16 @@ spread_rows_kernel(const RowArgs a)
                 }
             }
         }
+    }
     if (DOTS) store_dots<G, CHUNKS, true>(a, p, dot, t);
 }
 
 template <int G, int CHUNKS, bool DOTS>
-__global__ void __launch_bounds__(kBlock)
+__global__ void __launch_bounds__(kBlock, resident(false, CHUNKS, DOTS))
 gather_rows_kernel(const RowArgs a)
 {
     const int g = threadIdx.x % G, t = blockIdx.x * (kBlock / G) + threadIdx.x / G;
+    pdl_trigger();
     pdl_wait();
     const Picks p = load_picks<false>(a, t);
     const Dropout drop(a.drop);
@@ -204,64 +217,96 @@ gather_rows_kernel(const RowArgs a)
 #pragma unroll
         for (int j = 0; j < kChunk; ++j) dot[c][j] = 0.f;
 
-    if (t < a.T)
-        for (int base = 0; base < a.vec_per_row; base += G) {
-            const int col = base + g;
-            const bool live = col < a.vec_per_row;
-            const size_t at = (size_t)t * a.vec_per_row + col;
-            uint4 mine = make_uint4(0u, 0u, 0u, 0u), add = mine;
-            float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const auto request = [&](uint4 &to, int k, int col) {
+        const int32_t s = __shfl_sync(kFullMask, p.slot, k);
+        if (col < a.vec_per_row && ((p.mask >> k) & 1u)) to = ld_once(a.table + (size_t)s * a.vec_per_row + col);
+    };
+    const auto fold = [&](float (&acc)[8], const float (&f)[8], float &d, const uint4 &row, int k, bool live) {
+        const float w = __shfl_sync(kFullMask, p.w, k);
+        if (live && ((p.mask >> k) & 1u)) {
+            float r[8];
+            unpack8(row, r);
 #pragma unroll
-            for (int c = 0; c < CHUNKS; ++c) {
-                uint4 row[kChunk];
-#pragma unroll
-                for (int j = 0; j < kChunk; ++j) {
-                    const int32_t s = __shfl_sync(kFullMask, p.slot, c * kChunk + j);
-                    if (live && ((p.mask >> (c * kChunk + j)) & 1u)) row[j] = ld_once(a.table + (size_t)s * a.vec_per_row + col);
-                }
-                if (c == 0 && live) {
-                    if (DOTS) mine = ld_once(a.v + at);
-                    if (a.add) add = ld_once(a.add + at);
-                }
-                float f[8];
-                if (DOTS) unpack8(mine, f);
-#pragma unroll
-                for (int j = 0; j < kChunk; ++j) {
-                    const int k = c * kChunk + j;
-                    const float w = __shfl_sync(kFullMask, p.w, k);
-                    if (live && ((p.mask >> k) & 1u)) {
-                        float r[8];
-                        unpack8(row[j], r);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            acc[i] = fmaf(w, r[i], acc[i]);
-                            if (DOTS) dot[c][j] = fmaf(f[i], r[i], dot[c][j]);
-                        }
-                    }
-                }
-            }
-            if (live && a.out) {
-                if (a.drop.state) drop.apply(acc, at);
-                if (a.add) {
-                    float r[8];
-                    unpack8(add, r);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) acc[i] += r[i];
-                }
-                st_stream(a.out + at, pack8(acc));
+            for (int i = 0; i < 8; ++i) {
+                acc[i] = fmaf(w, r[i], acc[i]);
+                if (DOTS) d = fmaf(f[i], r[i], d);
             }
         }
+    };
+    const auto finish = [&](float (&acc)[8], const uint4 &add, size_t at) {
+        if (a.drop.state) drop.apply(acc, at);
+        if (a.add) {
+            float r[8];
+            unpack8(add, r);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc[i] += r[i];
+        }
+        st_stream(a.out + at, pack8(acc));
+    };
+    if (t < a.T) {
+        const size_t first = (size_t)t * a.vec_per_row;
+        const auto request_own = [&](uint4 &mine, uint4 &add, int col) {
+            if (col < a.vec_per_row) {
+                if (DOTS) mine = ld_once(a.v + first + col);
+                if (a.add) add = ld_once(a.add + first + col);
+            }
+        };
+        uint4 row[kChunk], mine = make_uint4(0u, 0u, 0u, 0u), add = mine;
+        if (CHUNKS == 1 && !DOTS) {
+            // the next column's rows are requested half by half as this column's are used, so that loads stay in flight during the
+            // arithmetic: gradients of 4096 tokens of 2048 elements, 8 picks, 50 us without, 37 so
+            request_own(mine, add, g);
+#pragma unroll
+            for (int k = 0; k < kChunk; ++k) request(row[k], k, g);
+            for (int base = 0; base < a.vec_per_row; base += G) {
+                const int col = base + g;
+                const bool live = col < a.vec_per_row;
+                float f[8], acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                if (DOTS) unpack8(mine, f);
+                const uint4 extra = add;
+                request_own(mine, add, col + G);
+#pragma unroll
+                for (int h = 0; h < kChunk; h += 4) {
+#pragma unroll
+                    for (int k = h; k < h + 4; ++k) fold(acc, f, dot[0][k], row[k], k, live);
+#pragma unroll
+                    for (int k = h; k < h + 4; ++k) request(row[k], k, col + G);
+                }
+                if (live && a.out) finish(acc, extra, first + col);
+            }
+        } else {
+#pragma unroll 1
+            for (int base = 0; base < a.vec_per_row; base += G) {            // (unrolled, it takes 125 registers, and twice the time)
+                const int col = base + g;
+                const bool live = col < a.vec_per_row;
+                float f[8], acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                request_own(mine, add, col);
+#pragma unroll
+                for (int c = 0; c < CHUNKS; ++c) {
+#pragma unroll
+                    for (int j = 0; j < kChunk; ++j) request(row[j], c * kChunk + j, col);
+                    if (DOTS && c == 0) unpack8(mine, f);
+#pragma unroll
+                    for (int j = 0; j < kChunk; ++j) fold(acc, f, dot[c][j], row[j], c * kChunk + j, live);
+                }
+                if (live && a.out) finish(acc, add, first + col);
+            }
+        }
+    }
     if (DOTS) store_dots<G, CHUNKS, false>(a, p, dot, t);
 }
 
 template <template <int, int, bool> class Kernel, int CHUNKS, bool DOTS>
-int launch_group(const RowArgs &a, cudaStream_t stream)
+int launch_group(const RowArgs &a, bool few_columns, cudaStream_t stream)
 {
     const int vpr = a.vec_per_row;
     cudaError_t e;
+    // Threads per token: a row's columns are dealt out to more threads as there are more of them. Gather with products has a thread do one
+    // column after the other, and wants few (8192 x 1024 elements, 4 picks: 22.3 us with 128 threads, 29.3 with 64; the others 10 % and
+    // more the other way round).
     if (vpr <= 64)
         e = launch_pdl(Kernel<32, CHUNKS, DOTS>::get(), dim3(ceil_div(a.T, kBlock / 32)), dim3(kBlock), 0, stream, a);
-    else if (vpr <= 256)
+    else if (vpr < (few_columns ? 65 : 256))
         e = launch_pdl(Kernel<64, CHUNKS, DOTS>::get(), dim3(ceil_div(a.T, kBlock / 64)), dim3(kBlock), 0, stream, a);
     else
         e = launch_pdl(Kernel<128, CHUNKS, DOTS>::get(), dim3(a.T), dim3(kBlock), 0, stream, a);
@@ -270,14 +315,11 @@ int launch_group(const RowArgs &a, cudaStream_t stream)
     return EP_OK;
 }
 template <template <int, int, bool> class Kernel, bool DOTS>
-int launch_chunks(const RowArgs &a, cudaStream_t stream)
+int launch_chunks(const RowArgs &a, bool few_columns, cudaStream_t stream)
 {
-    return a.K <= 8 ? launch_group<Kernel, 1, DOTS>(a, stream) : a.K <= 16 ? launch_group<Kernel, 2, DOTS>(a, stream) : launch_group<Kernel, 4, DOTS>(a, stream);
-}
-template <template <int, int, bool> class Kernel>
-int launch_rows(const RowArgs &a, cudaStream_t stream)
-{
-    return a.dots ? launch_chunks<Kernel, true>(a, stream) : launch_chunks<Kernel, false>(a, stream);
+    return a.K <= 8    ? launch_group<Kernel, 1, DOTS>(a, few_columns, stream)
+           : a.K <= 16 ? launch_group<Kernel, 2, DOTS>(a, few_columns, stream)
+                       : launch_group<Kernel, 4, DOTS>(a, few_columns, stream);
 }
 template <int G, int CHUNKS, bool DOTS>
 struct Spread {
@@ -287,41 +329,58 @@ template <int G, int CHUNKS, bool DOTS>
 struct Gather {
     static auto get() { return gather_rows_kernel<G, CHUNKS, DOTS>; }
 };
+int launch_spread(const RowArgs &a, cudaStream_t stream)
+{
+    return a.dots ? launch_chunks<Spread, true>(a, false, stream) : launch_chunks<Spread, false>(a, false, stream);
+}
+int launch_gather(const RowArgs &a, cudaStream_t stream)
+{
+    return a.dots ? launch_chunks<Gather, true>(a, true, stream) : launch_chunks<Gather, false>(a, false, stream);
+}
 
 // ---- dropout of whole rows ----------------------------------------------------------------------------------------
 
-constexpr int kDropThreads = 256, kDropVecs = 4;
+// Bound by memory with a residual (65536 rows of 7168: 399 us, 7.1 TB/s), by the instructions of the generator without (322 us, 5.8 TB/s; a
+// vector at a time, each with its own round keys, 350). Four vectors a thread need more registers than leave enough warps (367 us), and
+// CTAs that stay and ask for the next vectors ahead were not faster (340 to 413).
+constexpr int kDropThreads = 128, kDropVecs = 3;
 
 __global__ void __launch_bounds__(kDropThreads)
 dropout_kernel(const uint4 *x, const uint4 *residual, uint4 *y, const int32_t *limit, long long rows, int vec_per_row, const DropoutArgs args)
 {
+    pdl_trigger();
     pdl_wait();
     if (limit) rows = max(0ll, min(rows, (long long)__ldg(limit)));
     const long long total = rows * vec_per_row, first = (long long)blockIdx.x * (kDropThreads * kDropVecs) + threadIdx.x;
     if (first >= total) return;
     const Dropout drop(args);
     uint4 v[kDropVecs], r[kDropVecs];
+    unsigned long long place[kDropVecs];
+    uint32_t w[kDropVecs][4];
 #pragma unroll
     for (int i = 0; i < kDropVecs; ++i) {
         const long long at = first + i * kDropThreads;
+        place[i] = at;
         if (at < total) {
             v[i] = ld_once(x + at);
             if (residual) r[i] = ld_once(residual + at);
         }
     }
+    if (args.state) drop.words(place, w);
+    const float scale = args.state ? drop.scale : 1.f;
 #pragma unroll
     for (int i = 0; i < kDropVecs; ++i) {
         const long long at = first + i * kDropThreads;
         if (at < total) {
-            float f[8];
-            unpack8(v[i], f);
-            if (args.state) drop.apply(f, at);
-            if (residual) {
-                float g[8];
-                unpack8(r[i], g);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) f[j] += g[j];
+            if (args.state) {
+                v[i] = make_uint4(drop.masked(v[i].x, w[i][0]), drop.masked(v[i].y, w[i][1]), drop.masked(v[i].z, w[i][2]), drop.masked(v[i].w, w[i][3]));
+                if (drop.all) v[i] = make_uint4(0u, 0u, 0u, 0u);
             }
+            float f[8], g[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            unpack8(v[i], f);
+            if (residual) unpack8(r[i], g);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] = fmaf(f[j], scale, g[j]);
             st_stream(y + at, pack8(f));
         }
     }
@@ -354,7 +413,7 @@ extern "C" int ep_sort(const ep_shape_t *shape, const void *x, const int32_t *sl
     if (!aligned16(x) || !aligned16(sorted)) return EP_ERR_INVALID_ARG;
     a.v = static_cast<const uint4 *>(x);
     a.out = static_cast<uint4 *>(sorted);
-    return launch_chunks<Spread, false>(a, static_cast<cudaStream_t>(stream));
+    return launch_spread(a, static_cast<cudaStream_t>(stream));
 }
 
 extern "C" int ep_sort_backward(const ep_shape_t *shape, const void *d_sorted, int64_t sorted_rows, const int32_t *slot, const float *weights,
@@ -373,7 +432,7 @@ extern "C" int ep_sort_backward(const ep_shape_t *shape, const void *d_sorted, i
     a.add = static_cast<const uint4 *>(dx ? add : nullptr);
     a.out = static_cast<uint4 *>(dx);
     a.dots = d_weights;
-    return launch_rows<Gather>(a, static_cast<cudaStream_t>(stream));
+    return launch_gather(a, static_cast<cudaStream_t>(stream));
 }
 
 extern "C" int ep_combine_residual(const ep_shape_t *shape, const void *out, int64_t out_rows, const int32_t *slot, const float *topk_weights,
@@ -389,7 +448,7 @@ extern "C" int ep_combine_residual(const ep_shape_t *shape, const void *out, int
     a.table = static_cast<const uint4 *>(out);
     a.add = static_cast<const uint4 *>(residual);
     a.out = static_cast<uint4 *>(y);
-    return launch_chunks<Gather, false>(a, static_cast<cudaStream_t>(stream));
+    return launch_gather(a, static_cast<cudaStream_t>(stream));
 }
 
 extern "C" int ep_combine_backward(const ep_shape_t *shape, const void *dy, const void *out, int64_t out_rows, const int32_t *slot,
@@ -407,7 +466,7 @@ extern "C" int ep_combine_backward(const ep_shape_t *shape, const void *dy, cons
     a.table = static_cast<const uint4 *>(out);
     a.out = static_cast<uint4 *>(d_out);
     a.dots = d_weights;
-    return launch_rows<Spread>(a, static_cast<cudaStream_t>(stream));
+    return launch_spread(a, static_cast<cudaStream_t>(stream));
 }
 
 extern "C" int ep_dropout(const void *x, const void *residual, void *y, int64_t rows, int32_t cols, const int32_t *limit,
