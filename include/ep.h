@@ -703,8 +703,9 @@ int ep_dropout(const void *x, const void *residual, void *y, int64_t rows, int32
  *   ddown[a] = sum dmid[i]^T x[row]                 dup[a] = scale[a] * sum dy[row]^T mid[i]
  * bf16, the shapes of x, down and up; each may be NULL and is then not computed. base
  * [rows][in_features], what else dx is made of, may be dx itself or NULL. dmid is rounded
- * to bf16 once. Adapters without entries get zero ddown and dup. No atomics: the same bits
- * every time. workspace (for ddown alone): ep_adapter_matmul_backward_workspace_bytes()
+ * to bf16 once. Adapters without entries get zero ddown and dup. No sum depends on an
+ * order of atomics: the same call gives the same bits every time (ddown alone may differ in
+ * the last bit from ddown together with dup). workspace (for ddown or dup): ep_adapter_matmul_backward_workspace_bytes()
  * bytes (device, 256-byte aligned), uninitialised.
  */
 typedef struct {

@@ -28,6 +28,8 @@ constexpr int kLines = kRows * 128;       // bytes of 128 lines
 constexpr int kBlockColumns = 128;        // output columns of one accumulator
 constexpr int kMaxRank = 128;
 constexpr int kMaxCluster = 8;
+constexpr int kGradMost = 2 * 148;        // CTAs of the gradient kernel
+constexpr int kGradFeatures = kRows;      // of an item: an accumulator's lanes
 
 // a / b rounded up, for a up to 2^31 - 1
 __device__ __forceinline__ int quotient_up(int a, int b) { return (int)(((unsigned)a + (unsigned)b - 1u) / (unsigned)b); }
@@ -104,6 +106,133 @@ struct RankTables {
 constexpr int kRankSmem = kAreaBytes + 1024;
 static_assert(sizeof(RankTables) <= 1024, "two CTAs per SM");
 
+// ---- the pieces of the gradient kernel's work -----------------------------------------------------------------------
+
+// Made by one CTA, in front of the rank kernel's or by itself: a list of pieces (a run of an adapter's stages of 64 entries each), the
+// longest first, and behind them the adapters without entries, whose gradients are zeros. The same list every time.
+constexpr int kGradBins = 16;             // lengths that are told apart
+constexpr int kGradCuts = 8;              // cuts of the longest adapter that are tried
+__device__ __forceinline__ int cut_of(int d) { return d == 0 ? 1 : (d & 1 ? 2 : 3) << ((d - 1) >> 1); }        // 1, 2, 3, 4, 6, 8, 12, 16
+
+struct GradPiece {
+    int adapter, begin, n;                // its first entry and how many it has
+    int of;                               // its pieces
+    int k_from, k_to;                     // the piece's stages
+    int number, part;                     // which piece; the adapter's first part in the workspace, if there are several
+};
+
+struct PlanArgs {
+    const int32_t *offsets;
+    long long entries;
+    int A, piece, tiles, ctas;            // piece: stages of a piece at least, where an adapter has more
+    int counters;
+    int *arrived;                         // [counters], to be zeroed
+    int *pieces;                          // [2]: pieces with entries, and all
+    GradPiece *list;                      // NULL: no plan
+};
+
+struct PlanTables {
+    int most, sum, parts[kGradCuts], warp_sum[2][kThreads / 32];
+    int bins[(kGradBins + 1) * kThreads]; // [bin][thread] pieces, then where they start
+    int stages[kMaxExperts];
+};
+
+// The exclusive sum of v over the block's threads.
+__device__ __forceinline__ int block_scan(int v, int *warp_sum)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int scan = v;
+    for (int d = 1; d < 32; d <<= 1) {
+        const int u = __shfl_up_sync(kFullMask, scan, d);
+        if (lane >= d) scan += u;
+    }
+    if (lane == 31) warp_sum[warp] = scan;
+    __syncthreads();
+    scan -= v;
+    for (int w = 0; w < warp; ++w) scan += warp_sum[w];
+    return scan;
+}
+
+__device__ void plan_pieces(const PlanArgs &a, PlanTables &tab)
+{
+    const int per = (a.A + kThreads - 1) / kThreads, from = min(a.A, (int)threadIdx.x * per), to = min(a.A, from + per), lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) tab.most = 0, tab.sum = 0;
+    if (threadIdx.x < kGradCuts) tab.parts[threadIdx.x] = 0;
+    for (int i = threadIdx.x; i < a.counters; i += kThreads) a.arrived[i] = 0;
+    for (int b = 0; b <= kGradBins; ++b) tab.bins[b * kThreads + threadIdx.x] = 0;
+    __syncthreads();
+    const auto begin_of = [&](int e) { return segment_bound(__ldg(a.offsets + e), a.entries); };
+    int most = 0, sum = 0;
+    for (int e = from; e < to; ++e) {
+        const int n = quotient_up(max(0, begin_of(e + 1) - begin_of(e)), kTileK);
+        tab.stages[e] = n;
+        most = max(most, n), sum += n;
+    }
+    most = __reduce_max_sync(kFullMask, most), sum = __reduce_add_sync(kFullMask, sum);
+    if (lane == 0 && sum) atomicMax(&tab.most, most), atomicAdd(&tab.sum, sum);
+    __syncthreads();
+    // How long a piece may be: the longest adapter's stages over 1, 2, 3, 4, 6, 8, 12 or 16, whichever should end first: with the
+    // longest piece, whose stages take some 0.6 of the usual time while others are done already, or with a CTA's share of all. A part costs
+    // about five stages, and adding parts some eight at the end.
+    for (int d = 0; d < kGradCuts; ++d) {
+        const int piece = max(a.piece, quotient_up(tab.most, cut_of(d)));
+        int split = 0;
+        for (int e = from; e < to; ++e) {
+            const int of = quotient_up(tab.stages[e], piece);
+            split += of > 1 ? of : 0;
+        }
+        split = __reduce_add_sync(kFullMask, split);
+        if (lane == 0 && split) atomicAdd(&tab.parts[d], split);
+    }
+    __syncthreads();
+    int piece = 1;
+    float best = 3.4e38f;
+    for (int d = 0; d < kGradCuts; ++d) {
+        const int longest = max(a.piece, quotient_up(tab.most, cut_of(d)));
+        const float share = ((float)tab.sum + 5.f * tab.parts[d]) * a.tiles / a.ctas;
+        const float cost = fmaxf(0.6f * min(longest, tab.most), share) + (tab.parts[d] ? 8.f : 0.f);
+        if (cost < best) best = cost, piece = longest;
+    }
+    // ---- a counting sort, the adapters of a bin in their order
+    const auto bin_of = [&](int n, int of) { return n ? kGradBins - 1 - min(kGradBins - 1, (int)((float)n * kGradBins / ((float)of * (piece + 1)))) : kGradBins; };
+    int split = 0;
+    for (int e = from; e < to; ++e) {
+        const int n = tab.stages[e], of = quotient_up(n, piece);
+        tab.bins[bin_of(n, of) * kThreads + threadIdx.x] += n ? of : 1;
+        split += of > 1 ? of : 0;
+    }
+    __syncthreads();
+    int *const run = tab.bins + threadIdx.x * (kGradBins + 1);
+    int total = 0;
+    for (int i = 0; i <= kGradBins; ++i) total += run[i];
+    int start = block_scan(total, tab.warp_sum[0]), part = block_scan(split, tab.warp_sum[1]);
+    for (int i = 0; i <= kGradBins; ++i) {
+        const int v = run[i];
+        run[i] = start;
+        start += v;
+    }
+    if (threadIdx.x == kThreads - 1) a.pieces[1] = start;
+    __syncthreads();
+    if (threadIdx.x == 0) a.pieces[0] = tab.bins[kGradBins * kThreads];
+    __syncthreads();
+    for (int e = from; e < to; ++e) {
+        const int n = tab.stages[e], of = quotient_up(n, piece), begin = begin_of(e), count = max(0, begin_of(e + 1) - begin);
+        int &at = tab.bins[bin_of(n, of) * kThreads + threadIdx.x];
+        for (int i = 0; i < max(1, of); ++i)
+            a.list[at++] = GradPiece{e, begin, count, of, of > 1 ? (int)((long long)n * i / of) : 0, of > 1 ? (int)((long long)n * (i + 1) / of) : n, i, part};
+        part += of > 1 ? of : 0;
+    }
+}
+
+__global__ void __launch_bounds__(kThreads)
+plan_kernel(const PlanArgs a)
+{
+    extern __shared__ __align__(1024) char area[];
+    pdl_trigger();
+    pdl_wait();
+    plan_pieces(a, *reinterpret_cast<PlanTables *>(area));
+}
+
 struct RankArgs {
     const int32_t *offsets;               // [A+1]
     const int32_t *index;                 // entry -> row, or NULL: entry i is row i
@@ -130,7 +259,7 @@ __device__ __forceinline__ uint4 pack8(const float (&f)[8])
 // BACK: the weights are read along the other axis (up for the first product, down for the second), and the scale goes to `mid`.
 template <bool BACK>
 __global__ void __launch_bounds__(kThreads, 2)
-rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_first, const __grid_constant__ CUtensorMap map_second)
+rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUtensorMap map_first, const __grid_constant__ CUtensorMap map_second)
 {
     extern __shared__ __align__(1024) char area[];                           // no static shared memory: it would push the area off its boundary
     RankTables &tab = *reinterpret_cast<RankTables *>(area + kAreaBytes);
@@ -139,11 +268,15 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_first, con
 
     const int warp = __shfl_sync(kFullMask, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const int split = a.split, part = split > 1 ? (int)cluster_rank() : 0;
-    const int tile = blockIdx.x / split;
+    const int tile = (int)blockIdx.x / split - (plan.list != nullptr);
 
     pdl_wait();                                                              // nothing is read or written before this
     // ---- this cluster's tile: each thread counts the tiles of a run of adapters
     if (threadIdx.x == 0) where[0] = -1;
+    if (tile < 0) {                                                          // the first cluster plans what the gradient kernel does
+        if (part == 0) plan_pieces(plan, *reinterpret_cast<PlanTables *>(area));
+        return;
+    }
     {
         const int per = (a.A + kThreads - 1) / kThreads, from = min(a.A, (int)threadIdx.x * per), to = min(a.A, from + per);
         int sum = 0, begin = from < to ? segment_bound(__ldg(a.offsets + from), a.entries) : 0;
@@ -178,7 +311,7 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_first, con
                 begin = end;
             }
         }
-        if (threadIdx.x == 0 && blockIdx.x == 0 && a.status && __ldg(a.offsets + a.A) > a.entries) atomicOr(a.status, EP_STATUS_CAPACITY);
+        if (threadIdx.x == 0 && tile == 0 && part == 0 && a.status && __ldg(a.offsets + a.A) > a.entries) atomicOr(a.status, EP_STATUS_CAPACITY);
         __syncthreads();
     }
     const int adapter = where[0], entry0 = where[1], m = where[2];
@@ -558,10 +691,15 @@ rank_kernel(const RankArgs a, const __grid_constant__ CUtensorMap map_first, con
 
 // ---- the gradient kernel ------------------------------------------------------------------------------------------
 
-// One warp issues the products, four bring entries, four empty the accumulators, of which there are two, so that an item's results
-// leave under the next one's products. SPLIT: a cluster shares an item, one item per cluster.
-constexpr int kGradLoaders = 8;
-constexpr int kGradThreads = 32 * (5 + kGradLoaders);
+// An adapter's entries are cut into pieces of about the same length, at most `piece` stages of 64; an item is a piece and 128 features of
+// ddown or dup. Items are dealt out round by round, the longest pieces first, a piece's feature tiles next to each other: what runs at
+// the same time reads the same rows (equal runs of work that end inside items balance better, but take the rows apart: dup of 32768 rows
+// on 128 adapters alike 33 us instead of 15) and has the same length. The parts of an adapter with several pieces go to the workspace in
+// fp32, and who comes last adds them in their order, so that the bits are the same every time. One warp issues the products, eight
+// bring entries, four empty the accumulators, of which there are two, so that an item's results leave under the next one's products.
+constexpr int kGradEpilogueWarps = 4;
+constexpr int grad_threads(int stages) { return 32 * (2 + kGradEpilogueWarps + 2 * stages); }     // one each for the products and the items, two for each stage
+constexpr int kGradAhead = 4;             // items that are known ahead
 constexpr int kGradLd = kRows + 4;        // accumulators on their way out: [rank][128 features]
 constexpr int kGradColumns = 16;          // of them at a time
 constexpr int kGradOutBytes = kGradColumns * kGradLd * 4;
@@ -572,152 +710,182 @@ struct GradArgs {
     const uint16_t *x, *dmid, *dy, *mid;
     uint16_t *ddown, *dup;
     int32_t *status;
+    float *parts;                         // [parts of split adapters][feature tile][r16][128]
+    int *arrived;                         // [parts of split adapters][feature tile] zeros: how many parts are there, at an adapter's first
     long long rows, entries;
-    int H, N, rank, A, split;
+    int H, N, rank, A;
     int tiles_down, tiles_up;             // feature tiles of an adapter's ddown (0: not wanted) and dup
-    int items;                            // A * (tiles_down + tiles_up)
+    int *counter;                         // 0: items handed out beyond the CTAs' first
+    const int *pieces;                    // the plan
+    const GradPiece *list;
     int columns;                          // of tensor memory, one accumulator
 };
 
-template <bool SPLIT, int STAGES>
-__global__ void __launch_bounds__(kGradThreads, 2)
-adapter_grad_kernel(const GradArgs a)
+struct GradMaps {
+    CUtensorMap x, dmid, dy, mid;         // in boxes of 64 rows
+};
+
+// An item: a piece, and which features of which product.
+struct GradItem {
+    GradPiece p;
+    int f, m0, up, more;                  // more: 0 behind the last item
+};
+
+template <int STAGES>
+__global__ void __launch_bounds__(grad_threads(STAGES), STAGES == 4 ? 2 : 1)
+adapter_grad_kernel(const GradArgs a, const __grid_constant__ GradMaps maps)
 {
     extern __shared__ char raw[];
-    __shared__ uint64_t full_[STAGES], empty_[STAGES], acc_full_[2], acc_empty_[2], ex_full_;
+    __shared__ uint64_t full_[STAGES], empty_[STAGES], acc_full_[2], acc_empty_[2], item_full_[kGradAhead], item_empty_[kGradAhead];
+    __shared__ GradItem items_[kGradAhead];
     __shared__ uint32_t tmem_slot;
-    __shared__ int gave_up_;
+    __shared__ int gave_up_, last_;
     volatile int *gave_up = &gave_up_;
 
     const int warp = __shfl_sync(kFullMask, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-    const int split = SPLIT ? a.split : 1, part = SPLIT ? (int)cluster_rank() : 0;
-    const int tiles = a.tiles_down + a.tiles_up;
     const int chunks = (a.rank + 63) / 64, r16 = (a.rank + 15) & ~15;
-    constexpr int stages = STAGES, kLag = STAGES - 1;
+    constexpr int stages = STAGES;
     const int stage_bytes = kLines + chunks * 8192;
     const uint32_t ring = (smem_addr(raw) + 1023) & ~1023u;
     char *const ring_ptr = raw + (ring - smem_addr(raw));
-    float *const out = reinterpret_cast<float *>(SPLIT ? ring_ptr : ring_ptr + stages * stage_bytes);    // SPLIT: all columns, where the stages were
-    int *const bound = reinterpret_cast<int *>(ring_ptr + stages * stage_bytes + (SPLIT ? 0 : kGradOutBytes));
+    float *const out = reinterpret_cast<float *>(ring_ptr + stages * stage_bytes);
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < stages; ++s) bar_init(smem_addr(&full_[s]), kGradLoaders), bar_init(smem_addr(&empty_[s]), 1);
-        for (int s = 0; s < 2; ++s) bar_init(smem_addr(&acc_full_[s]), 1), bar_init(smem_addr(&acc_empty_[s]), 4);
-        bar_init(smem_addr(&ex_full_), split * 4);
+        for (int s = 0; s < stages; ++s) bar_init(smem_addr(&full_[s]), 2), bar_init(smem_addr(&empty_[s]), 1);
+        for (int s = 0; s < 2; ++s) bar_init(smem_addr(&acc_full_[s]), 1), bar_init(smem_addr(&acc_empty_[s]), kGradEpilogueWarps);
+        for (int s = 0; s < kGradAhead; ++s)
+            bar_init(smem_addr(&item_full_[s]), 1), bar_init(smem_addr(&item_empty_[s]), 1 + kGradEpilogueWarps + 2 * STAGES);
         gave_up_ = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     pdl_wait();
     if (warp == 0) tmem_alloc<1>(smem_addr(&tmem_slot), 2 * a.columns);
-    for (int i = threadIdx.x; i <= a.A; i += kGradThreads) bound[i] = segment_bound(__ldg(a.offsets + i), a.entries);
     tmem_fence_before();
-    if (SPLIT) cluster_sync();
     __syncthreads();
     tmem_fence_after();
     pdl_trigger();
     const uint32_t tmem = tmem_slot, full0 = smem_addr(full_), empty0 = smem_addr(empty_);
-    const int first = blockIdx.x / split, step = gridDim.x / split;
-
-    struct Item {
-        int adapter, m0, begin, n, k_from, k_to;
-        bool up;
-    };
-    const auto item_at = [&](int i) {
-        Item t;
-        t.adapter = i / tiles;
-        const int f = i - t.adapter * tiles;
-        t.up = f >= a.tiles_down;
-        t.m0 = (t.up ? f - a.tiles_down : f) * kRows;
-        t.begin = bound[t.adapter];
-        t.n = max(0, bound[t.adapter + 1] - t.begin);
-        const int all = quotient_up(t.n, kTileK);
-        t.k_from = (int)((long long)all * part / split), t.k_to = (int)((long long)all * (part + 1) / split);
-        return t;
+    // The next item, in every warp (or thread) that works on it.
+    GradItem t;
+    int slot = 0, slot_phase = 0;
+    const auto next = [&](bool warp_wide) {
+        if (!bar_wait(smem_addr(&item_full_[slot]), slot_phase, gave_up)) return false;
+        t = items_[slot];
+        if (warp_wide) __syncwarp();
+        if (!warp_wide || lane == 0) bar_arrive(smem_addr(&item_empty_[slot]));
+        if (++slot == kGradAhead) slot = 0, slot_phase ^= 1;
+        return t.more != 0;
     };
 
-    if (warp >= 5) {
-        // ---- entries into the ring: 16 lanes bring 128 features of one and its piece of the rank, every 16th entry. Pieces that no
-        // result depends on (features and ranks behind the last) are not brought; entries behind the segment's end are zeros.
-        const int thread = threadIdx.x - 32 * 5, piece = thread & 15, line = thread >> 4;
-        const uint32_t at = (piece >> 3) * 8192 + swizzled(line, piece & 7);
-        int s = 0, phase = 1, done = 0, waiting = 0;
-        bool ok = true;
-        const auto arrive = [&] {
-            fence_async();
-            __syncwarp();
-            if (lane == 0) bar_arrive(full0 + 8 * done);
-            if (++done == stages) done = 0;
-        };
-        for (int i = first; ok && i < a.items; i += step) {
-            const Item t = item_at(i);
-            const int features = t.up ? a.N : a.H;
-            const bool live = t.m0 + piece * 8 < features, real = piece * 8 < a.rank;
-            const uint16_t *const rows = (t.up ? a.dy : a.x) + (live ? t.m0 + piece * 8 : 0);
-            const uint16_t *const ranks = (t.up ? a.mid : a.dmid) + (real ? piece * 8 : 0) + (size_t)t.begin * a.rank;
-            const bool plain = a.index == nullptr;
-            const size_t row_step = (size_t)16 * features, rank_step = (size_t)16 * a.rank;
-            // indexed rows are looked up two stages ahead; -1 behind the end
-            int next[2][4];
-            const auto look = [&](int k, int (&row)[4]) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int e = k * kTileK + line + 16 * j;
-                    row[j] = k < t.k_to && e < t.n ? (plain ? t.begin + e : __ldg(a.index + t.begin + e)) : -1;
+    if (warp == 1 + kGradEpilogueWarps) {
+        // ---- items: the first is the CTA's own, the others who comes first gets
+        if (elect_one()) {
+            const int tiles = a.tiles_down + a.tiles_up, all = __ldcg(a.pieces + 1) * tiles;
+            for (int i = blockIdx.x;;) {
+                GradItem it = {};
+                if (i < all) {
+                    const int4 *from = reinterpret_cast<const int4 *>(a.list + i / tiles);
+                    const int4 lo = __ldcg(from), hi = __ldcg(from + 1);
+                    it.p = GradPiece{lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+                    it.f = i % tiles;
+                    it.up = it.f >= a.tiles_down;
+                    it.m0 = (it.up ? it.f - a.tiles_down : it.f) * kGradFeatures;
+                    it.more = 1;
                 }
-            };
-            if (!plain) look(t.k_from, next[0]), look(t.k_from + 1, next[1]);
-            for (int k = t.k_from; k < t.k_to; ++k) {
-                if (!(ok = __all_sync(kFullMask, bar_wait(empty0 + 8 * s, phase, gave_up)))) break;
-                const uint32_t dst = ring + s * stage_bytes + at;
-                const int e = k * kTileK + line;
-                const uint16_t *rank = ranks + (size_t)e * a.rank;
-                if (plain && (k + 1) * (long long)kTileK <= t.n) {           // a whole stage of rows one behind the other
-                    const uint16_t *row = rows + (size_t)(t.begin + e) * features;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j, row += row_step, rank += rank_step) {
-                        if (live) copy16(dst + j * 2048, row, true);
-                        if (real) copy16(dst + kLines + j * 2048, rank, true);
-                    }
-                } else {
-                    if (plain) look(k, next[0]);
-                    bool bad = false;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j, rank += rank_step) {
-                        const unsigned row = (unsigned)next[0][j];
-                        const bool there = row < (unsigned)a.rows;           // others are zeros, in both operands
-                        bad |= !there && e + 16 * j < t.n;
-                        if (live) copy16(dst + j * 2048, rows + (there ? (size_t)row * (unsigned)features : 0), there);
-                        if (real) copy16(dst + kLines + j * 2048, there ? rank : ranks, there);
-                        next[0][j] = next[1][j];
-                    }
-                    if (bad && a.status && piece == 0) atomicOr(a.status, EP_STATUS_BAD_INDEX);
-                    if (!plain) look(k + 2, next[1]);
-                }
-                copy_group();
-                if (++s == stages) s = 0, phase ^= 1;
-                if (waiting == kLag) copy_wait<kLag>(), arrive(); else ++waiting;
+                if (!bar_wait(smem_addr(&item_empty_[slot]), slot_phase ^ 1, gave_up)) break;
+                items_[slot] = it;
+                bar_arrive(smem_addr(&item_full_[slot]));
+                if (++slot == kGradAhead) slot = 0, slot_phase ^= 1;
+                if (!it.more) break;
+                i = atomicAdd(a.counter, 1) + gridDim.x;
             }
         }
+    } else if (warp >= 2 + kGradEpilogueWarps) {
+        // ---- entries into the ring: two warps for each of its places. A whole stage of rows one behind the other comes in boxes. Rows by
+        // index, and a segment's last ones, are copied 16 bytes a thread, zeros where there is none (in both operands); a thread waits
+        // for its own before it hands them to the tensor cores, and other warps' stages are under way meanwhile. (With all warps on every
+        // stage that hand-over waits for the later stages, too: dup of 16384 x 8192 rows on four adapters of unequal length 80 us, so 58;
+        // with gather4 copies by index 148, so 60.)
+        const int s = (warp - 2 - kGradEpilogueWarps) >> 1, thread = (threadIdx.x - 32 * (2 + kGradEpilogueWarps)) & 63, piece = thread & 15, line = thread >> 4;
+        const bool first = (thread >> 5) == 0;                               // of the two warps
+        const uint32_t full = full0 + 8 * s, dst = ring + s * stage_bytes, at = dst + (piece >> 3) * 8192;
+        const uint32_t at_even = at + swizzled(line, piece & 7), at_odd = at + swizzled(line + 4, piece & 7);
+        int phase = 1, skip = s;                                             // stages until this place's next one
+        bool ok = true, sent = false;
+        while (ok && next(true)) {
+            const int features = t.up ? a.N : a.H;
+            const bool live = t.m0 + piece * 8 < features, real = piece * 8 < a.rank, plain = a.index == nullptr;
+            const uint16_t *const rows = (t.up ? a.dy : a.x) + (live ? t.m0 + piece * 8 : 0);
+            const uint16_t *const ranks = (t.up ? a.mid : a.dmid) + (real ? piece * 8 : 0);
+            int k = t.p.k_from + skip;
+            for (; k < t.p.k_to; k += stages) {
+                if (!(ok = __all_sync(kFullMask, bar_wait(empty0 + 8 * s, phase, gave_up)))) break;
+                phase ^= 1;
+                if (plain && (k + 1) * (long long)kTileK <= t.p.n) {
+                    if (lane == 0) {
+                        if (first) {
+                            const int row = t.p.begin + k * kTileK;
+                            bar_expect(full, stage_bytes);
+                            tma_load<1>(dst, t.up ? &maps.dy : &maps.x, t.m0, row, 0, full);
+                            tma_load<1>(dst + 8192, t.up ? &maps.dy : &maps.x, t.m0 + 64, row, 0, full);
+                            for (int c = 0; c < chunks; ++c) tma_load<1>(dst + kLines + c * 8192, t.up ? &maps.mid : &maps.dmid, 64 * c, row, 0, full);
+                            sent = true;
+                        } else {
+                            bar_arrive(full);
+                        }
+                    }
+                    continue;
+                }
+                bool bad = false;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    int row[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int e = k * kTileK + line + 4 * (8 * h + j);
+                        row[j] = e < t.p.n ? (plain ? t.p.begin + e : __ldg(a.index + t.p.begin + e)) : -1;
+                    }
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int e = k * kTileK + line + 4 * (8 * h + j);
+                        const bool there = (unsigned)row[j] < (unsigned)a.rows;
+                        const uint32_t to = (j & 1 ? at_odd : at_even) + (4 * h + (j >> 1)) * 1024;
+                        bad |= !there && e < t.p.n;
+                        if (live) copy16(to, rows + (there ? (size_t)(unsigned)row[j] * (unsigned)features : 0), there);
+                        if (real) copy16(to + kLines, ranks + (there ? (size_t)(unsigned)(t.p.begin + e) * (unsigned)a.rank : 0), there);
+                    }
+                }
+                if (bad && a.status && piece == 0) atomicOr(a.status, EP_STATUS_BAD_INDEX);
+                copy_group();
+                copy_wait<0>();
+                fence_async();
+                __syncwarp();
+                if (lane == 0) bar_arrive(full);
+            }
+            skip = k - t.p.k_to;
+        }
         copy_wait<0>();
-        for (; ok && waiting > 0; --waiting) arrive();
+        if (!ok && sent) {                                                   // gave up: let the last boxes land
+            int none = 0;
+            bar_wait(full, phase, &none);
+        }
     } else if (warp == 0 && elect_one()) {
         // ---- products
         int s = 0, phase = 0, used = 0;
         bool ok = true;
         const uint32_t idesc = instr_desc(kRows, r16, true, true);
-        for (int i = first; ok && i < a.items; i += step) {
-            const Item t = item_at(i);
-            if (t.k_from == t.k_to) continue;
+        while (ok && next(false)) {
+            if (t.p.n == 0) continue;
             const int acc = used & 1;
             if (!(ok = bar_wait(smem_addr(&acc_empty_[acc]), ((used >> 1) & 1) ^ 1, gave_up))) break;
             tmem_fence_after();
-            for (int k = t.k_from; k < t.k_to; ++k) {
+            for (int k = t.p.k_from; k < t.p.k_to; ++k) {
                 if (!(ok = bar_wait(full0 + 8 * s, phase, gave_up))) break;
                 tmem_fence_after();
                 const uint32_t at = ring + s * stage_bytes;
                 const uint64_t da = desc_mn_major(at), db = desc_mn_major(at + kLines);
 #pragma unroll
-                for (int j = 0; j < kTileK / 16; ++j) mma_bf16<1>(tmem + acc * a.columns, da + j * 128, db + j * 128, idesc, k > t.k_from || j > 0);
+                for (int j = 0; j < kTileK / 16; ++j) mma_bf16<1>(tmem + acc * a.columns, da + j * 128, db + j * 128, idesc, k > t.p.k_from || j > 0);
                 mma_commit<1>(empty0 + 8 * s);
                 if (++s == stages) s = 0, phase ^= 1;
             }
@@ -725,110 +893,106 @@ adapter_grad_kernel(const GradArgs a)
             ++used;
         }
     } else if (warp >= 1) {
-        // ---- accumulators out, through shared memory; SPLIT: added up over the CTAs that share them
+        // ---- accumulators out, through shared memory, or as a part of an item's sums
         const int q = warp & 3, thread = threadIdx.x - 32;
+        const auto together = [] { asm volatile("bar.sync 1, 128;" ::: "memory"); };        // the four warps
         int used = 0;
         bool ok = true;
-        for (int i = first; ok && i < a.items; i += step) {
-            const Item t = item_at(i);
-            const bool some = t.k_from < t.k_to;
-            const int acc = used & 1, features = t.up ? a.N : a.H;
-            const float scale = t.up && a.scale ? __ldg(a.scale + t.adapter) : 1.f;
-            if (some) {
-                ok = bar_wait(smem_addr(&acc_full_[acc]), (used >> 1) & 1, gave_up);
-                tmem_fence_after();
-                ++used;
-            }
-            uint32_t v[32];
-            // columns [c0, c0 + 32) of the accumulator, or zeros
-            const auto load = [&](int c0) {
-                if (some) {
-                    tmem_load32(tmem + (uint32_t(q * 32) << 16) + acc * a.columns + c0, v);
-                } else {
-#pragma unroll
-                    for (int c = 0; c < 32; ++c) v[c] = 0u;
-                }
-            };
+        while (ok && next(true)) {
+            const int acc = used & 1, features = t.up ? a.N : a.H, m0 = t.m0, tiles = a.tiles_down + a.tiles_up;
+            const float scale = t.up && a.scale ? __ldg(a.scale + t.p.adapter) : 1.f;
+            const bool whole = t.p.of == 1;
+            float *const mine = a.parts + (((size_t)(t.p.part + t.p.number) * tiles + t.f)) * r16 * kRows;
             // 8 results: ddown, 8 features of a rank; dup, 8 ranks of a feature
             const auto store = [&](float (&z)[8], int feature, int rank) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) z[j] *= scale;
-                uint16_t *dst = t.up ? a.dup + ((size_t)t.adapter * a.N + t.m0 + feature) * a.rank + rank
-                                     : a.ddown + ((size_t)t.adapter * a.rank + rank) * a.H + t.m0 + feature;
+                uint16_t *dst = t.up ? a.dup + ((size_t)t.p.adapter * a.N + m0 + feature) * a.rank + rank
+                                     : a.ddown + ((size_t)t.p.adapter * a.rank + rank) * a.H + m0 + feature;
                 *reinterpret_cast<uint4 *>(dst) = pack8(z);
             };
-            if (SPLIT) {
-                for (int c0 = 0; ok && c0 < r16; c0 += 32) {
-                    load(c0);
+            if (t.p.n == 0) {
+                const int real = min(kRows, features - m0);
+                for (int j = thread; j < real * a.rank / 8; j += 128) {
+                    uint16_t *dst = t.up ? a.dup + ((size_t)t.p.adapter * a.N + m0) * a.rank + j * 8
+                                         : a.ddown + ((size_t)t.p.adapter * a.rank + j / (real / 8)) * a.H + m0 + j % (real / 8) * 8;
+                    *reinterpret_cast<uint4 *>(dst) = make_uint4(0u, 0u, 0u, 0u);
+                }
+                continue;
+            }
+            ok = bar_wait(smem_addr(&acc_full_[acc]), (used >> 1) & 1, gave_up);
+            tmem_fence_after();
+            ++used;
+            for (int c0 = 0; ok && c0 < r16; c0 += 32) {
+                uint32_t v[32];
+                tmem_load32(tmem + (uint32_t(q * 32) << 16) + acc * a.columns + c0, v);
+                if (c0 + 32 >= r16) {                                        // this warp has read its last column
+                    tmem_fence_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(smem_addr(&acc_empty_[acc]));
+                }
+                if (!whole) {
 #pragma unroll
                     for (int c = 0; c < 32; ++c)
-                        if (c0 + c < r16) out[(c0 + c) * kGradLd + q * 32 + lane] = __uint_as_float(v[c]);
+                        if (c0 + c < r16) mine[(c0 + c) * kRows + q * 32 + lane] = __uint_as_float(v[c]);
+                    continue;
                 }
-                __syncwarp();
-                if (ok && lane < split) bar_arrive_cluster_release(in_cta(smem_addr(&ex_full_), lane));
-                ok = ok && bar_wait<true>(smem_addr(&ex_full_), 0, gave_up);
-                const int total = t.up ? kRows * (a.rank / 8) : a.rank * (kRows / 8);
-                const int from = total * part / split, to = total * (part + 1) / split;
-                for (int j = from + thread; ok && j < to; j += 128) {
-                    const int feature = t.up ? j % kRows : j % (kRows / 8) * 8, rank = t.up ? j / kRows * 8 : j / (kRows / 8);
-                    if (t.m0 + feature >= features) continue;
-                    float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                    const uint32_t src = smem_addr(out + rank * kGradLd + feature);
-                    for (int s = 0; s < split; ++s) {
-                        const uint32_t at = in_cta(src, s);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (c0 + kGradColumns * h >= a.rank) break;
+#pragma unroll
+                    for (int c = 0; c < kGradColumns; ++c) out[c * kGradLd + q * 32 + lane] = __uint_as_float(v[kGradColumns * h + c]);
+                    together();
+                    const int ranks = min(kGradColumns, a.rank - c0 - kGradColumns * h), total = t.up ? kRows * (ranks / 8) : ranks * (kRows / 8);
+                    for (int j = thread; j < total; j += 128) {
+                        const int feature = t.up ? j % kRows : j % (kRows / 8) * 8, rank = t.up ? j / kRows * 8 : j / (kRows / 8);
+                        if (m0 + feature >= features) continue;
+                        const float *src = out + rank * kGradLd + feature;
+                        float z[8];
                         if (t.up) {
 #pragma unroll
-                            for (int l = 0; l < 8; ++l) {
-                                float w;
-                                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(w) : "r"(at + l * kGradLd * 4) : "memory");
-                                z[l] += w;
-                            }
+                            for (int l = 0; l < 8; ++l) z[l] = src[l * kGradLd];
                         } else {
-                            const float4 lo = load_cluster(at), hi = load_cluster(at + 16);
+                            const float4 lo = *reinterpret_cast<const float4 *>(src), hi = *reinterpret_cast<const float4 *>(src + 4);
+                            z[0] = lo.x, z[1] = lo.y, z[2] = lo.z, z[3] = lo.w, z[4] = hi.x, z[5] = hi.y, z[6] = hi.z, z[7] = hi.w;
+                        }
+                        store(z, feature, c0 + kGradColumns * h + rank);
+                    }
+                    together();                                              // `out` may be written again
+                }
+            }
+            if (whole || !ok) continue;
+            // who comes last adds the parts
+            __threadfence();
+            together();
+            if (thread == 0) last_ = atomicAdd(a.arrived + ((size_t)t.p.part * tiles + t.f), 1) == t.p.of - 1;
+            together();
+            if (last_) {
+                __threadfence();
+                for (int j = thread; j < (t.up ? kRows * (a.rank / 8) : a.rank * (kRows / 8)); j += 128) {
+                    const int feature = t.up ? j % kRows : j % (kRows / 8) * 8, rank = t.up ? j / kRows * 8 : j / (kRows / 8);
+                    if (m0 + feature >= features) continue;
+                    float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 2
+                    for (int p = 0; p < t.p.of; ++p) {
+                        const float *src = a.parts + ((((size_t)(t.p.part + p) * tiles + t.f)) * r16 + rank) * kRows + feature;
+                        if (t.up) {
+#pragma unroll
+                            for (int l = 0; l < 8; ++l) z[l] += __ldcg(src + l * kRows);
+                        } else {
+                            const float4 lo = __ldcg(reinterpret_cast<const float4 *>(src)), hi = __ldcg(reinterpret_cast<const float4 *>(src + 4));
                             z[0] += lo.x, z[1] += lo.y, z[2] += lo.z, z[3] += lo.w, z[4] += hi.x, z[5] += hi.y, z[6] += hi.z, z[7] += hi.w;
                         }
                     }
                     store(z, feature, rank);
                 }
-            } else {
-                for (int c0 = 0; ok && c0 < r16; c0 += 32) {
-                    load(c0);
-                    if (some && c0 + 32 >= r16) {                            // this warp has read its last column
-                        tmem_fence_before();
-                        __syncwarp();
-                        if (lane == 0) bar_arrive(smem_addr(&acc_empty_[acc]));
-                    }
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        if (c0 + kGradColumns * h >= a.rank) break;
-#pragma unroll
-                        for (int c = 0; c < kGradColumns; ++c) out[c * kGradLd + q * 32 + lane] = __uint_as_float(v[kGradColumns * h + c]);
-                        asm volatile("bar.sync 1, 128;" ::: "memory");       // the four warps
-                        const int ranks = min(kGradColumns, a.rank - c0 - kGradColumns * h), total = t.up ? kRows * (ranks / 8) : ranks * (kRows / 8);
-                        for (int j = thread; j < total; j += 128) {
-                            const int feature = t.up ? j % kRows : j % (kRows / 8) * 8, rank = t.up ? j / kRows * 8 : j / (kRows / 8);
-                            if (t.m0 + feature >= features) continue;
-                            const float *src = out + rank * kGradLd + feature;
-                            float z[8];
-                            if (t.up) {
-#pragma unroll
-                                for (int l = 0; l < 8; ++l) z[l] = src[l * kGradLd];
-                            } else {
-                                const float4 lo = *reinterpret_cast<const float4 *>(src), hi = *reinterpret_cast<const float4 *>(src + 4);
-                                z[0] = lo.x, z[1] = lo.y, z[2] = lo.z, z[3] = lo.w, z[4] = hi.x, z[5] = hi.y, z[6] = hi.z, z[7] = hi.w;
-                            }
-                            store(z, feature, c0 + kGradColumns * h + rank);
-                        }
-                        asm volatile("bar.sync 1, 128;" ::: "memory");       // `out` may be written again
-                    }
-                }
             }
+            together();                                                      // `last_` may be written again
         }
     }
     __syncwarp();
     tmem_fence_before();
     __syncthreads();
-    if (SPLIT) cluster_sync();                                               // the others' reads come from this CTA's memory
     tmem_fence_after();
     if (warp == 0) tmem_free<1>(tmem, 2 * a.columns);
     if (threadIdx.x == 0 && gave_up_ && a.status) atomicOr(a.status, EP_STATUS_TIMEOUT);
@@ -880,7 +1044,7 @@ int launch_cluster(Kernel kernel, std::atomic<uint64_t> &ready, int64_t groups, 
 
 // One launch of the rank kernel: `in` [rows][in], weights down [A][rank][*], up [A][*][rank].
 template <bool BACK>
-int launch_rank(const ep_adapter_t &m, TensorMapEncode encode, RankArgs a, const void *in, const void *down, const void *up, cudaStream_t stream)
+int launch_rank(const ep_adapter_t &m, TensorMapEncode encode, RankArgs a, const PlanArgs &plan, const void *in, const void *down, const void *up, cudaStream_t stream)
 {
     static std::atomic<uint64_t> ready{0};
     const uint64_t H = m.in_features, N = m.out_features, r = m.rank, A = m.num_adapters;
@@ -906,10 +1070,41 @@ int launch_rank(const ep_adapter_t &m, TensorMapEncode encode, RankArgs a, const
         if (even > 64 && even < kRows) a.width = (int)(even + 3) / 4 * 4;
     }
     tiles = m.entries / a.width + adapters;
-    return launch_cluster(rank_kernel<BACK>, ready, tiles, a.split, kThreads, kRankSmem, kRankSmem, stream, a, map_first, map_second);
+    return launch_cluster(rank_kernel<BACK>, ready, tiles + (plan.list ? 1 : 0), a.split, kThreads, kRankSmem, kRankSmem, stream, a, plan, map_first, map_second);
 }
 
 size_t up256(size_t n) { return (n + 255) & ~size_t(255); }
+
+// The gradient kernel's launch and workspace.
+struct GradPlan {
+    int ctas, stages, smem, piece;
+    int64_t counters;
+    size_t counter_bytes, list_bytes, dmid_bytes, parts_bytes;
+};
+int feature_tiles(int features) { return (features + kGradFeatures - 1) / kGradFeatures; }
+GradPlan plan_grads(const ep_adapter_t &m)
+{
+    GradPlan p;
+    const int r16 = (m.rank + 15) & ~15, chunks = (m.rank + 63) / 64, stage = kLines + chunks * 8192;
+    const int64_t tiles = feature_tiles(m.in_features) + feature_tiles(m.out_features), all = m.entries / kTileK;
+    // Pieces of at least eight stages, and not so short that there are more than some three a CTA and feature tile.
+    const int64_t even = (all * tiles + 3 * kGradMost - 1) / (3 * kGradMost);
+    p.piece = (int)(even < 8 ? 8 : even);
+    // An adapter with more stages than that has more than 64 * piece entries: there are at most `cuts` of those, and their pieces are at
+    // most that many more.
+    const int64_t cuts = all / p.piece, split = cuts + (m.num_adapters < cuts ? m.num_adapters : cuts);
+    const int64_t pieces = m.num_adapters + cuts;
+    p.stages = chunks == 1 ? 4 : 6;                                          // two CTAs on an SM, or one
+    p.smem = 1024 + kGradOutBytes + p.stages * stage;
+    const int64_t most = chunks == 1 ? kGradMost : kGradMost / 2, items = pieces * tiles;
+    p.ctas = (int)(items < most ? items : most);
+    p.counters = 1 + split * tiles;
+    p.counter_bytes = up256((size_t)p.counters * 4 + 8);
+    p.list_bytes = up256((size_t)pieces * sizeof(GradPiece));
+    p.dmid_bytes = up256((size_t)m.entries * m.rank * 2);
+    p.parts_bytes = (size_t)(split * tiles) * r16 * kGradFeatures * 4;
+    return p;
+}
 
 }  // namespace
 }  // namespace ep
@@ -931,14 +1126,15 @@ extern "C" int ep_adapter_matmul(const ep_adapter_t *m, const void *x, const int
     a.offsets = adapter_offsets, a.index = row_index, a.status = status, a.scale = scale;
     a.base = static_cast<const uint16_t *>(base);
     a.out = static_cast<uint16_t *>(y), a.mid = static_cast<uint16_t *>(mid);
-    return launch_rank<false>(*m, encode, a, x, down, up, static_cast<cudaStream_t>(stream));
+    return launch_rank<false>(*m, encode, a, PlanArgs{}, x, down, up, static_cast<cudaStream_t>(stream));
 }
 
 extern "C" size_t ep_adapter_matmul_backward_workspace_bytes(const ep_adapter_t *m)
 {
     using namespace ep;
     if (check_adapter(m) != EP_OK) return 0;
-    return up256((size_t)m->entries * m->rank * 2) + 256;
+    const GradPlan p = plan_grads(*m);
+    return p.counter_bytes + p.list_bytes + p.dmid_bytes + p.parts_bytes;
 }
 
 extern "C" int ep_adapter_matmul_backward(const ep_adapter_t *m, const void *dy, const void *x, const int32_t *adapter_offsets, const int32_t *row_index,
@@ -961,9 +1157,21 @@ extern "C" int ep_adapter_matmul_backward(const ep_adapter_t *m, const void *dy,
         return EP_OK;
     }
     if (!dy || !adapter_offsets || ((dx || ddown) && !up) || (dx && !down) || (ddown && !x) || (dup && !mid)) return EP_ERR_NULL;
-    void *dmid = workspace;
-    if (ddown && !workspace) return EP_ERR_NULL;
-    if (ddown && workspace_bytes < ep_adapter_matmul_backward_workspace_bytes(m)) return EP_ERR_CAPACITY;
+    if ((ddown || dup) && !workspace) return EP_ERR_NULL;
+    if ((ddown || dup) && workspace_bytes < ep_adapter_matmul_backward_workspace_bytes(m)) return EP_ERR_CAPACITY;
+    const GradPlan plan = plan_grads(*m);
+    char *const ws = static_cast<char *>(workspace);
+    void *dmid = ws + plan.counter_bytes + plan.list_bytes;
+    PlanArgs pieces = {};
+    if (ddown || dup) {
+        const int64_t tiles = (ddown ? feature_tiles(m->in_features) : 0) + (dup ? feature_tiles(m->out_features) : 0);
+        if (((int64_t)m->num_adapters + 1) * (feature_tiles(m->in_features) + feature_tiles(m->out_features)) >= (int64_t(1) << 31) - 8192) return EP_ERR_INVALID_ARG;
+        pieces.offsets = adapter_offsets, pieces.entries = m->entries;
+        pieces.A = m->num_adapters, pieces.piece = plan.piece, pieces.tiles = (int)tiles, pieces.ctas = plan.ctas;
+        pieces.counters = (int)plan.counters;
+        pieces.pieces = reinterpret_cast<int *>(ws), pieces.arrived = pieces.pieces + 2;
+        pieces.list = reinterpret_cast<GradPiece *>(ws + plan.counter_bytes);
+    }
     TensorMapEncode encode;
     rc = tensor_map_encoder(&encode);
     if (rc != EP_OK) return rc;
@@ -973,32 +1181,39 @@ extern "C" int ep_adapter_matmul_backward(const ep_adapter_t *m, const void *dy,
         a.base = static_cast<const uint16_t *>(base);
         a.out = static_cast<uint16_t *>(dx);
         a.mid = ddown ? static_cast<uint16_t *>(dmid) : nullptr;
-        rc = launch_rank<true>(*m, encode, a, dy, down, up, stream);
+        rc = launch_rank<true>(*m, encode, a, pieces, dy, down, up, stream);
         if (rc != EP_OK) return rc;
     }
     if (!ddown && !dup) return EP_OK;
+    if (!dx && !ddown) {
+        static std::atomic<uint64_t> planned{0};
+        rc = launch_cluster(plan_kernel, planned, 1, 1, kThreads, (int)sizeof(PlanTables), (int)sizeof(PlanTables), stream, pieces);
+        if (rc != EP_OK) return rc;
+    }
     GradArgs g = {};
     g.offsets = adapter_offsets, g.index = row_index, g.scale = scale, g.status = status;
     g.x = static_cast<const uint16_t *>(x), g.dmid = static_cast<const uint16_t *>(dmid);
     g.dy = static_cast<const uint16_t *>(dy), g.mid = static_cast<const uint16_t *>(mid);
-    g.ddown = static_cast<uint16_t *>(ddown), g.dup = static_cast<uint16_t *>(dup);
-    g.rows = m->rows, g.entries = m->entries, g.H = m->in_features, g.N = m->out_features, g.rank = m->rank, g.A = m->num_adapters;
-    g.tiles_down = ddown ? (m->in_features + kRows - 1) / kRows : 0;
-    g.tiles_up = dup ? (m->out_features + kRows - 1) / kRows : 0;
-    const int64_t items = (int64_t)g.A * (g.tiles_down + g.tiles_up), average = m->entries / m->num_adapters / kTileK;
-    if (items * kMaxCluster >= (int64_t(1) << 31)) return EP_ERR_INVALID_ARG;
-    g.items = (int)items;
-    g.split = 1;
-    while (g.split < kMaxCluster && items * g.split * 2 <= 2 * 148 && average >= 4 * g.split) g.split *= 2;
-    const int r16 = (m->rank + 15) & ~15, chunks = (m->rank + 63) / 64, stage = kLines + chunks * 8192, table = (g.A + 1) * 4;
-    g.columns = r16 <= 32 ? 32 : r16 <= 64 ? 64 : 128;
-    static std::atomic<uint64_t> ready[4];
-    const int fixed = 1024 + kGradOutBytes + table;                          // beside the stages
-    if (g.split > 1) {                                                       // over half of an SM's memory each: see the rank kernel
-        if (chunks == 1) return launch_cluster(adapter_grad_kernel<true, 4>, ready[0], items, g.split, kGradThreads, kRankSmem, kRankSmem, stream, g);
-        return launch_cluster(adapter_grad_kernel<true, 6>, ready[1], items, g.split, kGradThreads, fixed + 6 * stage, 222 * 1024, stream, g);
+    GradMaps maps = {};
+    if (ddown) {
+        rc = make_map(encode, &maps.x, x, H, m->rows, 1, kTileK);
+        if (rc == EP_OK) rc = make_map(encode, &maps.dmid, dmid, r, m->entries, 1, kTileK);
+        if (rc != EP_OK) return rc;
     }
-    if (chunks == 1 && fixed + 4 * stage <= kRankSmem - 1024)                // two on an SM
-        return launch_cluster(adapter_grad_kernel<false, 4>, ready[2], items < 296 ? items : 296, 1, kGradThreads, fixed + 4 * stage, kRankSmem, stream, g);
-    return launch_cluster(adapter_grad_kernel<false, 6>, ready[3], items < 148 ? items : 148, 1, kGradThreads, fixed + 6 * stage, 222 * 1024, stream, g);
+    if (dup) {
+        rc = make_map(encode, &maps.dy, dy, N, m->rows, 1, kTileK);
+        if (rc == EP_OK) rc = make_map(encode, &maps.mid, mid, r, m->entries, 1, kTileK);
+        if (rc != EP_OK) return rc;
+    }
+    g.ddown = static_cast<uint16_t *>(ddown), g.dup = static_cast<uint16_t *>(dup);
+    g.pieces = pieces.pieces, g.list = pieces.list, g.counter = pieces.arrived, g.arrived = pieces.arrived + 1;
+    g.parts = reinterpret_cast<float *>(static_cast<char *>(dmid) + plan.dmid_bytes);
+    g.rows = m->rows, g.entries = m->entries, g.H = m->in_features, g.N = m->out_features, g.rank = m->rank, g.A = m->num_adapters;
+    g.tiles_down = ddown ? feature_tiles(m->in_features) : 0;
+    g.tiles_up = dup ? feature_tiles(m->out_features) : 0;
+    const int r16 = (m->rank + 15) & ~15;
+    g.columns = r16 <= 32 ? 32 : r16 <= 64 ? 64 : 128;
+    static std::atomic<uint64_t> ready[2];
+    if (plan.stages == 4) return launch_cluster(adapter_grad_kernel<4>, ready[0], plan.ctas, 1, grad_threads(4), plan.smem, kRankSmem, stream, g, maps);
+    return launch_cluster(adapter_grad_kernel<6>, ready[1], plan.ctas, 1, grad_threads(6), plan.smem, 222 * 1024, stream, g, maps);
 }
