@@ -76,6 +76,10 @@ __device__ __forceinline__ void tmem_wait16(uint32_t (&v)[16])
                    "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])::"memory");
 }
 
+// The two halves of a barrier of the cluster.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
 // Bytes (a multiple of 16, from a 16-byte boundary) on their way into L2.
 __device__ __forceinline__ void l2_prefetch(const void *p, uint32_t bytes)
 {
@@ -97,7 +101,7 @@ constexpr int kMaxStages = 4, kMaxUnits = 5;
 constexpr int kLag = 2;                   // stages a loader has in flight behind the one it asks for
 
 struct RankTables {
-    uint64_t full[kMaxStages], empty[kMaxStages], unit_full[kMaxUnits], unit_empty[kMaxUnits], mid_full, mid_ready, acc_full[2], acc_empty[2],
+    uint64_t full[kMaxStages], empty[kMaxStages], unit_full[kMaxUnits], unit_empty[kMaxUnits], mid_full, mid_ready, mid_ready_all, acc_full[2], acc_empty[2],
         ex_full;
     uint32_t tmem_slot;
     int gave_up, warp_sum[kThreads / 32], where[3];
@@ -270,9 +274,20 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
     const int split = a.split, part = split > 1 ? (int)cluster_rank() : 0;
     const int tile = (int)blockIdx.x / split - (plan.list != nullptr);
 
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kMaxStages; ++s) bar_init(smem_addr(&tab.full[s]), 1 + kEpilogueWarps), bar_init(smem_addr(&tab.empty[s]), 1);
+        for (int s = 0; s < kMaxUnits; ++s) bar_init(smem_addr(&tab.unit_full[s]), 1), bar_init(smem_addr(&tab.unit_empty[s]), 1);
+        for (int s = 0; s < 2; ++s) bar_init(smem_addr(&tab.acc_full[s]), 1), bar_init(smem_addr(&tab.acc_empty[s]), kEpilogueWarps);
+        bar_init(smem_addr(&tab.mid_full), 1);
+        bar_init(smem_addr(&tab.mid_ready), kEpilogueWarps);
+        bar_init(smem_addr(&tab.mid_ready_all), split * kEpilogueWarps);
+        bar_init(smem_addr(&tab.ex_full), split * kEpilogueWarps);
+        tab.gave_up = 0;
+        where[0] = -1;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
     pdl_wait();                                                              // nothing is read or written before this
     // ---- this cluster's tile: each thread counts the tiles of a run of adapters
-    if (threadIdx.x == 0) where[0] = -1;
     if (tile < 0) {                                                          // the first cluster plans what the gradient kernel does
         if (part == 0) plan_pieces(plan, *reinterpret_cast<PlanTables *>(area));
         return;
@@ -322,43 +337,40 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
     const int blocks = a.out ? (a.out_features + kBlockColumns - 1) / kBlockColumns : 0;
     const int b_from = (int)((long long)blocks * part / split), b_to = (int)((long long)blocks * (part + 1) / split);
     const int stage_bytes = kLines + chunks * 8192, stages = kRingBytes / stage_bytes;
-    const int loaders = min(kEpilogueWarps, (m + 3) / 4), quarters = (m + 31) / 32;        // warps that bring rows; quarters of the lanes with rows
+    const int quarters = (m + 31) / 32;                                      // of the lanes, with rows
     const bool narrow = quarters == 1;                                       // each quarter of the lanes holds the same rows, see below
-    const int units = kAreaBytes / kLines - chunks - quarters;
+    // The parts that a cluster's CTAs have of the first product are sent to all of them where there is room for all of all beside the
+    // ring; more of it is added up by shares (see below).
+    const bool send = split > 1 && narrow && split * m * r16 * 4 <= kAreaBytes - kRingBytes;
+    const int units = kAreaBytes / kLines - chunks - quarters - (send ? 1 : 0);
     const uint32_t ring = smem_addr(area), unit_base = ring + (chunks + quarters) * kLines;
     char *const buffers = area + chunks * kLines;
     float *const exchange = reinterpret_cast<float *>(buffers);              // [m][r16], 16-byte pieces turned so that neither axis meets a bank twice
     const int ex_turn = r16 % 32 == 0 ? 7 : 6;
     const auto ex_at = [&](int row, int piece) { return row * r16 + ((piece ^ (ex_turn == 7 ? row & 7 : (row & 6) >> 1)) << 2); };
 
-    if (threadIdx.x == 0) {
-        for (int s = 0; s < kMaxStages; ++s) bar_init(smem_addr(&tab.full[s]), 1 + loaders), bar_init(smem_addr(&tab.empty[s]), 1);
-        for (int s = 0; s < kMaxUnits; ++s) bar_init(smem_addr(&tab.unit_full[s]), 1), bar_init(smem_addr(&tab.unit_empty[s]), 1);
-        for (int s = 0; s < 2; ++s) bar_init(smem_addr(&tab.acc_full[s]), 1), bar_init(smem_addr(&tab.acc_empty[s]), narrow ? kEpilogueWarps : 2 * quarters);
-        bar_init(smem_addr(&tab.mid_full), 1);
-        bar_init(smem_addr(&tab.mid_ready), split * kEpilogueWarps);
-        bar_init(smem_addr(&tab.ex_full), split * kEpilogueWarps);
-        tab.gave_up = 0;
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
-    if (warp == 1) tmem_alloc<1>(smem_addr(&tab.tmem_slot), 2 * kBlockColumns);
-    for (int i = threadIdx.x; i < kRows; i += kThreads) {
-        int row = -1;
-        if (i < m) {
-            row = a.index ? __ldg(a.index + entry0 + i) : entry0 + i;
-            if (row < 0 || row >= a.rows) {
-                if (a.status) atomicOr(a.status, EP_STATUS_BAD_INDEX);
-                row = -1;
+    // From here on the weights' warp does not wait for the others. A cluster's CTAs write to each other's memory only after cluster_wait().
+    if (split > 1) cluster_arrive();
+    if (warp > 0) {
+        if (warp == 1) tmem_alloc<1>(smem_addr(&tab.tmem_slot), 2 * kBlockColumns);
+        const int i = (int)threadIdx.x - 64;
+        if (i >= 0 && i < kRows) {
+            int row = -1;
+            if (i < m) {
+                row = a.index ? __ldg(a.index + entry0 + i) : entry0 + i;
+                if (row < 0 || row >= a.rows) {
+                    if (a.status) atomicOr(a.status, EP_STATUS_BAD_INDEX);
+                    row = -1;
+                }
             }
+            row_of[i] = row;
         }
-        row_of[i] = row;
+        tmem_fence_before();
+        asm volatile("bar.sync 1, %0;" ::"n"(kThreads - 32) : "memory");
+        tmem_fence_after();
+        if (warp == 1) pdl_trigger();
     }
-    tmem_fence_before();
-    if (split > 1) cluster_sync();
-    __syncthreads();
-    tmem_fence_after();
-    pdl_trigger();
-    const uint32_t tmem = tab.tmem_slot;
+    const uint32_t tmem = warp > 0 ? tab.tmem_slot : 0u;
     const uint32_t full0 = smem_addr(tab.full), empty0 = smem_addr(tab.empty), unit_full0 = smem_addr(tab.unit_full), unit_empty0 = smem_addr(tab.unit_empty);
 
     if (warp == 0 && elect_one()) {
@@ -436,7 +448,7 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
         }
         if (ok) mma_commit<1>(smem_addr(&tab.mid_full));
         if (ok && blocks) {
-            ok = bar_wait<true>(smem_addr(&tab.mid_ready), 0, gave_up);
+            ok = bar_wait<true>(smem_addr(split > 1 && !send ? &tab.mid_ready_all : &tab.mid_ready), 0, gave_up);
             fence_async();                                                   // what the cluster's other CTAs wrote, too
             tmem_fence_after();
             const uint32_t idesc2 = instr_desc(kRows, kBlockColumns, false, BACK);
@@ -467,7 +479,7 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
         if (a.base && narrow && thread < m && b_to > b_from && row_of[thread] >= 0)       // few rows: their base into L2, under the first product
             l2_prefetch(a.base + (size_t)row_of[thread] * a.out_features + b_from * kBlockColumns,
                         (min(b_to * kBlockColumns, a.out_features) - b_from * kBlockColumns) * 2);
-        if (warp - 2 < loaders) {
+        {
             // ---- rows into the ring: eight lanes a row's line, four rows a warp, every 32 rows
             const int line = 4 * (warp - 2) + (lane >> 3), piece = lane & 7, n_k = k_to - k_from;
             const uint16_t *src[4];
@@ -507,11 +519,14 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[i] *= mid_scale;
             const uint4 v = pack8(f);
-            if (a.mid && row < m && col < a.rank) *reinterpret_cast<uint4 *>(a.mid + (size_t)(entry0 + row) * a.rank + col) = v;
+            if (a.mid && row < m && col < a.rank && (!send || part == 0)) *reinterpret_cast<uint4 *>(a.mid + (size_t)(entry0 + row) * a.rank + col) = v;
             return v;
         };
         const auto operand_at = [&](int row, int col) { return (col >> 6) * kLines + swizzled(row, (col & 63) >> 3); };
-        if (ok) {
+        __syncwarp();
+        if (split > 1) cluster_wait();                                       // all are there
+        float *const sent = reinterpret_cast<float *>(area + kRingBytes);    // [CTA][m][r16]
+        if (ok && (!narrow || q == 0)) {
             for (int c0 = half * 32; c0 < r16; c0 += 64) {
                 uint32_t v[32];
                 tmem_load32(tmem + (uint32_t(q * 32) << 16) + c0, v);
@@ -525,10 +540,15 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
                             const uint4 w = rounded(my_row, c0 + 8 * j, f);
                             if (!narrow) {
                                 *reinterpret_cast<uint4 *>(area + operand_at(my_row, c0 + 8 * j)) = w;
-                            } else if (q == 0) {
+                            } else {
 #pragma unroll
                                 for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4 *>(area + operand_at(32 * i + lane, c0 + 8 * j)) = w;
                             }
+                        } else if (send && my_row < m) {
+                            const uint32_t to = smem_addr(sent + (part * m + my_row) * r16 + c0 + 8 * j);
+                            const uint4 lo = make_uint4(v[8 * j], v[8 * j + 1], v[8 * j + 2], v[8 * j + 3]);
+                            const uint4 hi = make_uint4(v[8 * j + 4], v[8 * j + 5], v[8 * j + 6], v[8 * j + 7]);
+                            for (int s = 0; s < split; ++s) store_cluster(in_cta(to, s), lo), store_cluster(in_cta(to, s) + 16, hi);
                         } else if (my_row < m) {
                             const int piece = c0 / 4 + 2 * j;
                             *reinterpret_cast<uint4 *>(exchange + ex_at(my_row, piece)) = make_uint4(v[8 * j], v[8 * j + 1], v[8 * j + 2], v[8 * j + 3]);
@@ -544,7 +564,19 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
             if (lane < split) bar_arrive_cluster_release(in_cta(smem_addr(&tab.ex_full), lane));
             ok = bar_wait<true>(smem_addr(&tab.ex_full), 0, gave_up);
             const int groups = r16 / 8;
-            for (int i = thread * split + part; ok && i < m * groups; i += 32 * kEpilogueWarps * split) {
+            for (int i = thread; ok && send && i < m * groups; i += 32 * kEpilogueWarps) {
+                const int row = i / groups, col = i % groups * 8;
+                float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                for (int s = 0; s < split; ++s) {
+                    const float4 *from = reinterpret_cast<const float4 *>(sent + (s * m + row) * r16 + col);
+                    const float4 l = from[0], h = from[1];
+                    f[0] += l.x, f[1] += l.y, f[2] += l.z, f[3] += l.w, f[4] += h.x, f[5] += h.y, f[6] += h.z, f[7] += h.w;
+                }
+                const uint4 v = rounded(row, col, f);
+#pragma unroll
+                for (int i4 = 0; i4 < 4; ++i4) *reinterpret_cast<uint4 *>(area + operand_at(32 * i4 + row, col)) = v;
+            }
+            for (int i = thread * split + part; ok && !send && i < m * groups; i += 32 * kEpilogueWarps * split) {
                 const int row = i / groups, col = i % groups * 8;
                 const uint32_t lo = smem_addr(exchange + ex_at(row, col / 4)), hi = smem_addr(exchange + ex_at(row, col / 4 + 1));
                 float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -567,8 +599,12 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
         fence_async();
         tmem_fence_before();
         __syncwarp();
-        if (lane < split) bar_arrive_cluster_release(in_cta(smem_addr(&tab.mid_ready), lane));
-        if (split > 1) ok = ok && bar_wait<true>(smem_addr(&tab.mid_ready), 0, gave_up);     // all have read: the buffers are free
+        if (split == 1 || send) {
+            if (lane == 0) bar_arrive(smem_addr(&tab.mid_ready));
+        } else {
+            if (lane < split) bar_arrive_cluster_release(in_cta(smem_addr(&tab.mid_ready_all), lane));
+            ok = ok && bar_wait<true>(smem_addr(&tab.mid_ready_all), 0, gave_up);            // all have read: the buffers are free
+        }
         // ---- blocks of the output. A warp has 32 rows and 64 columns of one: whole lines of `base` come into its buffer in the
         // background, a block ahead; there each lane adds its row's accumulators and rounds, and whole lines go out.
         char *const buffer = buffers + (2 * q + half) * 2 * kBufferBytes;
@@ -641,6 +677,10 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
             __syncwarp();                                                    // the buffer may be written again
         }
         copy_wait<0>();
+        for (int b = b_from; q >= quarters && !narrow && b < b_to; ++b, ++used) {                // lanes without rows
+            if (!(ok = ok && bar_wait(smem_addr(&tab.acc_full[used & 1]), (used >> 1) & 1, gave_up))) break;
+            if (lane == 0) bar_arrive(smem_addr(&tab.acc_empty[used & 1]));
+        }
         // ... of up to 32 rows: every quarter of the lanes has them, and each of the eight warps 16 of a block's columns, straight from
         // the accumulators: 256 rows on 64 adapters of 2048 x 8192 take 0.3 us a block so, with one quarter's two warps at work 0.9
         if (narrow) {
@@ -681,9 +721,10 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
         }
     }
     __syncwarp();
+    if (split > 1 && warp < 2) cluster_wait();
     tmem_fence_before();
     __syncthreads();
-    if (split > 1) cluster_sync();                                           // the others' reads come from this CTA's memory
+    if (split > 1 && !send) cluster_sync();                                  // the others' reads come from this CTA's memory
     tmem_fence_after();
     if (warp == 1) tmem_free<1>(tmem, 2 * kBlockColumns);
     if (threadIdx.x == 0 && tab.gave_up && a.status) atomicOr(a.status, EP_STATUS_TIMEOUT);
@@ -1068,6 +1109,13 @@ int launch_rank(const ep_adapter_t &m, TensorMapEncode encode, RankArgs a, const
     if (slots / a.split > adapters) {
         const int64_t even = (m.entries + slots / a.split - adapters - 1) / (slots / a.split - adapters);
         if (even > 64 && even < kRows) a.width = (int)(even + 3) / 4 * 4;
+    }
+    // A few more tiles (an adapter's last is half empty, on average) than fit at once would run by themselves at the end: then about
+    // two rounds of narrower ones (32768 rows, 128 adapters of 2048 x 1024: 70 us with 128 rows, 66 with 64).
+    const int64_t likely = m.entries / kRows + adapters / 2;
+    if (likely > slots && 2 * likely < 3 * slots) {
+        const int64_t even = m.entries / (2 * slots - slots / 16 - adapters / 2) + 1;
+        a.width = (int)((even < 64 ? 64 : even) + 3) / 4 * 4;
     }
     tiles = m.entries / a.width + adapters;
     return launch_cluster(rank_kernel<BACK>, ready, tiles + (plan.list ? 1 : 0), a.split, kThreads, kRankSmem, kRankSmem, stream, a, plan, map_first, map_second);
