@@ -2,9 +2,8 @@
 
     router -> layout + dispatch -> group -> gated experts -> combine        y = sum_k w_k W2_e( silu(Wg_e x) * (Wu_e x) )
 
-with the balance loss, and the gradients of the input, the router's logits and the experts' weights. The router's projection, the
-gradient of the combine's weights and the sum of the two branches' gradients are torch, and part of the times. Nothing waits for the GPU,
-so that a step can be captured in a CUDA graph.
+with the balance loss, and the gradients of the input, the router's logits and the experts' weights. The router's projection and its
+gradient are torch, and part of the times. Nothing waits for the GPU, so that a step can be captured in a CUDA graph.
 
     python examples/moe_layer.py [--tokens 4096 --hidden 2048 --inner 1024 --experts 128 --top-k 8 --ranks 8 --steps 10]
 
@@ -48,7 +47,7 @@ class MoELayer:
         self.ws = torch.empty(max(16, ep.ep_layout_workspace_bytes(T, K, E, R)), dtype=torch.uint8, device=device)
         self.recv, self.x, self.up, self.gate = rows(T * min(K, R), H), rows(P, H), rows(P, N), rows(P, N)
         self.hidden, self.out, self.y = rows(P, N), rows(P, H), rows(T, H)
-        self.ones = torch.ones(T, K, device=device)
+        self.d_out = rows(P, H)
 
     def forward(self, x):
         """x [T, H] bf16 -> y [T, H] bf16; the loss is in self.routing.loss."""
@@ -68,21 +67,16 @@ class MoELayer:
         """Gradients of sum(dy * y) + d_loss * loss: a dict of tensors."""
         T, H, N, E, K, R, lay, r = self.T, self.H, self.N, self.E, self.K, self.R, self.lay, self.routing
         P, off = T * K, lay.expert_offsets
-        slot = lay.pair_slot.long().clamp(min=0)
-        valid = lay.pair_slot >= 0
         # combine: a pair's output row gets its token's gradient times its weight, its weight the product of the two rows
-        w_pair = torch.zeros(P + 1, 1, device=dy.device)                    # entries that name no pair go to the last one
-        w_pair[torch.where(valid, slot, P), 0] = r.topk_weights
-        d_out = ep.ep_combine(dy, lay.pair_token.view(P, 1), w_pair[:P], torch.empty(P, H, dtype=torch.bfloat16, device=dy.device), 1, 1)
-        d_weights = torch.stack([(dy.float() * self.out[slot[:, k]].float()).sum(1) for k in range(K)], 1) * valid
+        d_weights = torch.empty(T, K, device=dy.device)
+        d_out = ep.ep_combine_backward(dy, lay.pair_slot, r.topk_weights, self.d_out, out=self.out, d_weights=d_weights, status=lay.status)
         down = ep.ep_expert_matmul_backward(d_out, self.hidden, off, self.w_down, status=lay.status)
         gate = ep.ep_expert_matmul_backward(down.dx, self.x, off, self.w_gate, pre=self.gate, activation=ep.ACT_SILU, operand=self.up,
                                             operand_op=ep.OPERAND_MUL, grads=ep.alloc_expert_grads(P, H, N, E, operand=True), status=lay.status)
         up = ep.ep_expert_matmul_backward(gate.doperand, self.x, off, self.w_up, status=lay.status)
-        # dispatch: a token's rows come back with unit weights, here from the pair space, once per branch
-        dx = torch.empty_like(dy)
-        ep.ep_combine(gate.dx, lay.pair_slot, self.ones, dx, E, R)
-        dx = dx + ep.ep_combine(up.dx, lay.pair_slot, self.ones, torch.empty_like(dy), E, R)
+        # dispatch: the gradients of a token's rows come back to it from the pair space, the second branch's onto the first's
+        dx = ep.ep_sort_backward(gate.dx, lay.pair_slot, torch.empty_like(dy), status=lay.status)
+        ep.ep_sort_backward(up.dx, lay.pair_slot, dx, add=dx, status=lay.status)
         d_logits = ep.ep_route_backward(self.logits, self.router, r, d_weights=d_weights, d_loss=d_loss)
         return {"x": dx.float() + d_logits @ self.w_router, "w_gate": gate.dweight, "w_up": up.dweight, "w_down": down.dweight,
                 "logits": d_logits, "topk_weights": d_weights}
