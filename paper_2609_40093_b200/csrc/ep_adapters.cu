@@ -28,6 +28,7 @@ constexpr int kLines = kRows * 128;       // bytes of 128 lines
 constexpr int kBlockColumns = 128;        // output columns of one accumulator
 constexpr int kMaxRank = 128;
 constexpr int kMaxCluster = 8;
+constexpr int kPartStages = 8;            // of the contracted features, for every CTA but one that shares them
 constexpr int kGradMost = 2 * 148;        // CTAs of the gradient kernel
 constexpr int kGradFeatures = kRows;      // of an item: an accumulator's lanes
 
@@ -247,7 +248,8 @@ struct RankArgs {
     uint16_t *mid;                        // [entries][rank], may be NULL
     long long rows, entries;
     const uint16_t *in_rows, *second;     // [rows][in]; the second product's weights
-    int in, out_features, rank, A, split, width;      // width: rows of a tile at most
+    int in, out_features, rank, A, width; // width: rows of a tile at most
+    int split, copies;                    // CTAs of a cluster, that share the contracted features; clusters that share the output's blocks
 };
 
 __device__ __forceinline__ void unpack8(const uint4 &v, float (&f)[8])
@@ -272,7 +274,7 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
 
     const int warp = __shfl_sync(kFullMask, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const int split = a.split, part = split > 1 ? (int)cluster_rank() : 0;
-    const int tile = (int)blockIdx.x / split - (plan.list != nullptr);
+    const int cluster = (int)blockIdx.x / split - (plan.list != nullptr), tile = cluster < 0 ? -1 : cluster / a.copies, copy = cluster - tile * a.copies;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kMaxStages; ++s) bar_init(smem_addr(&tab.full[s]), 1 + kEpilogueWarps), bar_init(smem_addr(&tab.empty[s]), 1);
@@ -326,7 +328,7 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
                 begin = end;
             }
         }
-        if (threadIdx.x == 0 && tile == 0 && part == 0 && a.status && __ldg(a.offsets + a.A) > a.entries) atomicOr(a.status, EP_STATUS_CAPACITY);
+        if (threadIdx.x == 0 && cluster == 0 && part == 0 && a.status && __ldg(a.offsets + a.A) > a.entries) atomicOr(a.status, EP_STATUS_CAPACITY);
         __syncthreads();
     }
     const int adapter = where[0], entry0 = where[1], m = where[2];
@@ -335,7 +337,8 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
     const int chunks = (a.rank + 63) / 64, r16 = (a.rank + 15) & ~15;
     const int all_k = (a.in + kTileK - 1) / kTileK, k_from = all_k * part / split, k_to = all_k * (part + 1) / split;
     const int blocks = a.out ? (a.out_features + kBlockColumns - 1) / kBlockColumns : 0;
-    const int b_from = (int)((long long)blocks * part / split), b_to = (int)((long long)blocks * (part + 1) / split);
+    const int sharing = split * a.copies, share = copy * split + part;
+    const int b_from = (int)((long long)blocks * share / sharing), b_to = (int)((long long)blocks * (share + 1) / sharing);
     const int stage_bytes = kLines + chunks * 8192, stages = kRingBytes / stage_bytes;
     const int quarters = (m + 31) / 32;                                      // of the lanes, with rows
     const bool narrow = quarters == 1;                                       // each quarter of the lanes holds the same rows, see below
@@ -519,7 +522,7 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[i] *= mid_scale;
             const uint4 v = pack8(f);
-            if (a.mid && row < m && col < a.rank && (!send || part == 0)) *reinterpret_cast<uint4 *>(a.mid + (size_t)(entry0 + row) * a.rank + col) = v;
+            if (a.mid && copy == 0 && row < m && col < a.rank && (!send || part == 0)) *reinterpret_cast<uint4 *>(a.mid + (size_t)(entry0 + row) * a.rank + col) = v;
             return v;
         };
         const auto operand_at = [&](int row, int col) { return (col >> 6) * kLines + swizzled(row, (col & 63) >> 3); };
@@ -1099,14 +1102,19 @@ int launch_rank(const ep_adapter_t &m, TensorMapEncode encode, RankArgs a, const
         else rc = BACK ? make_map(encode, &map_second, down, H, r, A, 64) : make_map(encode, &map_second, up, r, N, A, 128);
     }
     if (rc != EP_OK) return rc;
-    // At most this many tiles of `width` rows; two CTAs per SM. Clusters while they fit at once, then narrower tiles up to that number.
+    // At most this many tiles of `width` rows; two CTAs per SM. While they fit at once: clusters that share a tile's contracted features (at
+    // least eight stages a CTA: the exchange takes as long as that many), then clusters that share its output's blocks, each with a first
+    // product of its own (at least two blocks a CTA); then narrower tiles up to that number.
     const int64_t adapters = m.entries < m.num_adapters ? m.entries : m.num_adapters, slots = 2 * 148;
     int64_t tiles = m.entries / kRows + adapters;
-    const int stages = (a.in + kTileK - 1) / kTileK;
+    const int stages = (a.in + kTileK - 1) / kTileK, blocks = a.out ? (a.out_features + kBlockColumns - 1) / kBlockColumns : 0;
     a.split = 1;
-    while (a.split < kMaxCluster && tiles * a.split * 2 <= slots && stages >= 4 * a.split) a.split *= 2;
+    while (a.split < kMaxCluster && tiles * a.split * 2 <= slots && stages >= kPartStages * a.split) a.split *= 2;
+    a.copies = (int)(slots / (tiles * a.split));
+    if (a.copies > blocks / (2 * a.split)) a.copies = blocks / (2 * a.split);
+    if (a.copies < 1) a.copies = 1;
     a.width = kRows;
-    if (slots / a.split > adapters) {
+    if (a.copies == 1 && slots / a.split > adapters) {
         const int64_t even = (m.entries + slots / a.split - adapters - 1) / (slots / a.split - adapters);
         if (even > 64 && even < kRows) a.width = (int)(even + 3) / 4 * 4;
     }
@@ -1118,7 +1126,7 @@ int launch_rank(const ep_adapter_t &m, TensorMapEncode encode, RankArgs a, const
         a.width = (int)((even < 64 ? 64 : even) + 3) / 4 * 4;
     }
     tiles = m.entries / a.width + adapters;
-    return launch_cluster(rank_kernel<BACK>, ready, tiles + (plan.list ? 1 : 0), a.split, kThreads, kRankSmem, kRankSmem, stream, a, plan, map_first, map_second);
+    return launch_cluster(rank_kernel<BACK>, ready, tiles * a.copies + (plan.list ? 1 : 0), a.split, kThreads, kRankSmem, kRankSmem, stream, a, plan, map_first, map_second);
 }
 
 size_t up256(size_t n) { return (n + 255) & ~size_t(255); }
