@@ -5,7 +5,7 @@
 //             ddown[a] = dmid^T x                 dup[a] = scale[a] * dy^T mid                          sums over the rows
 //
 // The first two lines are one kernel, the rank kernel: in -> (rank) -> out with the weights read along either axis. A tile is
-// up to 128 rows of one adapter, the lanes of the accumulators; its rows may lie anywhere (tile::gather4 copies, four rows each).
+// up to 128 rows of one adapter, the lanes of the accumulators; its rows may lie anywhere.
 // The first product contracts the features into at most 128 columns of tensor memory; they are rounded to bf16 (they are the operand of
 // another product), laid out in shared memory as that product's row operand, and the output follows in blocks of 128 columns, whose
 // epilogue adds to `base` in fp32 and rounds once. Nothing between the products goes through memory.
@@ -99,7 +99,6 @@ constexpr int kThreads = 64 + 32 * kEpilogueWarps;
 constexpr int kRingBytes = 96 * 1024, kAreaBytes = 112 * 1024;
 constexpr int kBufferBytes = 32 * 128;    // an epilogue warp's 32 rows x 64 columns of bf16; two of them
 constexpr int kMaxStages = 4, kMaxUnits = 5;
-constexpr int kLag = 2;                   // stages a loader has in flight behind the one it asks for
 
 struct RankTables {
     uint64_t full[kMaxStages], empty[kMaxStages], unit_full[kMaxUnits], unit_empty[kMaxUnits], mid_full, mid_ready, mid_ready_all, acc_full[2], acc_empty[2],
@@ -265,7 +264,7 @@ __device__ __forceinline__ uint4 pack8(const float (&f)[8])
 // BACK: the weights are read along the other axis (up for the first product, down for the second), and the scale goes to `mid`.
 template <bool BACK>
 __global__ void __launch_bounds__(kThreads, 2)
-rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUtensorMap map_first, const __grid_constant__ CUtensorMap map_second)
+rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUtensorMap map_in, const __grid_constant__ CUtensorMap map_first, const __grid_constant__ CUtensorMap map_second)
 {
     extern __shared__ __align__(1024) char area[];                           // no static shared memory: it would push the area off its boundary
     RankTables &tab = *reinterpret_cast<RankTables *>(area + kAreaBytes);
@@ -277,7 +276,7 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
     const int cluster = (int)blockIdx.x / split - (plan.list != nullptr), tile = cluster < 0 ? -1 : cluster / a.copies, copy = cluster - tile * a.copies;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kMaxStages; ++s) bar_init(smem_addr(&tab.full[s]), 1 + kEpilogueWarps), bar_init(smem_addr(&tab.empty[s]), 1);
+        for (int s = 0; s < kMaxStages; ++s) bar_init(smem_addr(&tab.full[s]), a.index ? 3 : 1), bar_init(smem_addr(&tab.empty[s]), 1);
         for (int s = 0; s < kMaxUnits; ++s) bar_init(smem_addr(&tab.unit_full[s]), 1), bar_init(smem_addr(&tab.unit_empty[s]), 1);
         for (int s = 0; s < 2; ++s) bar_init(smem_addr(&tab.acc_full[s]), 1), bar_init(smem_addr(&tab.acc_empty[s]), kEpilogueWarps);
         bar_init(smem_addr(&tab.mid_full), 1);
@@ -341,6 +340,7 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
     const int b_from = (int)((long long)blocks * share / sharing), b_to = (int)((long long)blocks * (share + 1) / sharing);
     const int stage_bytes = kLines + chunks * 8192, stages = kRingBytes / stage_bytes;
     const int quarters = (m + 31) / 32;                                      // of the lanes, with rows
+    const bool boxes = a.index == nullptr;                                   // rows one behind the other
     const bool narrow = quarters == 1;                                       // each quarter of the lanes holds the same rows, see below
     // The parts that a cluster's CTAs have of the first product are sent to all of them where there is room for all of all beside the
     // ring; more of it is added up by shares (see below).
@@ -378,7 +378,7 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
 
     if (warp == 0 && elect_one()) {
         // ---- weights
-        const uint32_t bytes = (uint32_t)(BACK ? chunks * 8192 : r16 * 128);
+        const uint32_t bytes = (uint32_t)((BACK ? chunks * 8192 : r16 * 128) + (boxes ? quarters * 4096 : 0));
         int s = 0, phase = 1, sent = 0;
         bool ok = true;
         for (int k = k_from; k < k_to; ++k) {
@@ -390,6 +390,8 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
             } else {
                 tma_load<1>(dst, &map_first, k * kTileK, 0, adapter, full);
             }
+            if (boxes)                                                       // rows behind the tile's last are lanes that nobody looks at
+                for (int i = 0; i < quarters; ++i) tma_load<1>(dst - kLines + i * 4096, &map_in, k * kTileK, entry0 + 32 * i, 0, full);
             ++sent;
             if (b_to > b_from && b_to - b_from <= 16 && sent == min(stages, k_to - k_from)) {
                 // few blocks a CTA: nobody else has brought the second weights into L2
@@ -482,38 +484,28 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
         if (a.base && narrow && thread < m && b_to > b_from && row_of[thread] >= 0)       // few rows: their base into L2, under the first product
             l2_prefetch(a.base + (size_t)row_of[thread] * a.out_features + b_from * kBlockColumns,
                         (min(b_to * kBlockColumns, a.out_features) - b_from * kBlockColumns) * 2);
-        {
-            // ---- rows into the ring: eight lanes a row's line, four rows a warp, every 32 rows
-            const int line = 4 * (warp - 2) + (lane >> 3), piece = lane & 7, n_k = k_to - k_from;
-            const uint16_t *src[4];
-            bool there[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int row = row_of[line + 32 * i];
-                there[i] = row >= 0;
-                src[i] = a.in_rows + (size_t)max(row, 0) * a.in;
-            }
-            int s = 0, phase = 1, done = 0;
-            for (int i = 0; i < n_k + kLag; ++i) {
-                if (i < n_k) {
-                    if (!(ok = __all_sync(kFullMask, bar_wait(empty0 + 8 * s, phase, gave_up)))) break;
-                    const int col = (k_from + i) * kTileK + piece * 8, at = col < a.in ? col : 0;
-                    const uint32_t dst = ring + s * stage_bytes + swizzled(line, piece);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        if (line + 32 * j < m) copy16(dst + j * 32 * 128, src[j] + at, there[j] && col < a.in);
-                    if (++s == stages) s = 0, phase ^= 1;
+        if (!boxes && (warp - 2) >> 1 < stages) {
+            // ---- rows by index into the ring: two warps for each of its places, eight lanes a row's line. A thread waits for its own
+            // copies before it hands them to the tensor cores; the other places' are under way meanwhile.
+            const int place = (warp - 2) >> 1, line = (thread & 63) >> 3, piece = lane & 7;
+            const uint32_t full = full0 + 8 * place, empty = empty0 + 8 * place, dst = ring + place * stage_bytes + swizzled(line, piece);
+            int phase = 1;
+            for (int k = k_from + place; k < k_to; k += stages, phase ^= 1) {
+                if (!(ok = __all_sync(kFullMask, bar_wait(empty, phase, gave_up)))) break;
+                const int col = k * kTileK + piece * 8;
+                const bool real = col < a.in;
+                const uint16_t *const src = a.in_rows + (real ? col : 0);
+#pragma unroll 4
+                for (int j = line; j < m; j += 8) {
+                    const int row = row_of[j];
+                    copy16(dst + (j - line) * 128, src + (size_t)max(row, 0) * a.in, real && row >= 0);
                 }
                 copy_group();
-                if (i >= kLag) {
-                    copy_wait<kLag>();
-                    fence_async();
-                    __syncwarp();
-                    if (lane == 0) bar_arrive(full0 + 8 * done);
-                    if (++done == stages) done = 0;
-                }
+                copy_wait<0>();
+                fence_async();
+                __syncwarp();
+                if (lane == 0) bar_arrive(full);
             }
-            copy_wait<0>();
         }
         ok = ok && bar_wait(smem_addr(&tab.mid_full), 0, gave_up);
         tmem_fence_after();
@@ -583,11 +575,17 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
                 const int row = i / groups, col = i % groups * 8;
                 const uint32_t lo = smem_addr(exchange + ex_at(row, col / 4)), hi = smem_addr(exchange + ex_at(row, col / 4 + 1));
                 float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                for (int s = 0; s < split; s += 2) {                         // split is a power of two; four reads under way
-                    const float4 l0 = load_cluster(in_cta(lo, s)), h0 = load_cluster(in_cta(hi, s));
-                    const float4 l1 = load_cluster(in_cta(lo, s + 1)), h1 = load_cluster(in_cta(hi, s + 1));
-                    f[0] += l0.x, f[1] += l0.y, f[2] += l0.z, f[3] += l0.w, f[4] += h0.x, f[5] += h0.y, f[6] += h0.z, f[7] += h0.w;
-                    f[0] += l1.x, f[1] += l1.y, f[2] += l1.z, f[3] += l1.w, f[4] += h1.x, f[5] += h1.y, f[6] += h1.z, f[7] += h1.w;
+                for (int s = 0; s < split; s += 4) {                         // split is 2, 4 or 8; eight reads under way
+                    float4 l[4], h[4];
+#pragma unroll
+                    for (int p = 0; p < 4; ++p)
+                        if (p < split) l[p] = load_cluster(in_cta(lo, s + p)), h[p] = load_cluster(in_cta(hi, s + p));
+#pragma unroll
+                    for (int p = 0; p < 4; ++p)
+                        if (p < split) {
+                            f[0] += l[p].x, f[1] += l[p].y, f[2] += l[p].z, f[3] += l[p].w;
+                            f[4] += h[p].x, f[5] += h[p].y, f[6] += h[p].z, f[7] += h[p].w;
+                        }
                 }
                 const uint4 v = rounded(row, col, f);
                 const uint32_t to = ring + operand_at(row, col);
@@ -1095,8 +1093,9 @@ int launch_rank(const ep_adapter_t &m, TensorMapEncode encode, RankArgs a, const
     a.rows = m.rows, a.entries = m.entries, a.rank = m.rank, a.A = m.num_adapters;
     a.in = BACK ? m.out_features : m.in_features, a.out_features = BACK ? m.in_features : m.out_features;
     a.in_rows = static_cast<const uint16_t *>(in), a.second = static_cast<const uint16_t *>(BACK ? down : up);
-    CUtensorMap map_first, map_second;
-    int rc = BACK ? make_map(encode, &map_first, up, r, N, A, 64) : make_map(encode, &map_first, down, H, r, A, (uint32_t)((r + 15) & ~15));
+    CUtensorMap map_in = {}, map_first, map_second;
+    int rc = a.index ? EP_OK : make_map(encode, &map_in, in, a.in, m.rows, 1, 32);
+    if (rc == EP_OK) rc = BACK ? make_map(encode, &map_first, up, r, N, A, 64) : make_map(encode, &map_first, down, H, r, A, (uint32_t)((r + 15) & ~15));
     if (rc == EP_OK) {
         if (!a.out) map_second = map_first;
         else rc = BACK ? make_map(encode, &map_second, down, H, r, A, 64) : make_map(encode, &map_second, up, r, N, A, 128);
@@ -1126,7 +1125,7 @@ int launch_rank(const ep_adapter_t &m, TensorMapEncode encode, RankArgs a, const
         a.width = (int)((even < 64 ? 64 : even) + 3) / 4 * 4;
     }
     tiles = m.entries / a.width + adapters;
-    return launch_cluster(rank_kernel<BACK>, ready, tiles * a.copies + (plan.list ? 1 : 0), a.split, kThreads, kRankSmem, kRankSmem, stream, a, plan, map_first, map_second);
+    return launch_cluster(rank_kernel<BACK>, ready, tiles * a.copies + (plan.list ? 1 : 0), a.split, kThreads, kRankSmem, kRankSmem, stream, a, plan, map_in, map_first, map_second);
 }
 
 size_t up256(size_t n) { return (n + 255) & ~size_t(255); }
