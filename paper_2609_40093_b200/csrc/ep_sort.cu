@@ -16,7 +16,9 @@
 namespace ep {
 namespace {
 
-constexpr int kBlock = 128;
+constexpr int kBlock = 128, kWide = 512;   // threads of a CTA; kWide where a whole CTA of that many has a token
+template <int G>
+constexpr int kBlockOf = G > kBlock ? G : kBlock;
 constexpr int kChunk = 8;   // rows in flight per column
 
 // CTAs per SM that the compiler leaves registers for. Left to itself it takes 125 and more where there are products, to have several
@@ -118,7 +120,7 @@ __device__ __forceinline__ Picks load_picks(const RowArgs &a, int t)
 template <int G, int CHUNKS, bool SHARED_ONCE>
 __device__ __forceinline__ void store_dots(const RowArgs &a, const Picks &p, float (&dot)[CHUNKS][kChunk], int t)
 {
-    __shared__ float part[kBlock / 32][CHUNKS * kChunk];
+    __shared__ float part[kBlockOf<G> / 32][CHUNKS * kChunk];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
@@ -137,10 +139,10 @@ __device__ __forceinline__ void store_dots(const RowArgs &a, const Picks &p, flo
 }
 
 template <int G, int CHUNKS, bool DOTS>
-__global__ void __launch_bounds__(kBlock, resident(true, CHUNKS, DOTS))
+__global__ void __launch_bounds__(kBlockOf<G>, G > kBlock ? 1 : resident(true, CHUNKS, DOTS))
 spread_rows_kernel(const RowArgs a)
 {
-    const int g = threadIdx.x % G, t = blockIdx.x * (kBlock / G) + threadIdx.x / G;
+    const int g = threadIdx.x % G, t = blockIdx.x * (kBlockOf<G> / G) + threadIdx.x / G;
     pdl_trigger();                                                       // the next kernel's CTAs may take the places that get free
     pdl_wait();                                                          // nothing is read or written before this
     const Picks p = load_picks<true>(a, t);
@@ -203,10 +205,10 @@ spread_rows_kernel(const RowArgs a)
 }
 
 template <int G, int CHUNKS, bool DOTS>
-__global__ void __launch_bounds__(kBlock, resident(false, CHUNKS, DOTS))
+__global__ void __launch_bounds__(kBlockOf<G>, G > kBlock ? 1 : resident(false, CHUNKS, DOTS))
 gather_rows_kernel(const RowArgs a)
 {
-    const int g = threadIdx.x % G, t = blockIdx.x * (kBlock / G) + threadIdx.x / G;
+    const int g = threadIdx.x % G, t = blockIdx.x * (kBlockOf<G> / G) + threadIdx.x / G;
     pdl_trigger();
     pdl_wait();
     const Picks p = load_picks<false>(a, t);
@@ -304,7 +306,12 @@ int launch_group(const RowArgs &a, bool few_columns, cudaStream_t stream)
     // Threads per token: a row's columns are dealt out to more threads as there are more of them. Gather with products has a thread do one
     // column after the other, and wants few (8192 x 1024 elements, 4 picks: 22.3 us with 128 threads, 29.3 with 64; the others 10 % and
     // more the other way round).
-    if (vpr <= 64)
+    // Few tokens: 512 threads for each, so that all of a row's columns are under way at once. With at most a token per SM that is faster
+    // for all (140 tokens of 4096 elements, 8 picks: gradients 6.0 -> 3.2 and 6.3 -> 3.7 us); with more, CTAs that read the table hold too many
+    // registers (560 x 2160, 7 picks: 8.0 -> 9.3), while those that only write gain on (7.5 -> 5.2; 1000 x 7168, 8 picks: 27.5 -> 22.6).
+    if (vpr > kBlock && a.T <= (a.table ? 148 : 8 * 148))
+        e = launch_pdl(Kernel<kWide, CHUNKS, DOTS>::get(), dim3(a.T), dim3(kWide), 0, stream, a);
+    else if (vpr <= 64)
         e = launch_pdl(Kernel<32, CHUNKS, DOTS>::get(), dim3(ceil_div(a.T, kBlock / 32)), dim3(kBlock), 0, stream, a);
     else if (vpr < (few_columns ? 65 : 256))
         e = launch_pdl(Kernel<64, CHUNKS, DOTS>::get(), dim3(ceil_div(a.T, kBlock / 64)), dim3(kBlock), 0, stream, a);

@@ -45,7 +45,7 @@ def _data(T, K, H, seed, masked=0.2, shared=False, spare=3):
     return slot, w, table, x, add, named
 
 
-SHAPES = [(1, 1, 8), (3, 2, 264), (64, 2, 512), (37, 6, 520), (130, 8, 2048), (33, 8, 2056), (5, 9, 72), (19, 16, 1032), (7, 32, 136), (9, 17, 2064)]
+SHAPES = [(1, 1, 8), (3, 2, 264), (64, 2, 512), (37, 6, 520), (130, 8, 2048), (33, 8, 2056), (5, 9, 72), (19, 16, 1032), (7, 32, 136), (9, 17, 2064), (2, 11, 6304), (149, 3, 1096), (700, 1, 1032)]
 
 
 @pytest.mark.parametrize("shared", [False, True])
