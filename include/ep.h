@@ -706,7 +706,9 @@ int ep_dropout(const void *x, const void *residual, void *y, int64_t rows, int32
  * to bf16 once. Adapters without entries get zero ddown and dup. No sum depends on an
  * order of atomics: the same call gives the same bits every time (ddown alone may differ in
  * the last bit from ddown together with dup). workspace (for ddown or dup): ep_adapter_matmul_backward_workspace_bytes()
- * bytes (device, 256-byte aligned), uninitialised.
+ * bytes (device, 256-byte aligned), uninitialised; calls that share one must be
+ * stream-ordered. Offsets that decrease and so name more than `entries` entries leave ddown
+ * and dup unwritten, with EP_STATUS_CAPACITY.
  */
 typedef struct {
     int64_t rows;    /* of x, base and y */

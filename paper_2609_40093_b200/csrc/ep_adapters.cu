@@ -138,9 +138,11 @@ struct PlanArgs {
     int *arrived;                         // [counters], to be zeroed
     int *pieces;                          // [2]: pieces with entries, and all
     GradPiece *list;                      // NULL: no plan
+    int32_t *status;
 };
 
 struct PlanTables {
+    unsigned long long entries;
     int most, sum, parts[kGradCuts], warp_sum[2][kThreads / 32];
     int bins[(kGradBins + 1) * kThreads]; // [bin][thread] pieces, then where they start
     int stages[kMaxExperts];
@@ -165,17 +167,27 @@ __device__ __forceinline__ int block_scan(int v, int *warp_sum)
 __device__ void plan_pieces(const PlanArgs &a, PlanTables &tab)
 {
     const int per = (a.A + kThreads - 1) / kThreads, from = min(a.A, (int)threadIdx.x * per), to = min(a.A, from + per), lane = threadIdx.x & 31;
-    if (threadIdx.x == 0) tab.most = 0, tab.sum = 0;
+    if (threadIdx.x == 0) tab.most = 0, tab.sum = 0, tab.entries = 0;
     if (threadIdx.x < kGradCuts) tab.parts[threadIdx.x] = 0;
     for (int i = threadIdx.x; i < a.counters; i += kThreads) a.arrived[i] = 0;
     for (int b = 0; b <= kGradBins; ++b) tab.bins[b * kThreads + threadIdx.x] = 0;
     __syncthreads();
     const auto begin_of = [&](int e) { return segment_bound(__ldg(a.offsets + e), a.entries); };
     int most = 0, sum = 0;
+    unsigned long long entries = 0;
     for (int e = from; e < to; ++e) {
-        const int n = quotient_up(max(0, begin_of(e + 1) - begin_of(e)), kTileK);
+        const int count = max(0, begin_of(e + 1) - begin_of(e)), n = quotient_up(count, kTileK);
         tab.stages[e] = n;
+        entries += count;
         most = max(most, n), sum += n;
+    }
+    atomicAdd(&tab.entries, entries);
+    __syncthreads();
+    if (threadIdx.x == 0 && a.status && (tab.entries > (unsigned long long)a.entries || __ldg(a.offsets + a.A) > a.entries))
+        atomicOr(a.status, EP_STATUS_CAPACITY);
+    if (tab.entries > (unsigned long long)a.entries) {                       // offsets that decrease: the list has no room for what they name
+        if (threadIdx.x == 0) a.pieces[0] = 0, a.pieces[1] = 0;
+        return;
     }
     most = __reduce_max_sync(kFullMask, most), sum = __reduce_add_sync(kFullMask, sum);
     if (lane == 0 && sum) atomicMax(&tab.most, most), atomicAdd(&tab.sum, sum);
@@ -321,7 +333,7 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
             for (int i = from; i < to; ++i) {
                 const int end = segment_bound(__ldg(a.offsets + i + 1), a.entries), count = max(0, end - begin);
                 const int pieces = quotient_up(count, a.width);
-                if (tile < run + pieces) {
+                if (tile >= run && tile < run + pieces) {
                     const int width = (quotient_up(count, pieces) + 3) & ~3, piece = tile - run;
                     where[0] = i;
                     where[1] = begin + piece * width;
@@ -1231,6 +1243,7 @@ extern "C" int ep_adapter_matmul_backward(const ep_adapter_t *m, const void *dy,
         pieces.counters = (int)plan.counters;
         pieces.pieces = reinterpret_cast<int *>(ws), pieces.arrived = pieces.pieces + 2;
         pieces.list = reinterpret_cast<GradPiece *>(ws + plan.counter_bytes);
+        pieces.status = status;
     }
     TensorMapEncode encode;
     rc = tensor_map_encoder(&encode);

@@ -189,6 +189,24 @@ def test_offsets_and_rows_out_of_range():
     assert float((grads.ddown.double().cpu() - want[1]).norm() / want[1].norm()) < 2 * HALF
 
 
+def test_offsets_that_decrease_are_refused_on_the_device():
+    """They name every entry many times over: more pieces than the workspace has room for."""
+    T, H, N, r, A = 3000, 64, 64, 8, 64
+    x = torch.randn(T, H, device="cuda").to(BF)
+    ad = ep.Adapters((torch.randn(A, r, H, device="cuda") / 8).to(BF), torch.randn(A, N, r, device="cuda").to(BF))
+    off = torch.tensor([T * (i % 2) for i in range(A + 1)], dtype=torch.int32, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    mid, grads = torch.zeros(T, r, dtype=BF, device="cuda"), ep.alloc_adapter_grads(x, ad)
+    ws = torch.full((grads.workspace.numel() + 512,), 0x5A, dtype=torch.uint8, device="cuda")
+    grads.workspace, grads.ddown, grads.dup = ws[256:-256], grads.ddown.fill_(3.0), grads.dup.fill_(3.0)
+    for dx in (grads.dx, None):
+        grads.dx = dx
+        status.zero_()
+        ep.ep_adapter_matmul_backward(x, x, off, ad, mid, grads, status=status)
+        assert int(status) == ep.STATUS_CAPACITY and (grads.ddown == 3).all() and (grads.dup == 3).all()
+        assert (ws[:256] == 0x5A).all() and (ws[-256:] == 0x5A).all()
+
+
 def test_no_entries():
     T, H, N, r, A = 4, 64, 64, 8, 3
     x = torch.ones(T, H, dtype=BF, device="cuda")
