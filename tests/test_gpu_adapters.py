@@ -77,7 +77,8 @@ CASES = [  # rows, H, N, r, A, distribution, mixed, share without
     (130, 200, 8, 128, 2, "one", False, 0.0), (128, 8, 200, 64, 1, "one", False, 0.0), (129, 2048, 384, 72, 5, "few", False, 0.2),
     (700, 264, 520, 40, 3, "few", True, 0.3), (1003, 520, 264, 24, 12, "few", True, 0.1), (1500, 4096, 128, 128, 1, "one", True, 0.0),
     (2000, 128, 2048, 32, 300, "few", False, 0.0), (300, 1024, 1024, 112, 2, "spread", True, 0.0), (3000, 768, 640, 64, 2, "spread", False, 0.0),
-    (40, 640, 640, 8, 4096, "few", True, 0.5),
+    (40, 640, 640, 8, 4096, "few", True, 0.5), (50, 1024, 1544, 32, 1, "one", True, 0.0), (64, 136, 2056, 128, 1, "one", False, 0.0),
+    (190, 2048, 520, 24, 4, "spread", True, 0.0), (33, 4096, 136, 16, 1, "one", False, 0.0),
 ]
 
 
