@@ -526,11 +526,12 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
         }
         ok = ok && bar_wait(smem_addr(&tab.mid_full), 0, gave_up);
         tmem_fence_after();
-        // 8 columns of a row, rounded: the second product's operand, and `mid`
+        // 8 columns of a row, rounded: the second product's operand, and `mid`. Columns from the rank on, up to the step of 16, are zeros whatever
+        // the row holds: an infinite element times the first weights' padding is NaN, which the second's would not take away.
         const auto rounded = [&](int row, int col, float (&f)[8]) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[i] *= mid_scale;
-            const uint4 v = pack8(f);
+            const uint4 v = col < a.rank ? pack8(f) : make_uint4(0u, 0u, 0u, 0u);
             if (a.mid && copy == 0 && row < m && col < a.rank && (!send || part == 0)) *reinterpret_cast<uint4 *>(a.mid + (size_t)(entry0 + row) * a.rank + col) = v;
             return v;
         };
