@@ -691,8 +691,8 @@ int ep_dropout(const void *x, const void *residual, void *y, int64_t rows, int32
  * adapter of its own. adapter_offsets [num_adapters+1] starts at 0 and does not decrease;
  * an offset past `entries` is cut there and sets EP_STATUS_CAPACITY. Entries from
  * adapter_offsets[num_adapters] on are not used, and rows that no entry names not
- * touched. A row outside [0, rows) is skipped (its mid is 0) with EP_STATUS_BAD_INDEX. An
- * entry list that names a row twice loses one of the two sums.
+ * touched. A row outside [0, rows) is skipped (its mid is 0) with EP_STATUS_BAD_INDEX, also
+ * where rows is 0. An entry list that names a row twice loses one of the two sums.
  * Limits: in_features and out_features multiples of 8, from 8 to 2^24 - 8; rank a multiple
  * of 8, from 8 to 128; 1 <= num_adapters <= 4096; rows, entries < 2^31; entries <= rows
  * without row_index. y, mid may not overlap x or weights. Waits inside the kernels are

@@ -1146,6 +1146,32 @@ int launch_rank(const ep_adapter_t &m, TensorMapEncode encode, RankArgs a, const
     return launch_cluster(rank_kernel<BACK>, ready, tiles * a.copies + (plan.list ? 1 : 0), a.split, kThreads, kRankSmem, kRankSmem, stream, a, plan, map_in, map_first, map_second);
 }
 
+// A call without rows: each entry that an adapter has names one that does not exist, and its mid is 0. One without entries, too: the offsets
+// may still name some.
+__global__ void __launch_bounds__(kThreads)
+no_rows_kernel(const int32_t *offsets, int A, long long entries, int rank, uint16_t *mid, int32_t *status)
+{
+    pdl_trigger();
+    pdl_wait();
+    const int32_t end = __ldg(offsets + A);
+    const int named = segment_bound(end, entries), first = blockIdx.x * kThreads + threadIdx.x;
+    const int found = (end > entries ? EP_STATUS_CAPACITY : 0) | (named > 0 ? EP_STATUS_BAD_INDEX : 0);
+    if (first == 0 && status && found) atomicOr(status, found);
+    const long long vectors = mid ? (long long)named * (rank / 8) : 0;
+    for (long long i = first; i < vectors; i += (long long)gridDim.x * kThreads) reinterpret_cast<uint4 *>(mid)[i] = make_uint4(0u, 0u, 0u, 0u);
+}
+int without_rows(const ep_adapter_t &m, const int32_t *offsets, void *mid, int32_t *status, cudaStream_t stream)
+{
+    if (m.entries == 0 && (!status || !offsets)) return EP_OK;               // nothing to write, nobody to tell
+    if (!offsets) return EP_ERR_NULL;
+    if (m.entries > 0 && !aligned16(mid)) return EP_ERR_INVALID_ARG;
+    const int64_t blocks = mid ? (m.entries * (m.rank / 8) + kThreads - 1) / kThreads : 1, most = 8 * 148;
+    EP_CUDA_TRY(launch_pdl(no_rows_kernel, dim3((unsigned)(blocks < 1 ? 1 : blocks < most ? blocks : most)), dim3(kThreads), 0, stream, offsets,
+                           m.num_adapters, (long long)m.entries, m.rank, static_cast<uint16_t *>(mid), status));
+    EP_LAUNCH_CHECK(1);
+    return EP_OK;
+}
+
 size_t up256(size_t n) { return (n + 255) & ~size_t(255); }
 
 // The gradient kernel's launch and workspace.
@@ -1189,7 +1215,7 @@ extern "C" int ep_adapter_matmul(const ep_adapter_t *m, const void *x, const int
     int rc = check_adapter(m);
     if (rc != EP_OK) return rc;
     if (!row_index && m->entries > m->rows) return EP_ERR_INVALID_ARG;
-    if (m->entries == 0 || m->rows == 0) return EP_OK;
+    if (m->entries == 0 || m->rows == 0) return without_rows(*m, adapter_offsets, mid, status, static_cast<cudaStream_t>(stream));
     if (!x || !adapter_offsets || !down || (y && !up) || (!y && !mid)) return EP_ERR_NULL;
     if (!aligned16(x) || !aligned16(down) || !aligned16(up) || !aligned16(base) || !aligned16(y) || !aligned16(mid)) return EP_ERR_INVALID_ARG;
     TensorMapEncode encode;
@@ -1218,7 +1244,7 @@ extern "C" int ep_adapter_matmul_backward(const ep_adapter_t *m, const void *dy,
     int rc = check_adapter(m);
     if (rc != EP_OK) return rc;
     if (!row_index && m->entries > m->rows) return EP_ERR_INVALID_ARG;
-    if (!dx && !ddown && !dup) return EP_ERR_NULL;
+    if (!dx && !ddown && !dup && m->rows > 0) return EP_ERR_NULL;            // a dx without rows has no address
     const size_t A = m->num_adapters, r = m->rank, H = m->in_features, N = m->out_features;
     if (!aligned16(dy) || !aligned16(x) || !aligned16(down) || !aligned16(up) || !aligned16(mid) || !aligned16(base) || !aligned16(dx) ||
         !aligned16(ddown) || !aligned16(dup) || (reinterpret_cast<uintptr_t>(workspace) & 255u))
@@ -1227,7 +1253,7 @@ extern "C" int ep_adapter_matmul_backward(const ep_adapter_t *m, const void *dy,
     if (m->entries == 0 || m->rows == 0) {
         if (ddown) EP_CUDA_TRY(cudaMemsetAsync(ddown, 0, A * r * H * 2, stream));
         if (dup) EP_CUDA_TRY(cudaMemsetAsync(dup, 0, A * N * r * 2, stream));
-        return EP_OK;
+        return without_rows(*m, adapter_offsets, nullptr, status, stream);
     }
     if (!dy || !adapter_offsets || ((dx || ddown) && !up) || (dx && !down) || (ddown && !x) || (dup && !mid)) return EP_ERR_NULL;
     if ((ddown || dup) && !workspace) return EP_ERR_NULL;
