@@ -508,7 +508,7 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
             const uint32_t full = full0 + 8 * place, empty = empty0 + 8 * place, dst = ring + place * stage_bytes + swizzled(line, piece);
             int phase = 1;
             for (int k = k_from + place; k < k_to; k += stages, phase ^= 1) {
-                if (!(ok = __all_sync(kFullMask, bar_wait(empty, phase, gave_up)))) break;
+                if (!(ok = warp_wait(empty, phase, gave_up))) break;
                 const int col = k * kTileK + piece * 8;
                 const bool real = col < a.in;
                 const uint16_t *const src = a.in_rows + (real ? col : 0);
@@ -524,7 +524,7 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
                 if (lane == 0) bar_arrive(full);
             }
         }
-        ok = ok && bar_wait(smem_addr(&tab.mid_full), 0, gave_up);
+        ok = ok && warp_wait(smem_addr(&tab.mid_full), 0, gave_up);
         tmem_fence_after();
         // 8 columns of a row, rounded: the second product's operand, and `mid`. Columns from the rank on, up to the step of 16, are zeros whatever
         // the row holds: an infinite element times the first weights' padding is NaN, which the second's would not take away.
@@ -575,7 +575,7 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
             // ---- the parts of all CTAs: each CTA adds a share of the elements, in the order of the CTAs, and tells all of them
             __syncwarp();
             if (lane < split) bar_arrive_cluster_release(in_cta(smem_addr(&tab.ex_full), lane));
-            ok = bar_wait<true>(smem_addr(&tab.ex_full), 0, gave_up);
+            ok = warp_wait<true>(smem_addr(&tab.ex_full), 0, gave_up);
             const int groups = r16 / 8;
             for (int i = thread; ok && send && i < m * groups; i += 32 * kEpilogueWarps) {
                 const int row = i / groups, col = i % groups * 8;
@@ -622,7 +622,7 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
             if (lane == 0) bar_arrive(smem_addr(&tab.mid_ready));
         } else {
             if (lane < split) bar_arrive_cluster_release(in_cta(smem_addr(&tab.mid_ready_all), lane));
-            ok = ok && bar_wait<true>(smem_addr(&tab.mid_ready_all), 0, gave_up);            // all have read: the buffers are free
+            ok = ok && warp_wait<true>(smem_addr(&tab.mid_ready_all), 0, gave_up);           // all have read: the buffers are free
         }
         // ---- blocks of the output. A warp has 32 rows and 64 columns of one: whole lines of `base` come into its buffer in the
         // background, a block ahead; there each lane adds its row's accumulators and rounds, and whole lines go out.
@@ -652,7 +652,7 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
             request(b + 1, acc ^ 1);
             copy_wait<1>();
             __syncwarp();
-            if (!(ok = bar_wait(smem_addr(&tab.acc_full[acc]), (used >> 1) & 1, gave_up))) break;
+            if (!(ok = warp_wait(smem_addr(&tab.acc_full[acc]), (used >> 1) & 1, gave_up))) break;
             tmem_fence_after();
             char *const mine = buffer + acc * kBufferBytes;
             // 16 columns at a time, the next ones on their way
@@ -697,7 +697,7 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
         }
         copy_wait<0>();
         for (int b = b_from; q >= quarters && !narrow && b < b_to; ++b, ++used) {                // lanes without rows
-            if (!(ok = ok && bar_wait(smem_addr(&tab.acc_full[used & 1]), (used >> 1) & 1, gave_up))) break;
+            if (!(ok = ok && warp_wait(smem_addr(&tab.acc_full[used & 1]), (used >> 1) & 1, gave_up))) break;
             if (lane == 0) bar_arrive(smem_addr(&tab.acc_empty[used & 1]));
         }
         // ... of up to 32 rows: every quarter of the lanes has them, and each of the eight warps 16 of a block's columns, straight from
@@ -717,7 +717,7 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
             ask(b_from);
             for (int b = b_from; ok && b < b_to; ++b, ++used) {
                 const int acc = used & 1;
-                if (!(ok = bar_wait(smem_addr(&tab.acc_full[acc]), (used >> 1) & 1, gave_up))) break;
+                if (!(ok = warp_wait(smem_addr(&tab.acc_full[acc]), (used >> 1) & 1, gave_up))) break;
                 tmem_fence_after();
                 uint32_t v[16];
                 tmem_request16(tmem + (uint32_t(q * 32) << 16) + acc * kBlockColumns + first, v);
@@ -829,7 +829,8 @@ adapter_grad_kernel(const GradArgs a, const __grid_constant__ GradMaps maps)
     GradItem t;
     int slot = 0, slot_phase = 0;
     const auto next = [&](bool warp_wide) {
-        if (!bar_wait(smem_addr(&item_full_[slot]), slot_phase, gave_up)) return false;
+        const uint32_t full = smem_addr(&item_full_[slot]);
+        if (!(warp_wide ? warp_wait(full, slot_phase, gave_up) : bar_wait(full, slot_phase, gave_up))) return false;
         t = items_[slot];
         if (warp_wide) __syncwarp();
         if (!warp_wide || lane == 0) bar_arrive(smem_addr(&item_empty_[slot]));
@@ -879,7 +880,7 @@ adapter_grad_kernel(const GradArgs a, const __grid_constant__ GradMaps maps)
             const uint16_t *const ranks = (t.up ? a.mid : a.dmid) + (real ? piece * 8 : 0);
             int k = t.p.k_from + skip;
             for (; k < t.p.k_to; k += stages) {
-                if (!(ok = __all_sync(kFullMask, bar_wait(empty0 + 8 * s, phase, gave_up)))) break;
+                if (!(ok = warp_wait(empty0 + 8 * s, phase, gave_up))) break;
                 phase ^= 1;
                 if (plain && (k + 1) * (long long)kTileK <= t.p.n) {
                     if (lane == 0) {
@@ -956,11 +957,22 @@ adapter_grad_kernel(const GradArgs a, const __grid_constant__ GradMaps maps)
         // ---- accumulators out, through shared memory, or as a part of an item's sums
         const int q = warp & 3, thread = threadIdx.x - 32;
         const auto together = [] { asm volatile("bar.sync 1, 128;" ::: "memory"); };        // the four warps
+        // together(), and whether all of them go on: each may have given up by itself, and none must wait there for one that has left
+        const auto agreed = [](bool go) {
+            uint32_t all;
+            asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n bar.red.and.pred p, 1, 128, q;\n selp.u32 %0, 1, 0, p;\n}"
+                         : "=r"(all)
+                         : "r"(uint32_t(go))
+                         : "memory");
+            return all != 0;
+        };
         int used = 0;
-        bool ok = true;
-        while (ok && next(true)) {
+        for (;;) {
+            bool go = next(true);
+            const float scale = go && t.up && a.scale ? __ldg(a.scale + t.p.adapter) : 1.f;
+            if (go && t.p.n) go = warp_wait(smem_addr(&acc_full_[used & 1]), (used >> 1) & 1, gave_up);
+            if (!agreed(go)) break;                                          // no wait that may run out from here to the next item
             const int acc = used & 1, features = t.up ? a.N : a.H, m0 = t.m0, tiles = a.tiles_down + a.tiles_up;
-            const float scale = t.up && a.scale ? __ldg(a.scale + t.p.adapter) : 1.f;
             const bool whole = t.p.of == 1;
             float *const mine = a.parts + (((size_t)(t.p.part + t.p.number) * tiles + t.f)) * r16 * kRows;
             // 8 results: ddown, 8 features of a rank; dup, 8 ranks of a feature
@@ -980,10 +992,9 @@ adapter_grad_kernel(const GradArgs a, const __grid_constant__ GradMaps maps)
                 }
                 continue;
             }
-            ok = bar_wait(smem_addr(&acc_full_[acc]), (used >> 1) & 1, gave_up);
             tmem_fence_after();
             ++used;
-            for (int c0 = 0; ok && c0 < r16; c0 += 32) {
+            for (int c0 = 0; c0 < r16; c0 += 32) {
                 uint32_t v[32];
                 tmem_load32(tmem + (uint32_t(q * 32) << 16) + acc * a.columns + c0, v);
                 if (c0 + 32 >= r16) {                                        // this warp has read its last column
@@ -1021,7 +1032,7 @@ adapter_grad_kernel(const GradArgs a, const __grid_constant__ GradMaps maps)
                     together();                                              // `out` may be written again
                 }
             }
-            if (whole || !ok) continue;
+            if (whole) continue;
             // who comes last adds the parts
             __threadfence();
             together();

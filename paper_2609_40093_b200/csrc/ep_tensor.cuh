@@ -85,6 +85,14 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
     }
 }
 
+// The same by a whole warp, with one answer for all its lanes: a lane that sees the phase end while another gives up must not go on alone,
+// since what follows are instructions of the whole warp.
+template <bool CLUSTER = false>
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *gave_up)
+{
+    return __all_sync(kFullMask, bar_wait<CLUSTER>(bar, parity, gave_up));
+}
+
 __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes)
 {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
