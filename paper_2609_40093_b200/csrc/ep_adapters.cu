@@ -743,7 +743,7 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
     if (split > 1 && warp < 2) cluster_wait();
     tmem_fence_before();
     __syncthreads();
-    if (split > 1 && !send) cluster_sync();                                  // the others' reads come from this CTA's memory
+    if (split > 1) cluster_sync();                                           // the others read from this CTA's memory and, where it gave up, may still write to it
     tmem_fence_after();
     if (warp == 1) tmem_free<1>(tmem, 2 * kBlockColumns);
     if (threadIdx.x == 0 && tab.gave_up && a.status) atomicOr(a.status, EP_STATUS_TIMEOUT);

@@ -54,3 +54,10 @@ def test_the_warps_that_empty_an_accumulator_leave_together():
     assert vote and "together()" not in loop[:vote.start()]
     assert not re.search(r"_wait\(|next\(|\bbreak;|\breturn\b", re.sub(r"if \(c0 [^;]*\) break;", "", loop[vote.end():]))
     assert text.count("together();") == loop.count("together();")
+
+
+def test_a_block_of_a_cluster_leaves_when_all_are_done():
+    """What is left of a block that has exited cannot be written to; one that gave up does not know whether the others still will."""
+    text = _kernel("rank_kernel")
+    end = text[text.rindex("__syncthreads();"):]
+    assert "if (split > 1) cluster_sync();" in end and "return;" not in text[text.index("cluster_arrive();"):]
