@@ -107,7 +107,7 @@ constexpr int kMaxStages = 4, kMaxUnits = 5;
 
 struct RankTables {
     uint64_t full[kMaxStages], empty[kMaxStages], unit_full[kMaxUnits], unit_empty[kMaxUnits], mid_full, mid_ready, mid_ready_all, acc_full[2], acc_empty[2],
-        ex_full;
+        ex_full, done;
     uint32_t tmem_slot;
     int gave_up, warp_sum[kThreads / 32], where[3];
     int row_of[kRows];
@@ -297,6 +297,7 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
         for (int s = 0; s < kMaxUnits; ++s) bar_init(smem_addr(&tab.unit_full[s]), 1), bar_init(smem_addr(&tab.unit_empty[s]), 1);
         for (int s = 0; s < 2; ++s) bar_init(smem_addr(&tab.acc_full[s]), 1), bar_init(smem_addr(&tab.acc_empty[s]), kEpilogueWarps);
         bar_init(smem_addr(&tab.mid_full), 1);
+        bar_init(smem_addr(&tab.done), 1);
         bar_init(smem_addr(&tab.mid_ready), kEpilogueWarps);
         bar_init(smem_addr(&tab.mid_ready_all), split * kEpilogueWarps);
         bar_init(smem_addr(&tab.ex_full), split * kEpilogueWarps);
@@ -393,10 +394,10 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
     const uint32_t tmem = warp > 0 ? tab.tmem_slot : 0u;
     const uint32_t full0 = smem_addr(tab.full), empty0 = smem_addr(tab.empty), unit_full0 = smem_addr(tab.unit_full), unit_empty0 = smem_addr(tab.unit_empty);
 
+    int s = 0, phase = 1, sent = 0, u = 0, uphase = 1, usent = 0;            // copies: the next places of the two rings, and how many were sent
     if (warp == 0 && elect_one()) {
         // ---- weights
         const uint32_t bytes = (uint32_t)((BACK ? chunks * 8192 : r16 * 128) + (boxes ? quarters * 4096 : 0));
-        int s = 0, phase = 1, sent = 0;
         bool ok = true;
         for (int k = k_from; k < k_to; ++k) {
             if (!(ok = bar_wait(empty0 + 8 * s, phase, gave_up))) break;
@@ -420,17 +421,9 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
             }
             if (++s == stages) s = 0, phase ^= 1;
         }
-        if (!ok) {                                                           // gave up: let the copies in flight land
-            for (int i = min(sent, stages); i > 0; --i) {
-                int none = 0;
-                if (s == 0) s = stages, phase ^= 1;
-                --s;
-                bar_wait(full0 + 8 * s, phase ^ 1, &none);
-            }
-        } else if (blocks) {
+        if (ok && blocks) {
             // ---- the second weights, once the ring's memory is free
             ok = bar_wait(smem_addr(&tab.mid_full), 0, gave_up);
-            int u = 0, uphase = 1, usent = 0;
             for (int b = b_from; ok && b < b_to; ++b)
                 for (int c = 0; c < chunks; ++c) {
                     if (!(ok = bar_wait(unit_empty0 + 8 * u, uphase, gave_up))) break;
@@ -444,13 +437,6 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
                     }
                     ++usent;
                     if (++u == units) u = 0, uphase ^= 1;
-                }
-            if (!ok)
-                for (int i = min(usent, units); i > 0; --i) {
-                    int none = 0;
-                    if (u == 0) u = units, uphase ^= 1;
-                    --u;
-                    bar_wait(unit_full0 + 8 * u, uphase ^ 1, &none);
                 }
         }
     } else if (warp == 1 && elect_one()) {
@@ -743,6 +729,25 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
     if (split > 1 && warp < 2) cluster_wait();
     tmem_fence_before();
     __syncthreads();
+    if (tab.gave_up) {
+        // Whoever gave up: copies may be on their way into this CTA's memory, and products may read it.
+        const auto land = [](uint32_t bars, int places, int at, int parity, int n) {
+            for (n = min(n, places); n > 0; --n) {
+                int none = 0;
+                if (at == 0) at = places, parity ^= 1;
+                --at;
+                bar_wait(bars + 8 * at, parity ^ 1, &none);
+            }
+        };
+        land(full0, stages, s, phase, sent);
+        land(unit_full0, units, u, uphase, usent);
+        if (warp == 1 && elect_one()) {
+            int none = 0;
+            mma_commit<1>(smem_addr(&tab.done));
+            bar_wait(smem_addr(&tab.done), 0, &none);
+        }
+        __syncthreads();
+    }
     if (split > 1) cluster_sync();                                           // the others read from this CTA's memory and, where it gave up, may still write to it
     tmem_fence_after();
     if (warp == 1) tmem_free<1>(tmem, 2 * kBlockColumns);
@@ -796,7 +801,7 @@ __global__ void __launch_bounds__(grad_threads(STAGES), STAGES == 4 ? 2 : 1)
 adapter_grad_kernel(const GradArgs a, const __grid_constant__ GradMaps maps)
 {
     extern __shared__ char raw[];
-    __shared__ uint64_t full_[STAGES], empty_[STAGES], acc_full_[2], acc_empty_[2], item_full_[kGradAhead], item_empty_[kGradAhead];
+    __shared__ uint64_t full_[STAGES], empty_[STAGES], acc_full_[2], acc_empty_[2], item_full_[kGradAhead], item_empty_[kGradAhead], done_;
     __shared__ GradItem items_[kGradAhead];
     __shared__ uint32_t tmem_slot;
     __shared__ int gave_up_, last_;
@@ -815,6 +820,7 @@ adapter_grad_kernel(const GradArgs a, const __grid_constant__ GradMaps maps)
         for (int s = 0; s < 2; ++s) bar_init(smem_addr(&acc_full_[s]), 1), bar_init(smem_addr(&acc_empty_[s]), kGradEpilogueWarps);
         for (int s = 0; s < kGradAhead; ++s)
             bar_init(smem_addr(&item_full_[s]), 1), bar_init(smem_addr(&item_empty_[s]), 1 + kGradEpilogueWarps + 2 * STAGES);
+        bar_init(smem_addr(&done_), 1);
         gave_up_ = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -838,6 +844,7 @@ adapter_grad_kernel(const GradArgs a, const __grid_constant__ GradMaps maps)
         return t.more != 0;
     };
 
+    uint32_t boxes = 0, boxes_phase = 0;                                     // where this thread's last boxes arrive; 0: it sent none
     if (warp == 1 + kGradEpilogueWarps) {
         // ---- items: the first is the CTA's own, the others who comes first gets
         if (elect_one()) {
@@ -872,7 +879,7 @@ adapter_grad_kernel(const GradArgs a, const __grid_constant__ GradMaps maps)
         const uint32_t full = full0 + 8 * s, dst = ring + s * stage_bytes, at = dst + (piece >> 3) * 8192;
         const uint32_t at_even = at + swizzled(line, piece & 7), at_odd = at + swizzled(line + 4, piece & 7);
         int phase = 1, skip = s;                                             // stages until this place's next one
-        bool ok = true, sent = false;
+        bool ok = true;
         while (ok && next(true)) {
             const int features = t.up ? a.N : a.H;
             const bool live = t.m0 + piece * 8 < features, real = piece * 8 < a.rank, plain = a.index == nullptr;
@@ -890,7 +897,7 @@ adapter_grad_kernel(const GradArgs a, const __grid_constant__ GradMaps maps)
                             tma_load<1>(dst, t.up ? &maps.dy : &maps.x, t.m0, row, 0, full);
                             tma_load<1>(dst + 8192, t.up ? &maps.dy : &maps.x, t.m0 + 64, row, 0, full);
                             for (int c = 0; c < chunks; ++c) tma_load<1>(dst + kLines + c * 8192, t.up ? &maps.mid : &maps.dmid, 64 * c, row, 0, full);
-                            sent = true;
+                            boxes = full;
                         } else {
                             bar_arrive(full);
                         }
@@ -926,10 +933,7 @@ adapter_grad_kernel(const GradArgs a, const __grid_constant__ GradMaps maps)
             skip = k - t.p.k_to;
         }
         copy_wait<0>();
-        if (!ok && sent) {                                                   // gave up: let the last boxes land
-            int none = 0;
-            bar_wait(full, phase, &none);
-        }
+        boxes_phase = phase;
     } else if (warp == 0 && elect_one()) {
         // ---- products
         int s = 0, phase = 0, used = 0;
@@ -1064,6 +1068,15 @@ adapter_grad_kernel(const GradArgs a, const __grid_constant__ GradMaps maps)
     __syncwarp();
     tmem_fence_before();
     __syncthreads();
+    if (gave_up_) {                                                          // whoever did: copies and products may be under way
+        int none = 0;
+        if (boxes) bar_wait(boxes, boxes_phase, &none);
+        if (warp == 0 && elect_one()) {
+            mma_commit<1>(smem_addr(&done_));
+            bar_wait(smem_addr(&done_), 0, &none);
+        }
+        __syncthreads();
+    }
     tmem_fence_after();
     if (warp == 0) tmem_free<1>(tmem, 2 * a.columns);
     if (threadIdx.x == 0 && gave_up_ && a.status) atomicOr(a.status, EP_STATUS_TIMEOUT);

@@ -61,3 +61,16 @@ def test_a_block_of_a_cluster_leaves_when_all_are_done():
     text = _kernel("rank_kernel")
     end = text[text.rindex("__syncthreads();"):]
     assert "if (split > 1) cluster_sync();" in end and "return;" not in text[text.index("cluster_arrive();"):]
+
+
+@pytest.mark.parametrize("kernel,flag,copies", [("rank_kernel", "tab.gave_up", ["land(full0, stages, s, phase, sent);", "land(unit_full0, units, u, uphase, usent);"]),
+                                                ("adapter_grad_kernel", "gave_up_", ["if (boxes) bar_wait(boxes, boxes_phase, &none);"])])
+def test_nothing_is_under_way_when_a_block_exits(kernel, flag, copies):
+    """Copies into a block's memory and products that read it are waited for whoever gave up, which the thread that issued them may not know
+    before all have met."""
+    text = _kernel(kernel)
+    at = text.index("if (%s) {" % flag)
+    block = _block(text, at)
+    assert re.search(r"__syncthreads\(\);\s*$", text[:at]) and re.search(r"__syncthreads\(\);\s*}$", block)
+    assert all(c in block for c in copies) and "mma_commit" in block and at < text.index("tmem_free")
+    assert "&none" not in text[:at]                                      # no thread decides that for itself
