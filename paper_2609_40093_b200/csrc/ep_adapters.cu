@@ -136,7 +136,7 @@ struct PlanArgs {
     int A, piece, tiles, ctas;            // piece: stages of a piece at least, where an adapter has more
     int counters;
     int *arrived;                         // [counters], to be zeroed
-    int *pieces;                          // [2]: pieces with entries, and all
+    int *pieces;                          // how many there are
     GradPiece *list;                      // NULL: no plan
     int32_t *status;
 };
@@ -186,7 +186,7 @@ __device__ void plan_pieces(const PlanArgs &a, PlanTables &tab)
     if (threadIdx.x == 0 && a.status && (tab.entries > (unsigned long long)a.entries || __ldg(a.offsets + a.A) > a.entries))
         atomicOr(a.status, EP_STATUS_CAPACITY);
     if (tab.entries > (unsigned long long)a.entries) {                       // offsets that decrease: the list has no room for what they name
-        if (threadIdx.x == 0) a.pieces[0] = 0, a.pieces[1] = 0;
+        if (threadIdx.x == 0) *a.pieces = 0;
         return;
     }
     most = __reduce_max_sync(kFullMask, most), sum = __reduce_add_sync(kFullMask, sum);
@@ -232,9 +232,7 @@ __device__ void plan_pieces(const PlanArgs &a, PlanTables &tab)
         run[i] = start;
         start += v;
     }
-    if (threadIdx.x == kThreads - 1) a.pieces[1] = start;
-    __syncthreads();
-    if (threadIdx.x == 0) a.pieces[0] = tab.bins[kGradBins * kThreads];
+    if (threadIdx.x == kThreads - 1) *a.pieces = start;
     __syncthreads();
     for (int e = from; e < to; ++e) {
         const int n = tab.stages[e], of = quotient_up(n, piece), begin = begin_of(e), count = max(0, begin_of(e + 1) - begin);
@@ -267,16 +265,6 @@ struct RankArgs {
     int in, out_features, rank, A, width; // width: rows of a tile at most
     int split, copies;                    // CTAs of a cluster, that share the contracted features; clusters that share the output's blocks
 };
-
-__device__ __forceinline__ void unpack8(const uint4 &v, float (&f)[8])
-{
-    f[0] = bf16_lo(v.x), f[1] = bf16_hi(v.x), f[2] = bf16_lo(v.y), f[3] = bf16_hi(v.y);
-    f[4] = bf16_lo(v.z), f[5] = bf16_hi(v.z), f[6] = bf16_lo(v.w), f[7] = bf16_hi(v.w);
-}
-__device__ __forceinline__ uint4 pack8(const float (&f)[8])
-{
-    return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
-}
 
 // BACK: the weights are read along the other axis (up for the first product, down for the second), and the scale goes to `mid`.
 template <bool BACK>
@@ -320,15 +308,7 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
             sum += quotient_up(max(0, end - begin), a.width);
             begin = end;
         }
-        int scan = sum;
-        for (int d = 1; d < 32; d <<= 1) {
-            const int v = __shfl_up_sync(kFullMask, scan, d);
-            if (lane >= d) scan += v;
-        }
-        if (lane == 31) warp_sum[warp] = scan;
-        __syncthreads();
-        int run = scan - sum;
-        for (int w = 0; w < warp; ++w) run += warp_sum[w];
+        int run = block_scan(sum, warp_sum);
         if (tile >= run && tile < run + sum) {                               // one thread: the tile is one of its adapters'
             begin = first;
             for (int i = from; i < to; ++i) {
@@ -760,8 +740,8 @@ rank_kernel(const RankArgs a, const PlanArgs plan, const __grid_constant__ CUten
 // ddown or dup. Items are dealt out round by round, the longest pieces first, a piece's feature tiles next to each other: what runs at
 // the same time reads the same rows (equal runs of work that end inside items balance better, but take the rows apart: dup of 32768 rows
 // on 128 adapters alike 33 us instead of 15) and has the same length. The parts of an adapter with several pieces go to the workspace in
-// fp32, and who comes last adds them in their order, so that the bits are the same every time. One warp issues the products, eight
-// bring entries, four empty the accumulators, of which there are two, so that an item's results leave under the next one's products.
+// fp32, and who comes last adds them in their order, so that the bits are the same every time. One warp issues the products, two
+// for each stage bring entries, four empty the accumulators, of which there are two, so that an item's results leave under the next one's products.
 constexpr int kGradEpilogueWarps = 4;
 constexpr int grad_threads(int stages) { return 32 * (2 + kGradEpilogueWarps + 2 * stages); }     // one each for the products and the items, two for each stage
 constexpr int kGradAhead = 4;             // items that are known ahead
@@ -770,15 +750,15 @@ constexpr int kGradColumns = 16;          // of them at a time
 constexpr int kGradOutBytes = kGradColumns * kGradLd * 4;
 
 struct GradArgs {
-    const int32_t *offsets, *index;
+    const int32_t *index;
     const float *scale;
     const uint16_t *x, *dmid, *dy, *mid;
     uint16_t *ddown, *dup;
     int32_t *status;
     float *parts;                         // [parts of split adapters][feature tile][r16][128]
     int *arrived;                         // [parts of split adapters][feature tile] zeros: how many parts are there, at an adapter's first
-    long long rows, entries;
-    int H, N, rank, A;
+    long long rows;
+    int H, N, rank;
     int tiles_down, tiles_up;             // feature tiles of an adapter's ddown (0: not wanted) and dup
     int *counter;                         // 0: items handed out beyond the CTAs' first
     const int *pieces;                    // the plan
@@ -848,7 +828,7 @@ adapter_grad_kernel(const GradArgs a, const __grid_constant__ GradMaps maps)
     if (warp == 1 + kGradEpilogueWarps) {
         // ---- items: the first is the CTA's own, the others who comes first gets
         if (elect_one()) {
-            const int tiles = a.tiles_down + a.tiles_up, all = __ldcg(a.pieces + 1) * tiles;
+            const int tiles = a.tiles_down + a.tiles_up, all = __ldcg(a.pieces) * tiles;
             for (int i = blockIdx.x;;) {
                 GradItem it = {};
                 if (i < all) {
@@ -1220,9 +1200,9 @@ GradPlan plan_grads(const ep_adapter_t &m)
     p.stages = chunks == 1 ? 4 : 6;                                          // two CTAs on an SM, or one
     p.smem = 1024 + kGradOutBytes + p.stages * stage;
     const int64_t most = chunks == 1 ? kGradMost : kGradMost / 2, items = pieces * tiles;
-    p.ctas = (int)(items < most ? items : most);
+    p.ctas = (int)(items < most ? items : most);                             // below 2^31: 4096 adapters x 2^18 tiles at most, and some 900 for the cuts
     p.counters = 1 + split * tiles;
-    p.counter_bytes = up256((size_t)p.counters * 4 + 8);
+    p.counter_bytes = up256((size_t)p.counters * 4 + 4);
     p.list_bytes = up256((size_t)pieces * sizeof(GradPiece));
     p.dmid_bytes = up256((size_t)m.entries * m.rank * 2);
     p.parts_bytes = (size_t)(split * tiles) * r16 * kGradFeatures * 4;
@@ -1288,11 +1268,10 @@ extern "C" int ep_adapter_matmul_backward(const ep_adapter_t *m, const void *dy,
     PlanArgs pieces = {};
     if (ddown || dup) {
         const int64_t tiles = (ddown ? feature_tiles(m->in_features) : 0) + (dup ? feature_tiles(m->out_features) : 0);
-        if (((int64_t)m->num_adapters + 1) * (feature_tiles(m->in_features) + feature_tiles(m->out_features)) >= (int64_t(1) << 31) - 8192) return EP_ERR_INVALID_ARG;
         pieces.offsets = adapter_offsets, pieces.entries = m->entries;
         pieces.A = m->num_adapters, pieces.piece = plan.piece, pieces.tiles = (int)tiles, pieces.ctas = plan.ctas;
         pieces.counters = (int)plan.counters;
-        pieces.pieces = reinterpret_cast<int *>(ws), pieces.arrived = pieces.pieces + 2;
+        pieces.pieces = reinterpret_cast<int *>(ws), pieces.arrived = pieces.pieces + 1;
         pieces.list = reinterpret_cast<GradPiece *>(ws + plan.counter_bytes);
         pieces.status = status;
     }
@@ -1315,7 +1294,7 @@ extern "C" int ep_adapter_matmul_backward(const ep_adapter_t *m, const void *dy,
         if (rc != EP_OK) return rc;
     }
     GradArgs g = {};
-    g.offsets = adapter_offsets, g.index = row_index, g.scale = scale, g.status = status;
+    g.index = row_index, g.scale = scale, g.status = status;
     g.x = static_cast<const uint16_t *>(x), g.dmid = static_cast<const uint16_t *>(dmid);
     g.dy = static_cast<const uint16_t *>(dy), g.mid = static_cast<const uint16_t *>(mid);
     GradMaps maps = {};
@@ -1332,7 +1311,7 @@ extern "C" int ep_adapter_matmul_backward(const ep_adapter_t *m, const void *dy,
     g.ddown = static_cast<uint16_t *>(ddown), g.dup = static_cast<uint16_t *>(dup);
     g.pieces = pieces.pieces, g.list = pieces.list, g.counter = pieces.arrived, g.arrived = pieces.arrived + 1;
     g.parts = reinterpret_cast<float *>(static_cast<char *>(dmid) + plan.dmid_bytes);
-    g.rows = m->rows, g.entries = m->entries, g.H = m->in_features, g.N = m->out_features, g.rank = m->rank, g.A = m->num_adapters;
+    g.rows = m->rows, g.H = m->in_features, g.N = m->out_features, g.rank = m->rank;
     g.tiles_down = ddown ? feature_tiles(m->in_features) : 0;
     g.tiles_up = dup ? feature_tiles(m->out_features) : 0;
     const int r16 = (m->rank + 15) & ~15;

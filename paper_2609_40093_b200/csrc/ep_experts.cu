@@ -205,16 +205,6 @@ struct Ring {
 // short and a tile's epilogue takes as long as its products: shared memory feeds both, and with fp32 words the dweight mode
 // took 220 us at 128 experts of 1024 x 2048 and 32768 rows, with pairs 195. (Stored straight from the accumulators' order,
 // 2 bytes a lane, a column took ten instructions.) Rows are 36 words apart: 16-byte reads of eight lanes fall on all banks.
-__device__ __forceinline__ void unpack8(const uint4 &v, float (&f)[8])
-{
-    f[0] = bf16_lo(v.x), f[1] = bf16_hi(v.x), f[2] = bf16_lo(v.y), f[3] = bf16_hi(v.y);
-    f[4] = bf16_lo(v.z), f[5] = bf16_hi(v.z), f[6] = bf16_lo(v.w), f[7] = bf16_hi(v.w);
-}
-__device__ __forceinline__ uint4 pack8(const float (&f)[8])
-{
-    return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
-}
-
 // z (8 features of one row) -> y, and pre if asked for.
 template <int ACT>
 __device__ __forceinline__ void finish8(const ProductArgs &a, float (&z)[8], const uint4 &operand, size_t at)
