@@ -190,11 +190,6 @@ struct Ring {
         ++stage, addr += bytes;
         if (stage == stages) stage = 0, phase ^= 1, addr = base;
     }
-    __device__ void back()
-    {
-        if (stage == 0) stage = stages, phase ^= 1;
-        --stage;
-    }
 };
 
 // ---- epilogues ---------------------------------------------------------------------------------------------------
@@ -254,7 +249,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ ColumnMaps map_b)
 {
     extern __shared__ char raw[];
-    __shared__ uint64_t full_[kMaxStages], empty_[kMaxStages], acc_full_[2], acc_empty_[2], ex_full_;
+    __shared__ uint64_t full_[kMaxStages], empty_[kMaxStages], acc_full_[2], acc_empty_[2], ex_full_, done_;
     __shared__ uint32_t tmem_slot;
     __shared__ int gave_up_;
     __shared__ int warp_sum[kThreads / 32];
@@ -279,6 +274,7 @@ product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, c
             bar_init(smem_addr(&acc_empty_[s]), kEpilogueWarps * CG);
         }
         if (SPLIT) bar_init(smem_addr(&ex_full_), split * kEpilogueWarps);
+        bar_init(smem_addr(&done_), 1);
         gave_up_ = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -329,6 +325,7 @@ product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, c
     constexpr bool kAMn = MODE != kForward, kBMn = MODE == kDweight;
     Tile t;
 
+    int in_flight = 0, next_stage = 0, next_phase = 0;                       // copies that may not have landed, and the ring's place behind them
     if (warp == 0 && elect_one()) {
         // ---- operands into the ring
         Ring ring(ring_base, stage_bytes, a.stages);
@@ -373,12 +370,7 @@ product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, c
                 ++sent;
             }
         }
-        if (!ok && rank == 0)                                                // gave up: let the copies in flight land
-            for (int i = min(sent, a.stages); i > 0; --i) {
-                int none = 0;
-                ring.back();
-                bar_wait(full0 + 8 * ring.stage, ring.phase, &none);
-            }
+        if (rank == 0) in_flight = min(sent, a.stages), next_stage = ring.stage, next_phase = ring.phase;      // a pair's are counted there
     } else if (warp == 1 && rank == 0 && elect_one()) {
         // ---- products
         Ring ring(ring_base, stage_bytes, a.stages);
@@ -413,7 +405,7 @@ product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, c
         const size_t ld = a.M;
         bool ok = walk.next(t) && t.all > 0;                                 // the grid has a cluster per tile: there is no second one
         if (ok && t.nk) {
-            ok = bar_wait(smem_addr(&acc_full_[0]), 0, gave_up);
+            ok = warp_wait(smem_addr(&acc_full_[0]), 0, gave_up);
             tmem_fence_after();
         }
         if (ok) {
@@ -430,7 +422,7 @@ product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, c
             }
             __syncwarp();
             if (lane < split) bar_arrive_cluster_release(in_cta(smem_addr(&ex_full_), lane));
-            ok = bar_wait<true>(smem_addr(&ex_full_), 0, gave_up);
+            ok = warp_wait<true>(smem_addr(&ex_full_), 0, gave_up);
         }
         const int width = ok ? (t.cols + split - 1) / split : 0;
         for (int i = thread; i < width * (kTileM / 8); i += 32 * kEpilogueWarps) {
@@ -479,7 +471,7 @@ product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, c
                     for (int i = 0; i < 4; ++i)
                         if (first + 8 * i < cols) r[i] = *reinterpret_cast<const uint4 *>(a.operand + corner + (first + 8 * i) * ld);
             }
-            if (!bar_wait(smem_addr(&acc_full_[acc]), (used >> 1) & 1, gave_up)) break;
+            if (!warp_wait(smem_addr(&acc_full_[acc]), (used >> 1) & 1, gave_up)) break;
             tmem_fence_after();
             const auto release = [&] {                                       // this warp has read its last column of the accumulator
                 tmem_fence_before();
@@ -556,6 +548,20 @@ product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a, c
     __syncwarp();
     tmem_fence_before();
     __syncthreads();
+    if (gave_up_) {                                                          // whoever did: copies and products may be under way
+        int none = 0;
+        for (; in_flight > 0; --in_flight) {
+            if (next_stage == 0) next_stage = a.stages, next_phase ^= 1;
+            --next_stage;
+            bar_wait(full0 + 8 * next_stage, next_phase, &none);
+            none = 0;
+        }
+        if (warp == 1 && rank == 0 && elect_one()) {
+            mma_commit<CG>(smem_addr(&done_));
+            bar_wait(smem_addr(&done_), 0, &none);
+        }
+        __syncthreads();
+    }
     if (CG == 2 || SPLIT) cluster_sync();                                    // the others' signals land in, and their reads come from, this CTA's memory
     tmem_fence_after();
     if (warp == 2) tmem_free<CG>(tmem, 2 * kAccColumns);

@@ -7,7 +7,7 @@ import re
 
 import pytest
 
-SOURCE = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2609_40093_b200", "csrc", "ep_adapters.cu")
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2609_40093_b200", "csrc")
 
 
 def _block(text, at):
@@ -21,8 +21,8 @@ def _block(text, at):
     raise AssertionError("unbalanced")
 
 
-def _kernel(name):
-    with open(SOURCE) as f:
+def _kernel(name, source="ep_adapters.cu"):
+    with open(os.path.join(CSRC, source)) as f:
         text = re.sub(r"//[^\n]*", "", f.read())
     text = re.sub(r'"(\\.|[^"\\])*"', '""', text)                       # braces of inline assembly
     return _block(text, text.index(name + "("))
