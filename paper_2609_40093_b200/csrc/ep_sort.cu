@@ -26,7 +26,9 @@ constexpr int kChunk = 8;   // rows in flight per column
 
 // CTAs per SM that the compiler leaves registers for. Left to itself it takes 125 and more where there are products, to have several
 // columns' loads under way in one thread; seven CTAs with 72 each and one column are faster (gather with products, 8192 tokens of
-// 1024 elements, 4 picks: 22.3 us with 72, 23.7 with 80, 25.5 with 64, 34.5 with 125).
+// 1024 elements, 4 picks: 22.3 us with 72, 23.7 with 80, 25.5 with 64, 34.5 with 125). More than 8 picks with products, 4096 tokens of 2048
+// elements, gather and spread: 12 picks 47 and 72 us with four CTAs, 58 and 81 with three, 44 and 69 with five; 24 picks 121 and 147 with three, 153 and
+// 147 with two, 143 and 135 with four. Without products, 12 picks: 37 and 37 with seven (gather) and twelve (spread), 41 and 37 with five and eight.
 constexpr int resident(bool spread, int chunks, bool dots) { return !dots ? (spread ? 12 : 7) : chunks == 1 ? 7 : chunks == 2 ? 4 : 3; }
 
 struct RowArgs {
@@ -317,6 +319,7 @@ int launch_group(const RowArgs &a, bool few_columns, cudaStream_t stream)
 template <template <int, int, bool> class Kernel, bool DOTS>
 int launch_chunks(const RowArgs &a, bool few_columns, cudaStream_t stream)
 {
+    // The kernel for 16 picks is there because the one for 32 is slower (12 picks of 4096 x 2048 with products: 90 us gather and 91 spread, 47 and 72).
     return a.K <= 8    ? launch_group<Kernel, 1, DOTS>(a, few_columns, stream)
            : a.K <= 16 ? launch_group<Kernel, 2, DOTS>(a, few_columns, stream)
                        : launch_group<Kernel, 4, DOTS>(a, few_columns, stream);
